@@ -80,7 +80,8 @@ typedef enum {
   F8_ERR_STATE = 10         /* chain used before f8_chain_prepare on that workspace        */
 } f8_status;
 
-typedef enum { F8_U8 = 0, F8_S8 = 1, F8_S32 = 2 } f8_dtype;
+/* The real types F8_F32 to F8_BF16 belong to the calls on tokens at the end of this file; the layers take the others. */
+typedef enum { F8_U8 = 0, F8_S8 = 1, F8_S32 = 2, F8_F32 = 3, F8_F16 = 4, F8_BF16 = 5 } f8_dtype;
 
 /* Per-call quantisation parameters (Eq. 2 / Eq. 9 / Eq. 6 in integer form). */
 typedef struct {
@@ -355,6 +356,111 @@ size_t f8_fold_work_doubles(int cout);
 f8_status f8_fold_conv_bn(const float *w, const float *gamma, const float *beta, const float *mu,
                           const float *sigma, const f8_fold_desc *d, int8_t *wq, int32_t *bq,
                           f8_stats *stats, double *work, void *stream);
+
+/* ---- tokens with scales from the data: serving a transformer layer in 8 bits ----
+ *
+ * The layers above have scales that are powers of two, fixed ahead of time.  The activations of a language model differ by orders
+ * of magnitude from token to token; the calls below give every token (row) a scale of its own when it comes:
+ *
+ *     scale = max(max_c |v_c| / 127, 2^-126),   code = round_half_even(v / scale)  (0 where v / scale is not a number),
+ *
+ * so a code c of that row stands for c * scale.  A row of zeros has codes 0; a row that holds a NaN or an infinity has a scale
+ * that is not finite, and every value or product made from it is NaN.
+ *
+ * Conventions: those at the head of this file.  Rows of a matrix lie `ld` elements apart and are contiguous inside; 16-byte
+ * aligned rows are read fastest, any row aligned to its element is taken.  Real tensors are F8_F32, F8_F16 or F8_BF16; sums,
+ * statistics and scales are 32 bits, a result is rounded once.  Nothing is allocated and nothing is kept between calls: scratch
+ * is the caller's (16-byte aligned, contents irrelevant before and after, one for each call that may overlap), so every call can
+ * be captured into a graph.  Results do not change from run to run.  No call copies to the host or waits. */
+
+/* Tokens [rows][cols] into 8 bits.  v = x, or with a gate v = act(gate) * x, element by element:
+ * act F8_ACT_SILU: g / (1 + e^-g); F8_ACT_GELU: g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2; F8_ACT_NONE: g.
+ * y_type F8_S8: y holds the codes; y_type == x_type: the values code * scale.  scale [rows] (may be NULL where y holds values).
+ * 1 <= cols <= 65536.  y may be x or gate themselves (same type and ld), otherwise they must not overlap. */
+enum { F8_ACT_NONE = 0, F8_ACT_SILU = 1, F8_ACT_GELU = 2 };
+typedef struct {
+  int32_t rows, cols;
+  int32_t x_type, y_type, act;
+  int64_t ldx, ldg, ldy;             /* elements; ldg is that of the gate */
+} f8_quant_tokens_desc;
+f8_status f8_quant_tokens(const void *x, const void *gate, void *y, float *scale, const f8_quant_tokens_desc *d, void *stream);
+
+/* The residual stream between two blocks and the norms on both sides, over rows of `cols` (1 .. 65536):
+ *     u = post(a),   r = res_scale * res + gate * u,   y = pre(r)
+ * post and pre are F8_NORM_NONE, F8_NORM_RMS  v / sqrt(mean v^2 + eps) * w + b  or F8_NORM_LAYER  (v - mean v) / sqrt(mean (v -
+ * mean v)^2 + eps) * w + b; w and b [cols] may be NULL (1 and 0), in w_type (F8_F32 or `type`).  a, res, gate, res_out and y are
+ * in `type`; y_type F8_S8 gives y as codes with their scale [rows] instead.  res NULL: r = gate * u.  gate NULL: 1; otherwise row
+ * t uses row t / gate_rows of it (gate_rows = rows: one gate per channel; the tokens of a sequence: one per sequence).  res_out
+ * (r, rounded where it is stored; y comes from the unrounded one) or y may be NULL, not both.  res_out and y may be a or res
+ * themselves (same type and ld). */
+enum { F8_NORM_NONE = 0, F8_NORM_RMS = 1, F8_NORM_LAYER = 2 };
+typedef struct {
+  int32_t rows, cols;
+  int32_t type, y_type, w_type;
+  int32_t post, pre, gate_rows;
+  float post_eps, pre_eps, res_scale;
+  int64_t lda, ldr, ldg, ldo, ldy;   /* elements: a, res, gate, res_out, y */
+} f8_norm_tokens_desc;
+f8_status f8_norm_tokens(const void *a, const void *res, const void *post_w, const void *post_b, const void *gate, const void *pre_w,
+                         const void *pre_b, void *res_out, void *y, float *scale, const f8_norm_tokens_desc *d, void *stream);
+
+/* Product of 8-bit tokens x [M][K] and 8-bit weights w [N][K]:
+ *     y[m][n] = sx[m] * sw[n] * sum_k x[m][k] w[n][k] + bias[n]
+ * with the sum exact in 32 bits; bias [N] float or NULL; y in y_type (real).  1 <= K <= F8_LINEAR_MAX_K.  x_type is F8_S8. */
+#define F8_LINEAR_MAX_K 131071
+typedef struct {
+  int32_t M, N, K;
+  int32_t x_type, y_type;
+  int64_t ldx, ldw, ldy;             /* elements */
+} f8_linear_desc;
+f8_status f8_linear_scaled(const int8_t *x, const float *sx, const int8_t *w, const float *sw, const float *bias, void *y,
+                           const f8_linear_desc *d, void *stream);
+/* The same from real tokens x [M][K] (x_type real, K <= 65536), quantised as by f8_quant_tokens.  The workspace holds their codes
+ * and scales: f8_linear_workspace_bytes(M, K) bytes. */
+size_t f8_linear_workspace_bytes(int M, int K);
+f8_status f8_linear_tokens(const void *x, const int8_t *w, const float *sw, const float *bias, void *y, const f8_linear_desc *d,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* A cache of keys and values in pages of page_size tokens.  Element (page, place, head, i) lies at page * page_stride + place *
+ * token_stride + head * head_stride + i of its array (elements; the strides may order heads and places either way), and in an
+ * 8-bit cache its scale at page * scale_page + place * scale_token + head * scale_head.  Keys and values have an array each
+ * (and a scale array each, scales not negative) of the same layout.  type F8_S8, F8_F16 or F8_BF16; dim a multiple of 16 up to
+ * 256; offsets may pass 32 bits. */
+typedef struct {
+  int32_t type;
+  int32_t pages, page_size, heads, dim;
+  int64_t page_stride, token_stride, head_stride;
+  int64_t scale_page, scale_token, scale_head;
+} f8_kv_layout;
+
+/* Keys and values of new tokens, k and v [tokens][heads][dim] (`type` real; strides in elements, dim contiguous), into the cache:
+ * token t goes to page slots[t] / page_size, place slots[t] % page_size.  An 8-bit cache takes a row's codes and scale, a 16-bit
+ * one its rounded values.  Negative slots and slots past the last page are skipped; no two tokens may share a slot. */
+typedef struct {
+  int32_t tokens, type;
+  int64_t k_token, k_head, v_token, v_head;
+} f8_kv_append_desc;
+f8_status f8_kv_append(const void *k, const void *v, const int64_t *slots, void *k_cache, void *v_cache, float *k_scale, float *v_scale,
+                       const f8_kv_layout *c, const f8_kv_append_desc *d, void *stream);
+
+/* Attention of one new token per request over its cached tokens: q and out [batch][q_heads][dim] in `type` (F8_F16 or F8_BF16; a
+ * 16-bit cache has the same type), query head h with cache head h / (q_heads / heads):
+ *     out = sum_t softmax_t(scale * q . k_t) v_t   over t < lens[b].
+ * Token t of request b lies in page table[b * table_ld + t / page_size], place t % page_size.  lens are clamped to 0 .. max_len,
+ * which the caller bounds ahead of the launch (max_len <= table_cols * page_size); a request without tokens gives zeros.  A table
+ * entry outside 0 .. pages - 1 takes its tokens out of the sums.  k_cache, v_cache and their strides are multiples of 16 bytes.
+ * Workspace: f8_attend_workspace_bytes(batch, q_heads, heads, dim, max_len) bytes, which may be 0 (then it may be NULL). */
+typedef struct {
+  int32_t batch, q_heads, type;
+  int32_t max_len, table_cols;
+  float scale;
+  int64_t table_ld;                  /* entries */
+  int64_t q_token, q_head, o_token, o_head;
+} f8_attend_desc;
+size_t f8_attend_workspace_bytes(int batch, int q_heads, int kv_heads, int dim, int max_len);
+f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cache, const float *k_scale, const float *v_scale,
+                          const int32_t *table, const int32_t *lens, void *out, const f8_kv_layout *c, const f8_attend_desc *d,
+                          void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---- helpers (host side, set-up only) ---- */
 

@@ -13,7 +13,7 @@ import torch
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libf8.so")
 
-F8_U8, F8_S8, F8_S32 = 0, 1, 2
+F8_U8, F8_S8, F8_S32, F8_F32, F8_F16, F8_BF16 = 0, 1, 2, 3, 4, 5
 F8_OP_CONV, F8_OP_DWCONV, F8_OP_MAXPOOL, F8_OP_GPOOL = 0, 1, 2, 3
 _TYPES = {"u8": F8_U8, "s8": F8_S8, "s32": F8_S32}
 _OPS = {"conv": F8_OP_CONV, "dwconv": F8_OP_DWCONV, "maxpool": F8_OP_MAXPOOL, "gpool": F8_OP_GPOOL}
@@ -29,6 +29,8 @@ EXPORTS = [
     "f8_tuning_set", "f8_tuning_get", "f8_mfma_i8_yardstick", "f8_mfma_i8_yardstick_operands",
     "f8_fix_quant_f32", "f8_fix_quant_code", "f8_pact_f32", "f8_pact_fix_f32", "f8_eta_fix", "f8_opt_fl",
     "f8_tensor_stats_f32", "f8_quant_error_f32", "f8_fold_work_doubles", "f8_fold_conv_bn",
+    "f8_quant_tokens", "f8_norm_tokens", "f8_linear_scaled", "f8_linear_workspace_bytes", "f8_linear_tokens",
+    "f8_kv_append", "f8_attend_workspace_bytes", "f8_attend_paged",
 ]
 F8_STATS_WORK_DOUBLES = 4096
 
@@ -71,6 +73,41 @@ class f8_fold_desc(ctypes.Structure):
     _fields_ = [("cout", ctypes.c_int32), ("k", ctypes.c_int32),
                 ("eta_in", ctypes.c_double), ("eta_out", ctypes.c_double),
                 ("fl_x", ctypes.c_int32), ("fl_w", ctypes.c_int32)]
+
+
+_i32, _i64, _f32c = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+
+
+class f8_quant_tokens_desc(ctypes.Structure):
+    _fields_ = [("rows", _i32), ("cols", _i32), ("x_type", _i32), ("y_type", _i32), ("act", _i32),
+                ("ldx", _i64), ("ldg", _i64), ("ldy", _i64)]
+
+
+class f8_norm_tokens_desc(ctypes.Structure):
+    _fields_ = [("rows", _i32), ("cols", _i32), ("type", _i32), ("y_type", _i32), ("w_type", _i32),
+                ("post", _i32), ("pre", _i32), ("gate_rows", _i32),
+                ("post_eps", _f32c), ("pre_eps", _f32c), ("res_scale", _f32c),
+                ("lda", _i64), ("ldr", _i64), ("ldg", _i64), ("ldo", _i64), ("ldy", _i64)]
+
+
+class f8_linear_desc(ctypes.Structure):
+    _fields_ = [("M", _i32), ("N", _i32), ("K", _i32), ("x_type", _i32), ("y_type", _i32),
+                ("ldx", _i64), ("ldw", _i64), ("ldy", _i64)]
+
+
+class f8_kv_layout(ctypes.Structure):
+    _fields_ = [("type", _i32), ("pages", _i32), ("page_size", _i32), ("heads", _i32), ("dim", _i32),
+                ("page_stride", _i64), ("token_stride", _i64), ("head_stride", _i64),
+                ("scale_page", _i64), ("scale_token", _i64), ("scale_head", _i64)]
+
+
+class f8_kv_append_desc(ctypes.Structure):
+    _fields_ = [("tokens", _i32), ("type", _i32), ("k_token", _i64), ("k_head", _i64), ("v_token", _i64), ("v_head", _i64)]
+
+
+class f8_attend_desc(ctypes.Structure):
+    _fields_ = [("batch", _i32), ("q_heads", _i32), ("type", _i32), ("max_len", _i32), ("table_cols", _i32), ("scale", _f32c),
+                ("table_ld", _i64), ("q_token", _i64), ("q_head", _i64), ("o_token", _i64), ("o_head", _i64)]
 
 
 _lib = None
@@ -131,6 +168,17 @@ def lib():
     L.f8_fold_work_doubles.argtypes = [i32]
     L.f8_fold_work_doubles.restype = sz
     L.f8_fold_conv_bn.argtypes = [vp] * 5 + [ctypes.POINTER(f8_fold_desc)] + [vp] * 5
+    P = ctypes.POINTER
+    L.f8_quant_tokens.argtypes = [vp] * 4 + [P(f8_quant_tokens_desc), vp]
+    L.f8_norm_tokens.argtypes = [vp] * 10 + [P(f8_norm_tokens_desc), vp]
+    L.f8_linear_scaled.argtypes = [vp] * 6 + [P(f8_linear_desc), vp]
+    L.f8_linear_workspace_bytes.argtypes = [i32, i32]
+    L.f8_linear_workspace_bytes.restype = sz
+    L.f8_linear_tokens.argtypes = [vp] * 5 + [P(f8_linear_desc), vp, sz, vp]
+    L.f8_kv_append.argtypes = [vp] * 7 + [P(f8_kv_layout), P(f8_kv_append_desc), vp]
+    L.f8_attend_workspace_bytes.argtypes = [i32] * 5
+    L.f8_attend_workspace_bytes.restype = sz
+    L.f8_attend_paged.argtypes = [vp] * 8 + [P(f8_kv_layout), P(f8_attend_desc), vp, sz, vp]
     L.f8_mfma_i8_yardstick.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double), vp]
     L.f8_mfma_i8_yardstick_operands.argtypes = [vp, i32, ctypes.c_uint32, ctypes.POINTER(ctypes.c_double), vp]
     L.f8_tuning_set.argtypes = [ctypes.c_char_p, i32]
@@ -396,6 +444,184 @@ def f8_fold_conv_bn(w, gamma, beta, mu, sigma, eta_in, eta_out, fl_x, fl_w=None,
                                  _ptr(_f32(sigma)), ctypes.byref(d), _ptr(wq), _ptr(bq), _ptr(buf), _ptr(work),
                                  _stream()), "f8_fold_conv_bn")
     return wq, bq, (None if buf is None else _read_stats(buf))
+
+
+# ---- tokens with scales from the data (real tensors in 32 or 16 bits on the GPU) --------------------
+
+_REAL = {torch.float32: F8_F32, torch.float16: F8_F16, torch.bfloat16: F8_BF16}
+_ACT = {None: 0, "silu": 1, "gelu": 2}
+_NORM = {None: 0, "rms": 1, "layer": 2}
+
+
+def _real(t):
+    kind = _REAL.get(t.dtype)
+    if kind is None:
+        raise TypeError("expected a float32, float16 or bfloat16 tensor, got %s" % t.dtype)
+    return kind
+
+
+def _matrix(t, shape=None):
+    """The row stride of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError("expected a matrix with contiguous rows, got shape %s, strides %s" % (tuple(t.shape), t.stride()))
+    if shape is not None and t.shape != shape:
+        raise ValueError("expected shape %s, got %s" % (tuple(shape), tuple(t.shape)))
+    # (a single row may report any stride)
+    return max(t.stride(0), t.shape[1])
+
+
+def _vector(t, n, dtype=None):
+    if t is None:
+        return None
+    if t.numel() != n or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+        raise ValueError("expected a contiguous vector of %d%s, got %s %s" % (n, " %s" % dtype if dtype else "", t.dtype, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _scratch(workspace, n, device):
+    """(tensor, its bytes) of at least n bytes; a tensor made here goes back to torch's allocator after the launch, which hands it
+    on in the order of the stream."""
+    if n == 0:
+        return None, 0
+    if workspace is None:
+        workspace = torch.empty(n, dtype=torch.uint8, device=device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def f8_quant_tokens(x, gate=None, act=None, values=False, out=None, scale=None):
+    """Tokens x [rows][cols] (times act(gate)) into 8 bits with a scale each: (codes int8, scale), or with values=True what the
+    codes stand for, in x's type: (values, scale)."""
+    rows, cols = x.shape
+    kind = _real(x)
+    if out is None:
+        out = torch.empty(rows, cols, dtype=x.dtype if values else torch.int8, device=x.device)
+    elif out.dtype != (x.dtype if values else torch.int8):
+        raise TypeError("out has to be %s" % (x.dtype if values else torch.int8))
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if gate is not None and gate.dtype != x.dtype:
+        raise TypeError("gate has to be in the type of x")
+    d = f8_quant_tokens_desc(rows, cols, kind, kind if values else F8_S8, _ACT[act], _matrix(x), 0 if gate is None else _matrix(gate, x.shape),
+                             _matrix(out, x.shape))
+    _check(lib().f8_quant_tokens(x.data_ptr(), _ptr(gate), out.data_ptr(), _vector(scale, rows, torch.float32), d, _stream()), "f8_quant_tokens")
+    return out, scale
+
+
+def f8_norm_tokens(a, res=None, post=None, post_w=None, post_b=None, gate=None, gate_rows=None, res_scale=1.0, pre="rms", pre_w=None,
+                   pre_b=None, eps=1e-6, post_eps=None, codes=False, keep_res=True, res_out=None, out=None, scale=None):
+    """r = res_scale * res + gate * post(a), y = pre(r) over rows [rows][cols].  post, pre: None, "rms" or "layer".  Returns
+    (r, y), or with codes=True (r, codes, scale); r is None with keep_res=False.  gate [n][cols]: gate_rows rows share a row of it."""
+    rows, cols = a.shape
+    kind = _real(a)
+    w = next((t for t in (post_w, post_b, pre_w, pre_b) if t is not None), a)
+    w_kind = _real(w)
+    for t in (post_w, post_b, pre_w, pre_b):
+        if t is not None and t.dtype != w.dtype:
+            raise TypeError("the weights have to be of one type")
+    for t in (res, gate, res_out, None if codes else out):
+        if t is not None and t.dtype != a.dtype:
+            raise TypeError("a, res, gate and the results have to be of one type")
+    ldg = 0
+    if gate is not None:
+        gate_rows = rows if gate_rows is None else int(gate_rows)
+        ldg = _matrix(gate)
+        if gate_rows < 1 or gate.shape[1] != cols or gate.shape[0] * gate_rows < rows:
+            raise ValueError("gate %s does not cover %d rows of %d, %d to a row of it" % (tuple(gate.shape), rows, cols, gate_rows))
+    if keep_res and res_out is None:
+        res_out = torch.empty(rows, cols, dtype=a.dtype, device=a.device)
+    if out is None:
+        out = torch.empty(rows, cols, dtype=torch.int8 if codes else a.dtype, device=a.device)
+    elif codes and out.dtype != torch.int8:
+        raise TypeError("out has to be int8")
+    if codes and scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=a.device)
+    d = f8_norm_tokens_desc(rows, cols, kind, F8_S8 if codes else kind, w_kind, _NORM[post], _NORM[pre], gate_rows or 0,
+                            eps if post_eps is None else post_eps, eps, res_scale, _matrix(a), 0 if res is None else _matrix(res, a.shape),
+                            ldg, 0 if res_out is None else _matrix(res_out, a.shape), _matrix(out, a.shape))
+    _check(lib().f8_norm_tokens(a.data_ptr(), _ptr(res), _vector(post_w, cols), _vector(post_b, cols), _ptr(gate), _vector(pre_w, cols),
+                                _vector(pre_b, cols), _ptr(res_out), out.data_ptr(), _vector(scale, rows, torch.float32) if codes else None,
+                                d, _stream()), "f8_norm_tokens")
+    return (res_out, out, scale) if codes else (res_out, out)
+
+
+def _linear_desc(x, w, y, y_dtype):
+    (M, K), N = x.shape, w.shape[0]
+    if w.dtype != torch.int8:
+        raise TypeError("the weights have to be int8")
+    if y is None:
+        y = torch.empty(M, N, dtype=y_dtype or torch.bfloat16, device=x.device)
+    d = f8_linear_desc(M, N, K, F8_S8 if x.dtype == torch.int8 else _real(x), _real(y), _matrix(x), _matrix(w, (N, K)), _matrix(y, (M, N)))
+    return d, y
+
+
+def f8_linear_scaled(x, sx, w, sw, bias=None, y=None, y_dtype=None):
+    """y[m][n] = sx[m] sw[n] sum_k x[m][k] w[n][k] (+ bias[n]) from int8 tokens x [M][K] and weights w [N][K]."""
+    if x.dtype != torch.int8:
+        raise TypeError("the tokens have to be int8")
+    d, y = _linear_desc(x, w, y, y_dtype)
+    _check(lib().f8_linear_scaled(x.data_ptr(), _vector(sx, d.M, torch.float32), w.data_ptr(), _vector(sw, d.N, torch.float32),
+                                  _vector(bias, d.N, torch.float32), y.data_ptr(), d, _stream()), "f8_linear_scaled")
+    return y
+
+
+def f8_linear_tokens(x, w, sw, bias=None, y=None, y_dtype=None, workspace=None):
+    """The same from real tokens, which are quantised on the way; y in x's type if nothing else is asked for."""
+    d, y = _linear_desc(x, w, y, y_dtype or x.dtype)
+    workspace, n = _scratch(workspace, lib().f8_linear_workspace_bytes(d.M, d.K), x.device)
+    _check(lib().f8_linear_tokens(x.data_ptr(), w.data_ptr(), _vector(sw, d.N, torch.float32), _vector(bias, d.N, torch.float32), y.data_ptr(),
+                                  d, _ptr(workspace), n, _stream()), "f8_linear_tokens")
+    return y
+
+
+def _kv_layout(k, v, k_scale, v_scale):
+    """Layout of a cache given as arrays [pages][page_size][heads][dim] (any strides with dim contiguous)."""
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or (k.stride(3) != 1 and k.shape[3] > 1):
+        raise ValueError("keys and values have to be two arrays [pages][page_size][heads][dim] of one layout, dim contiguous")
+    s = (0, 0, 0)
+    if k.dtype == torch.int8:
+        if k_scale is None or v_scale is None or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+            raise TypeError("an 8-bit cache has float32 scales")
+        if k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3] or k_scale.stride() != v_scale.stride():
+            raise ValueError("the scales have to be two arrays [pages][page_size][heads] of one layout")
+        s, kind = k_scale.stride(), F8_S8
+    else:
+        kind = _real(k)
+    return f8_kv_layout(kind, *k.shape, *k.stride()[:3], *s)
+
+
+def f8_kv_append(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None):
+    """Keys and values of new tokens, [tokens][heads][dim], into the cache's slots (page * page_size + place; negative: skipped)."""
+    c = _kv_layout(k_cache, v_cache, k_scale, v_scale)
+    if k.shape != v.shape or k.dtype != v.dtype or tuple(k.shape[1:]) != (c.heads, c.dim) or (c.dim > 1 and (k.stride(2) != 1 or v.stride(2) != 1)):
+        raise ValueError("k and v have to be [tokens][%d][%d] of one type, the last dimension contiguous" % (c.heads, c.dim))
+    d = f8_kv_append_desc(k.shape[0], _real(k), k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+    _check(lib().f8_kv_append(k.data_ptr(), v.data_ptr(), _vector(slots, k.shape[0], torch.int64), k_cache.data_ptr(), v_cache.data_ptr(),
+                              _ptr(k_scale), _ptr(v_scale), c, d, _stream()), "f8_kv_append")
+
+
+def f8_attend_paged(q, k_cache, v_cache, table, lens, k_scale=None, v_scale=None, scale=None, max_len=None, out=None, workspace=None):
+    """One new token per request, q [batch][q_heads][dim], over its lens[b] cached tokens, whose pages table [batch][cols] lists.
+    scale: of the scores (1 / sqrt(dim)); max_len: no request is longer (as long as the table allows)."""
+    c = _kv_layout(k_cache, v_cache, k_scale, v_scale)
+    B, H, D = q.shape
+    if D != c.dim or (D > 1 and q.stride(2) != 1):
+        raise ValueError("q has to be [batch][q_heads][%d], the last dimension contiguous" % c.dim)
+    if table.dtype != torch.int32 or table.shape[0] != B:
+        raise ValueError("the table has to be an int32 matrix [batch][cols]")
+    if out is None:
+        out = torch.empty(B, H, D, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape or out.dtype != q.dtype or (D > 1 and out.stride(2) != 1):
+        raise ValueError("out has to be like q")
+    cols = table.shape[1]
+    if max_len is None:
+        max_len = min(cols * c.page_size, 0x7fff0000)
+    L = lib()
+    workspace, n = _scratch(workspace, L.f8_attend_workspace_bytes(B, H, c.heads, D, max_len), q.device)
+    d = f8_attend_desc(B, H, _real(q), max_len, cols, D ** -0.5 if scale is None else scale, _matrix(table), q.stride(0), q.stride(1),
+                       out.stride(0), out.stride(1))
+    _check(L.f8_attend_paged(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), table.data_ptr(),
+                             _vector(lens, B, torch.int32), out.data_ptr(), c, d, _ptr(workspace), n, _stream()), "f8_attend_paged")
+    return out
 
 
 def out_hw(H, W, R, S, stride, pad):

@@ -1,0 +1,188 @@
+// The update of the residual stream between two blocks and the norms on both sides of it, in one pass over the rows:
+//
+//   u = norm_post(a)  (or a);   r = res_scale * res + gate * u;   y = norm_pre(r)  (or r),
+//   norm(v) = v / sqrt(mean v^2 + eps) * w + b                        (root mean square)
+//           = (v - mean v) / sqrt(mean (v - mean v)^2 + eps) * w + b  (layer)
+//
+// y in the type of a, or as 8-bit tokens (tokens_device.h) for the product behind.  r is rounded where it is stored; y comes
+// from the 32-bit one.  Bound by HBM: a row is held in registers in 32 bits from its first load to its last store, the sums run
+// over the workgroup in a fixed order, and the variance of a layer norm is that of the centred row, not a difference of moments.
+#include "tokens_device.h"
+#include "tokens_host.h"
+
+namespace f8 {
+namespace {
+
+struct NormParams {
+  const void *a, *res, *post_w, *post_b, *gate, *pre_w, *pre_b;
+  void *res_out, *y;
+  float *scale;
+  int64_t lda, ldr, ldg, ldo, ldy;
+  int rows, cols, post, pre, codes, w_f32;
+  float post_eps, pre_eps, res_scale, inv_cols;
+  FastDiv gate_rows;
+};
+
+// The weights are vectors of `cols` in the type of the rows or in 32 bits, read by every row (from cache).
+template <typename T, typename Map, bool VEC>
+__device__ __forceinline__ void load_weight(const void *w, int w_f32, int i, int t, int cols, float (&v)[8]) {
+  if (w_f32) load_piece<float, Map, VEC>(static_cast<const float *>(w), i, t, cols, v);
+  else load_piece<T, Map, VEC>(static_cast<const T *>(w), i, t, cols, v);
+}
+
+template <typename T, int TPR, int NV, bool VEC>
+__device__ __forceinline__ void normalise(float (&v)[NV][8], int form, float eps, const void *w, const void *b, const NormParams &p, int t,
+                                          float *lds) {
+  typedef RowMap<TPR, NV, VEC> Map;
+  constexpr int W = TPR / 64;
+  float mean = 0.0f;
+  if (form == F8_NORM_LAYER) {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += Map::col(i, j, t) < p.cols ? v[i][j] : 0.0f;
+    mean = row_sum<TPR>(s, lds) * p.inv_cols;
+  }
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float d = v[i][j] - mean;
+      v[i][j] = d;
+      s += Map::col(i, j, t) < p.cols ? d * d : 0.0f;
+    }
+  const float r = 1.0f / sqrtf(row_sum<TPR>(s, lds + W) * p.inv_cols + eps);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float g[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] *= r;
+    if (w) {
+      load_weight<T, Map, VEC>(w, p.w_f32, i, t, p.cols, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] *= g[j];
+    }
+    if (b) {
+      load_weight<T, Map, VEC>(b, p.w_f32, i, t, p.cols, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] += g[j];
+    }
+  }
+}
+
+template <typename T, int TPR, int NV, bool VEC>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_tokens_kernel(NormParams p) {
+  typedef RowMap<TPR, NV, VEC> Map;
+  constexpr int THREADS = TPR < 256 ? 256 : TPR, RPB = THREADS / TPR, W = TPR / 64;
+  __shared__ float lds[5 * (THREADS / 64)];          // a set of words for each of the five reductions of a row
+  const int row = blockIdx.x * RPB + (int)threadIdx.x / TPR, t = (int)threadIdx.x % TPR;
+  if (RPB > 1 && row >= p.rows) return;              // (waves on their own: no barrier below)
+  float v[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) load_piece<T, Map, VEC>(static_cast<const T *>(p.a) + row * p.lda, i, t, p.cols, v[i]);
+  if (p.post != F8_NORM_NONE) normalise<T, TPR, NV, VEC>(v, p.post, p.post_eps, p.post_w, p.post_b, p, t, lds);
+  if (p.gate) {
+    const T *gate = static_cast<const T *>(p.gate) + p.gate_rows.div((uint32_t)row) * p.ldg;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float g[8];
+      load_piece<T, Map, VEC>(gate, i, t, p.cols, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] *= g[j];
+    }
+  }
+  if (p.res) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float g[8];
+      load_piece<T, Map, VEC>(static_cast<const T *>(p.res) + row * p.ldr, i, t, p.cols, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = __builtin_fmaf(p.res_scale, g[j], v[i][j]);
+    }
+  }
+  if (p.res_out) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) store_piece<T, Map, VEC>(static_cast<T *>(p.res_out) + row * p.ldo, i, t, p.cols, v[i]);
+  }
+  if (!p.y) return;
+  if (p.pre != F8_NORM_NONE) normalise<T, TPR, NV, VEC>(v, p.pre, p.pre_eps, p.pre_w, p.pre_b, p, t, lds + 2 * W);
+  if (!p.codes) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) store_piece<T, Map, VEC>(static_cast<T *>(p.y) + row * p.ldy, i, t, p.cols, v[i]);
+    return;
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, Map::col(i, j, t) < p.cols ? magnitude(v[i][j]) : 0u);
+  const TokenScale s = token_scale(row_amax<TPR>(top, lds + 4 * W));
+  if (t == 0) p.scale[row] = s.scale;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    int q[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = code_of(v[i][j], s);
+    store_codes<Map, VEC>(static_cast<int8_t *>(p.y) + row * p.ldy, i, t, p.cols, q);
+  }
+}
+
+template <typename T, int TPR, int NV, bool VEC>
+void launch(const NormParams &p, hipStream_t s) {
+  constexpr int THREADS = TPR < 256 ? 256 : TPR, RPB = THREADS / TPR;
+  hipLaunchKernelGGL((norm_tokens_kernel<T, TPR, NV, VEC>), dim3((p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
+}
+
+template <typename T, bool VEC>
+void launch_row(const NormParams &p, hipStream_t s) {
+  if (p.cols <= 512) launch<T, 64, 1, VEC>(p, s);
+  else if (p.cols <= 1024) launch<T, 64, 2, VEC>(p, s);
+  else if (p.cols <= 2048) launch<T, 256, 1, VEC>(p, s);
+  else if (p.cols <= 4096) launch<T, 256, 2, VEC>(p, s);
+  else if (p.cols <= 8192) launch<T, 256, 4, VEC>(p, s);
+  else if (p.cols <= 16384) launch<T, 1024, 2, VEC>(p, s);
+  else launch<T, 1024, 8, VEC>(p, s);
+}
+
+template <typename T>
+f8_status launch_type(const NormParams &p, bool vec, hipStream_t s) {
+  vec ? launch_row<T, true>(p, s) : launch_row<T, false>(p, s);
+  return launch_status();
+}
+
+bool norm_form(int f) { return f == F8_NORM_NONE || f == F8_NORM_RMS || f == F8_NORM_LAYER; }
+
+}  // namespace
+}  // namespace f8
+
+using namespace f8;
+
+extern "C" f8_status f8_norm_tokens(const void *a, const void *res, const void *post_w, const void *post_b, const void *gate, const void *pre_w,
+                                    const void *pre_b, void *res_out, void *y, float *scale, const f8_norm_tokens_desc *d, void *stream) {
+  if (!d) return F8_ERR_NULL;
+  if (d->rows < 0 || d->cols < 1 || d->cols > ROW_MOST) return F8_ERR_SHAPE;
+  if (!real_type(d->type) || (d->y_type != F8_S8 && d->y_type != d->type) || (d->w_type != F8_F32 && d->w_type != d->type)) return F8_ERR_DTYPE;
+  if (!norm_form(d->post) || !norm_form(d->pre)) return F8_ERR_UNSUPPORTED;
+  if (!(d->post_eps >= 0.0f) || !(d->pre_eps >= 0.0f)) return F8_ERR_SHAPE;
+  if (d->lda < d->cols || (res && d->ldr < d->cols) || (res_out && d->ldo < d->cols) || (y && d->ldy < d->cols)) return F8_ERR_SHAPE;
+  if (gate && (d->gate_rows < 1 || d->ldg < d->cols)) return F8_ERR_SHAPE;
+  if (d->rows == 0) return F8_OK;
+  const bool codes = y && d->y_type == F8_S8;
+  if (!a || (!y && !res_out) || (codes && !scale)) return F8_ERR_NULL;
+  const size_t e = bytes_of(d->type), we = bytes_of(d->w_type), o = codes ? 1 : e, og = codes ? 8 : 16;
+  const void *rows[] = {a, res, gate, res_out}, *weights[] = {post_w, post_b, pre_w, pre_b};
+  const int64_t lds[] = {d->lda, d->ldr, d->ldg, d->ldo};
+  bool vec = aligned_to(y, og) && (!y || d->ldy * o % og == 0);
+  if (!aligned_to(y, o) || !aligned_to(scale, 4)) return F8_ERR_ALIGN;
+  for (int i = 0; i < 4; ++i) {
+    if (!aligned_to(rows[i], e) || !aligned_to(weights[i], we)) return F8_ERR_ALIGN;
+    vec = vec && aligned_to(rows[i], 16) && (!rows[i] || lds[i] * e % 16 == 0) && aligned_to(weights[i], 16);
+  }
+  const NormParams p{a, res, post_w, post_b, gate, pre_w, pre_b, res_out, y, scale, d->lda, d->ldr, d->ldg, d->ldo, d->ldy,
+                     d->rows, d->cols, d->post, d->pre, codes, d->w_type == F8_F32, d->post_eps, d->pre_eps, d->res_scale,
+                     1.0f / (float)d->cols, FastDiv((uint32_t)(gate ? d->gate_rows : 1))};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return d->type == F8_F32 ? launch_type<float>(p, vec, s) : d->type == F8_F16 ? launch_type<f16>(p, vec, s) : launch_type<bf16>(p, vec, s);
+}

@@ -1,0 +1,154 @@
+// Device-side pieces of the kernels on real-valued tokens: loads and stores of rows in 32 or 16 bits, reductions over the
+// threads of a row, and the 8-bit format of a token,
+//
+//   scale = max(max |v| / 127, 2^-126),   code = round_half_even(v / scale)  (0 where v / scale is not a number),
+//
+// which never divides by zero (a row of zeros has codes 0) and keeps what is not finite visible: a row with a NaN or an
+// infinity has a scale that is not finite, so that every value and every product made from it is NaN.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../../include/f8.h"
+#include "../f8_device.h"
+
+namespace f8 {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+constexpr int ROW_MOST = 65536;   // columns of a row that a workgroup holds in registers
+
+// How the elements of a row lie in its threads.  `TPR` threads share a row, each has NV pieces of 8.  VEC: the rows start on
+// 16 bytes, a piece is 8 neighbours (one or two 16-byte accesses).  Otherwise the 8 elements of a piece are TPR apart, so
+// that each access of a wave is one run of neighbours whatever the row's address.
+template <int TPR, int NV, bool VEC>
+struct RowMap {
+  static constexpr int most = TPR * NV * 8;
+  static __device__ __forceinline__ int col(int i, int j, int t) { return VEC ? (i * TPR + t) * 8 + j : (i * 8 + j) * TPR + t; }
+};
+
+template <typename T>
+__device__ __forceinline__ void unpack8(const v4i *raw, float (&v)[8]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = __int_as_float(raw[j >> 2][j & 3]);
+  } else if constexpr (__is_same(T, bf16)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] = __int_as_float(raw[0][j] << 16);
+      v[2 * j + 1] = __int_as_float(raw[0][j] & 0xffff0000);
+    }
+  } else {
+    typedef f16 h8 __attribute__((ext_vector_type(8)));
+    const h8 h = __builtin_bit_cast(h8, raw[0]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)h[j];
+  }
+}
+
+// 8 elements of piece i of a row into v; what lies past the row's end reads as 0.
+template <typename T, typename Map, bool VEC>
+__device__ __forceinline__ void load_piece(const T *row, int i, int t, int cols, float (&v)[8]) {
+  const int c = Map::col(i, 0, t);
+  if (VEC && c + 8 <= cols) {
+    v4i raw[2];
+    raw[0] = *reinterpret_cast<const v4i *>(row + c);
+    if (sizeof(T) == 4) raw[1] = *reinterpret_cast<const v4i *>(row + c + 4);
+    unpack8<T>(raw, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int e = Map::col(i, j, t);
+      v[j] = e < cols ? (float)row[e] : 0.0f;
+    }
+  }
+}
+
+template <typename T, typename Map, bool VEC>
+__device__ __forceinline__ void store_piece(T *row, int i, int t, int cols, const float (&v)[8]) {
+  const int c = Map::col(i, 0, t);
+  if (VEC && c + 8 <= cols) {
+    typedef T t8 __attribute__((ext_vector_type(8)));
+    t8 o;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = (T)v[j];
+    if constexpr (sizeof(T) == 4) {
+      const v4i *r = reinterpret_cast<const v4i *>(&o);
+      *reinterpret_cast<v4i *>(row + c) = r[0];
+      *reinterpret_cast<v4i *>(row + c + 4) = r[1];
+    } else {
+      *reinterpret_cast<v4i *>(row + c) = __builtin_bit_cast(v4i, o);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int e = Map::col(i, j, t);
+      if (e < cols) row[e] = (T)v[j];
+    }
+  }
+}
+
+template <typename Map, bool VEC>
+__device__ __forceinline__ void store_codes(int8_t *row, int i, int t, int cols, const int (&q)[8]) {
+  const int c = Map::col(i, 0, t);
+  if (VEC && c + 8 <= cols) {
+    const v2i o{(int)pack4(q[0], q[1], q[2], q[3]), (int)pack4(q[4], q[5], q[6], q[7])};
+    *reinterpret_cast<v2i *>(row + c) = o;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int e = Map::col(i, j, t);
+      if (e < cols) row[e] = (int8_t)q[j];
+    }
+  }
+}
+
+// Reductions over the TPR threads of a row, every thread gets the result; the order is fixed.  `lds`: a word for each wave, used
+// by one reduction at a time (a second one on the same words needs another set: see `turn`).
+template <int TPR, typename V, typename Op>
+__device__ __forceinline__ V reduce_row(V v, V *lds, Op op) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v = op(v, __shfl_xor(v, d));
+  if constexpr (TPR > 64) {
+    constexpr int W = TPR / 64;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) v = op(v, lds[w]);
+  }
+  return v;
+}
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float *lds) {
+  return reduce_row<TPR>(v, lds, [](float a, float b) { return a + b; });
+}
+// The largest magnitude by its bits: a NaN's bits lie above an infinity's, so one that is there wins.
+template <int TPR>
+__device__ __forceinline__ float row_amax(uint32_t bits, float *lds) {
+  return __uint_as_float(reduce_row<TPR>(bits, reinterpret_cast<uint32_t *>(lds), [](uint32_t a, uint32_t b) { return a > b ? a : b; }));
+}
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+struct TokenScale {
+  float scale, inv;
+};
+__device__ __forceinline__ TokenScale token_scale(float amax) {
+  float s = amax / 127.0f;
+  s = s < 1.17549435e-38f ? 1.17549435e-38f : s;   // (false for a NaN, which stays)
+  return TokenScale{s, 1.0f / s};
+}
+// v / scale, correctly rounded without a division for each element: the product with the reciprocal, corrected by its exact
+// remainder.  (One operation off in the last place would turn codes at ties.)
+__device__ __forceinline__ float over_scale(float v, const TokenScale &s) {
+  const float q = v * s.inv;
+  return __builtin_fmaf(__builtin_fmaf(-q, s.scale, v), s.inv, q);
+}
+__device__ __forceinline__ int code_of(float v, const TokenScale &s) {
+  const float q = __builtin_rintf(over_scale(v, s));
+  return q == q ? (int)q : 0;
+}
+
+}  // namespace f8
