@@ -1,0 +1,131 @@
+// Products of at most 16 tokens: the weights are the traffic, each byte of them is needed once.
+//
+// A workgroup takes 16 output channels, its eight waves a contiguous share of K each.  Weights go from memory straight into the
+// registers that are the row operand of the 16 x 16 x 64 matrix instruction (lane l: channel l % 16, 16 bytes of K), U slices of 64
+// columns in flight per wave; the tokens are the column operand, from L2 or, where they come as real numbers, from LDS: every
+// workgroup then quantises them itself while its first weights are on their way, which saves a launch.  The waves' 32-bit sums meet
+// in LDS by integer additions, whose order cannot matter.
+#include "linear.h"
+
+namespace f8 {
+namespace {
+
+constexpr int WAVES = 8, THREADS = 64 * WAVES, U = 8, HELD = LINEAR_FEW_HELD / WAVES;
+
+__device__ __forceinline__ v4i load16(const int8_t *p) {
+  v4i v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+
+// X: int8_t, or the real type of tokens that are quantised here.
+template <typename T, typename X>
+__global__ __launch_bounds__(THREADS) void linear_few_kernel(LinearParams p) {
+  constexpr bool REAL = sizeof(X) > 1;
+  __shared__ int sums[256];
+  __shared__ uint32_t tops[LINEAR_FEW];
+  __shared__ float scales[LINEAR_FEW];
+  extern __shared__ __attribute__((aligned(16))) int8_t codes[];        // [M][pitch]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int n0 = blockIdx.x * 16;
+  if (threadIdx.x < 256) sums[threadIdx.x] = 0;
+  const int slices = (p.K + 63) / 64, per = (slices + WAVES - 1) / WAVES, first = wave * per, last = min(slices, first + per);
+  // (channels and tokens past the end read the last one's row; their sums are not used)
+  const int8_t *w = p.w + min(n0 + c, p.N - 1) * p.ldw + g * 16;
+  const int m = min(c, p.M - 1), pitch = slices * 64 + 16;
+  auto whole = [&](int t) { return t + U <= last && (t + U) * 64 <= p.K; };
+  v4i fw[U];
+  if (whole(first)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) fw[u] = load16(w + (first + u) * 64);
+  }
+  if constexpr (REAL) {
+    const X *x = reinterpret_cast<const X *>(p.x);
+    if (threadIdx.x < LINEAR_FEW) tops[threadIdx.x] = 0;
+    __syncthreads();
+    // stretches of 512 columns of a row, a wave holds up to HELD of them between the maximum and the codes
+    const int stretches = (p.K + 511) / 512, tasks = p.M * stretches;
+    float v[HELD][8];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+      const int task = wave + WAVES * h;
+      if (task >= tasks) break;
+      const int r = task / stretches, k = (task - r * stretches) * 512 + lane * 8;
+      load_row8(x + r * p.ldx, k, p.K, p.x_vec, v[h]);
+    }
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+      const int task = wave + WAVES * h;
+      if (task >= tasks) break;
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[h][j]));
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+      if (lane == 0) atomicMax(&tops[task / stretches], top);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) {
+      const int task = wave + WAVES * h;
+      if (task >= tasks) break;
+      const int r = task / stretches, k = (task - r * stretches) * 512 + lane * 8;
+      const TokenScale s = token_scale(__uint_as_float(tops[r]));
+      if (k == 0) scales[r] = s.scale;
+      int q[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] = code_of(v[h][j], s);
+      if (k < slices * 64) *reinterpret_cast<v2i *>(codes + r * pitch + k) = v2i{(int)pack4(q[0], q[1], q[2], q[3]), (int)pack4(q[4], q[5], q[6], q[7])};
+    }
+  }
+  __syncthreads();
+  const int8_t *x = REAL ? codes + m * pitch + g * 16 : p.x + m * p.ldx + g * 16;
+  v4i acc{0, 0, 0, 0};
+  int t = first;
+  while (whole(t)) {
+    v4i fx[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) fx[u] = REAL ? *reinterpret_cast<const v4i *>(x + (t + u) * 64) : load16(x + (t + u) * 64);
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u], fx[u], acc, 0, 0, 0);
+    t += U;
+    if (whole(t)) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) fw[u] = load16(w + (t + u) * 64);
+    }
+  }
+  for (; t < last; ++t) {
+    const v4i a = load_row16(w - g * 16, true, t * 64 + g * 16, p.K);
+    const v4i b = REAL ? *reinterpret_cast<const v4i *>(x + t * 64) : load_row16(x - g * 16, true, t * 64 + g * 16, p.K);
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc, 0, 0, 0);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) atomicAdd(&sums[c * 16 + 4 * g + e], acc[e]);
+  __syncthreads();
+  if (threadIdx.x < 256) {
+    const int row = threadIdx.x / 16, n = n0 + threadIdx.x % 16;
+    if (row < p.M && n < p.N)
+      static_cast<T *>(p.y)[row * p.ldy + n] =
+          (T)__builtin_fmaf((float)sums[threadIdx.x] * (REAL ? scales[row] : p.sx[row]), p.sw[n], p.bias ? p.bias[n] : 0.0f);
+  }
+}
+
+template <typename T, typename X>
+f8_status launch(const LinearParams &p, hipStream_t s) {
+  const size_t lds = sizeof(X) > 1 ? (size_t)p.M * ((p.K + 63) / 64 * 64 + 16) : 0;
+  hipLaunchKernelGGL((linear_few_kernel<T, X>), dim3((p.N + 15) / 16), dim3(THREADS), lds, s, p);
+  return launch_status();
+}
+
+template <typename T>
+f8_status launch_type(const LinearParams &p, int x_type, hipStream_t s) {
+  return x_type == F8_S8 ? launch<T, int8_t>(p, s) : x_type == F8_F32 ? launch<T, float>(p, s) : x_type == F8_F16 ? launch<T, f16>(p, s) : launch<T, bf16>(p, s);
+}
+
+}  // namespace
+
+f8_status launch_linear_few(const LinearParams &p, int x_type, int y_type, hipStream_t s) {
+  return y_type == F8_F32 ? launch_type<float>(p, x_type, s) : y_type == F8_F16 ? launch_type<f16>(p, x_type, s) : launch_type<bf16>(p, x_type, s);
+}
+
+}  // namespace f8

@@ -4,60 +4,16 @@
 //
 // scaled in 32-bit floating point and rounded once to the type of y.
 //
-// linear_any_kernel takes any size, stride and alignment: 128 x 128 outputs per workgroup, weights as the row operand of the
-// 32 x 32 x 32 matrix instruction in the channel order of f8_device.h (weight_row), so that a lane ends with 16 neighbouring
-// channels of one token and stores them from its registers; operands go through registers into two LDS buffers.
-#include "tokens_device.h"
-#include "tokens_host.h"
+// Three kernels: at most 16 tokens, where the weights are the traffic (linear_few.hip); tiles through LDS for rows that start on 4
+// bytes (linear_tile.hip); and linear_any_kernel here for any stride and alignment: 128 x 128 outputs per workgroup, weights as the
+// row operand of the 32 x 32 x 32 matrix instruction in the channel order of f8_device.h (weight_row), so that a lane ends with 16
+// neighbouring channels of one token and stores them from its registers; operands go through registers into two LDS buffers.  It
+// takes 1.4 to 2.6 times as long as the tiles (1531 x 4096 x 5008 49 us against 35.5, 64 x 4096 x 4096 37 against 8.6, 8192 x 8192 x
+// 8192 857 against 462): unaligned 16-byte pieces, one K step of 64 ahead.
+#include "linear.h"
 
 namespace f8 {
 namespace {
-
-typedef int v16i __attribute__((ext_vector_type(16)));
-
-struct LinearParams {
-  const int8_t *x, *w;
-  const float *sx, *sw, *bias;
-  void *y;
-  int64_t ldx, ldw, ldy;
-  int M, N, K;
-};
-
-// 16 bytes of a row from column k on, at any address; past the row's end zeros.
-__device__ __forceinline__ v4i load_row16(const int8_t *row, bool real, int k, int K) {
-  v4i v{0, 0, 0, 0};
-  if (real && k + 16 <= K) {
-    __builtin_memcpy(&v, row + k, 16);
-  } else if (real) {
-    int8_t b[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) b[i] = k + i < K ? row[k + i] : 0;
-    __builtin_memcpy(&v, b, 16);
-  }
-  return v;
-}
-
-// The 16 channels n .. n + 15 of token m.
-template <typename T>
-__device__ __forceinline__ void store_scaled(const LinearParams &p, const v16i &acc, int m, int n, bool vec) {
-  if (m >= p.M || n >= p.N) return;
-  const float sx = p.sx[m];
-  T *y = static_cast<T *>(p.y) + m * p.ldy + n;
-  T o[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const bool real = n + i < p.N;
-    o[i] = (T)__builtin_fmaf((float)acc[i] * sx, real ? p.sw[n + i] : 0.0f, real && p.bias ? p.bias[n + i] : 0.0f);
-  }
-  if (vec && n + 16 <= p.N) {
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<v4i *>(y)[i] = reinterpret_cast<const v4i *>(o)[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (n + i < p.N) y[i] = o[i];
-  }
-}
 
 constexpr int ANY_TILE = 128, ANY_K = 64, ANY_PITCH = ANY_K + 16;
 
@@ -112,8 +68,8 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearParams p, int til
 }
 
 template <typename T>
-f8_status launch_linear(const LinearParams &p, hipStream_t s) {
-  const bool vec = aligned_to(p.y, 16) && p.ldy * sizeof(T) % 16 == 0;
+f8_status launch_any(const LinearParams &p, hipStream_t s) {
+  const bool vec = aligned_to(p.y, 16) && p.ldy * sizeof(T) % 16 == 0 && aligned_to(p.sw, 16) && aligned_to(p.bias, 16);
   const int64_t tm = (p.M + ANY_TILE - 1) / ANY_TILE, tn = (p.N + ANY_TILE - 1) / ANY_TILE;
   if (tm * tn > 0x7fffffff) return F8_ERR_UNSUPPORTED;
   hipLaunchKernelGGL(linear_any_kernel<T>, dim3((unsigned)(tm * tn)), dim3(256), 0, s, p, (int)tm, vec);
@@ -134,8 +90,30 @@ f8_status check_pointers(const void *x, const void *w, const float *sw, const fl
   return F8_OK;
 }
 
+// What linear_few_kernel takes: its weights at 5.9 TB/s, and every workgroup's reads of the tokens from L2 at 20.  Measured (us):
+// 1 x 4096 x 4096 5.5, 16 x 4096 x 4096 6.5, 1 x 16384 x 4096 13.8, 16 x 4096 x 16384 17.2; the best tile takes 8.0, 8.2, 18.5 and 12.6.
+float few_us(const LinearParams &p) {
+  const float bytes = (float)p.N * (float)p.K;
+  return 2.5f + bytes / 5.9e6f + bytes * (float)p.M / 16.0f / 20e6f;
+}
+
+// Whether linear_few_kernel also quantises the tokens.  A launch less is 2.3 us; every workgroup repeating the work costs about half of
+// that for each stretch of 512 columns that a wave holds, and as often as there are rounds of workgroups.  Two launches | one (us):
+// 1 x 4096 x 4096 8.4 | 6.4, 2 x 4096 x 4096 8.6 | 7.3, 4 x 2048 x 1000 5.7 | 4.9, 1 x 4096 x 16384 16.0 | 15.1, but 4 x 4096 x 4096
+// 8.9 | 9.4 and 2 x 4096 x 16384 16.2 | 18.6.
+bool few_quantises(int M, int N, int K) {
+  const int64_t stretches = (int64_t)M * ((K + 511) / 512);
+  return M <= LINEAR_FEW && stretches <= (N <= 8192 ? LINEAR_FEW_HELD : LINEAR_FEW_HELD / 2);
+}
+
 f8_status enqueue_linear(const LinearParams &p, int y_type, hipStream_t s) {
-  return y_type == F8_F32 ? launch_linear<float>(p, s) : y_type == F8_F16 ? launch_linear<f16>(p, s) : launch_linear<bf16>(p, s);
+  // tiles: rows on 4 bytes, and within reach of 31-bit offsets inside a tile
+  const bool tiles = aligned_to(p.x, 4) && aligned_to(p.w, 4) && p.ldx % 4 == 0 && p.ldw % 4 == 0 && p.ldx < (1 << 22) && p.ldw < (1 << 22);
+  float us = 0.0f;
+  const int tile = linear_tile_of(p.M, p.N, p.K, &us);
+  if (p.M <= LINEAR_FEW && (!tiles || few_us(p) < us)) return launch_linear_few(p, F8_S8, y_type, s);
+  if (tiles) return launch_linear_tile(p, y_type, tile, s);
+  return y_type == F8_F32 ? launch_any<float>(p, s) : y_type == F8_F16 ? launch_any<f16>(p, s) : launch_any<bf16>(p, s);
 }
 
 // Rows of codes in the workspace: whole 128 bytes, zeros behind the row's end.
@@ -158,7 +136,7 @@ f8_status f8_linear_scaled(const int8_t *x, const float *sx, const int8_t *w, co
   if (st != F8_OK) return st;
   if (!sx) return F8_ERR_NULL;
   if (!aligned_to(sx, 4)) return F8_ERR_ALIGN;
-  const LinearParams p{x, w, sx, sw, bias, y, d->ldx, d->ldw, d->ldy, d->M, d->N, d->K};
+  const LinearParams p{x, w, sx, sw, bias, y, d->ldx, d->ldw, d->ldy, d->M, d->N, d->K, 0};
   return enqueue_linear(p, d->y_type, static_cast<hipStream_t>(stream));
 }
 
@@ -178,13 +156,16 @@ f8_status f8_linear_tokens(const void *x, const int8_t *w, const float *sw, cons
   if (!workspace) return F8_ERR_NULL;
   if (!aligned_to(x, bytes_of(d->x_type)) || !aligned_to(workspace, 16)) return F8_ERR_ALIGN;
   if (workspace_bytes < f8_linear_workspace_bytes(d->M, d->K)) return F8_ERR_SHAPE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  LinearParams p{static_cast<const int8_t *>(x), w, nullptr, sw, bias, y, d->ldx, d->ldw, d->ldy, d->M, d->N, d->K,
+                 aligned_to(x, 16) && d->ldx * bytes_of(d->x_type) % 16 == 0};
+  if (few_quantises(d->M, d->N, d->K)) return launch_linear_few(p, d->x_type, d->y_type, s);
   const int64_t pitch = code_pitch(d->K);
   int8_t *codes = static_cast<int8_t *>(workspace);
   float *sx = reinterpret_cast<float *>(codes + d->M * pitch);
-  hipStream_t s = static_cast<hipStream_t>(stream);
   st = enqueue_quant_tokens(x, d->ldx, d->x_type, codes, pitch, (int)pitch, sx, d->M, d->K, s);
   if (st != F8_OK) return st;
-  const LinearParams p{codes, w, sx, sw, bias, y, pitch, d->ldw, d->ldy, d->M, d->N, d->K};
+  p.x = codes, p.sx = sx, p.ldx = pitch;
   return enqueue_linear(p, d->y_type, s);
 }
 
