@@ -2,8 +2,9 @@
 //
 //   s_t = scale * q . k_t,   p = softmax of s over the tokens of the request,   o = sum_t p_t v_t   (0 without tokens),
 //
-// query head h reads cache head h / G.  One workgroup takes a request, a cache head, up to 16 of the query heads that share it
-// and a stretch of its tokens; a second launch joins the stretches where there are several.
+// query head h reads cache head h / G.  A workgroup's unit of work is 128 tokens of a request, a cache head and up to 16 of the
+// query heads that share it; the units of all requests are dealt out evenly (see Runs), and a second launch joins the pairs that came
+// apart.
 //
 // Inside, a wave walks over tiles of 32 tokens on its own and keeps the running maximum, sum and output of its heads.  Both
 // products run on the matrix cores with 16 heads as columns, S^T = K Q^T and O^T = V^T P^T: a lane then owns one head, its
@@ -17,6 +18,11 @@
 // w_t = exp(s_t + log scale_t - m) with m the maximum of that sum, so that w is in [0, 1] whatever the scales are.  w is rounded
 // to 16 bits for the second product (as P is for 16-bit caches): relative 2^-12 (f16) or 2^-9 (bf16) of each weight, at random,
 // below the rounding of the 16-bit result.  Scores, maxima, sums and outputs are 32 bits.
+//
+// Bound by HBM: every cached byte is read once, in whole rows, one tile ahead per wave (131072 tokens of 8 heads, 277 MB: 67 us with
+// the second launch, 4.2 TB/s; 64 requests of up to 8192 tokens, 491 MB: 120 us, 4.1 TB/s; a large copy reaches 5.5).  The vector units
+// are a third busy (350 instructions a tile, most of them codes into f16).  Without the tile ahead the two took 97 and 239 us; with
+// the requests' lengths cut into equal stretches, a workgroup each, instead of units dealt out evenly, 68 and 167.
 #include <math.h>
 
 #include "tokens_device.h"
@@ -39,12 +45,53 @@ struct AttendParams {
   const float *k_scale, *v_scale;
   const int32_t *table, *lens;
   void *out;
-  float *part_o, *part_ml;                 // [batch][q_heads][splits][dim] and [..][2]
+  float *part_o, *part_ml;                 // [2 wgs][rows][dim] and [2 wgs][rows][2], rows = min(group, HEADS)
   int64_t qt, qh, ot, oh, page, token, head, spage, stoken, shead, table_ld;
-  int q_heads, group, dim, pages, max_len, splits, chunk;
+  int batch, kv_heads, group, chunks, dim, pages, max_len;
+  int wgs;                                 // 0: a workgroup to each pair
   FastDiv page_size;
   float scale;                             // of the scores, times log2 e
 };
+
+// How the work is dealt out.  A pair is a request and a cache head with up to 16 of its query heads; its units are rounds of a
+// workgroup's four waves over the request's tokens.  All pairs' units lie in a row, request by request, and each workgroup takes
+// an equal run of them, whatever the lengths are: a pair that a run does not hold whole is left in pieces for join_kernel, at most
+// two to a workgroup (slot 0 its first pair, slot 1 its last).  The lengths are only known on the device, so every workgroup adds
+// them up itself.
+constexpr int UNIT = WAVES * TILE;
+__device__ __forceinline__ int len_of(const AttendParams &p, int b) { return min(max(p.lens[b], 0), p.max_len); }
+__device__ __forceinline__ int units_of(const AttendParams &p, int b) { return (len_of(p, b) + UNIT - 1) / UNIT; }
+struct Runs {                                // equal runs of `total` units, the first `more` of them one longer
+  int64_t per, more;
+  __device__ __forceinline__ Runs(int64_t total, int wgs) : per(total / (uint32_t)wgs), more(total - per * wgs) {}
+  __device__ __forceinline__ int64_t start(int64_t i) const { return i * per + (i < more ? i : more); }
+  __device__ __forceinline__ int64_t of(int64_t unit) const {
+    const int64_t longer = more * (per + 1);
+    return unit < longer ? unit / (per + 1) : more + (unit - longer) / per;
+  }
+};
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+  return (int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+}
+
+// Two sums over a workgroup; `lds`: a pair of words per wave.
+template <int W>
+__device__ __forceinline__ void wg_sum(int64_t (&v)[2], int64_t (*lds)[2]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v[k] += __shfl_xor((long long)v[k], d);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6][k] = v[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    v[k] = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) v[k] += lds[w][k];
+  }
+  __syncthreads();
+}
 
 // Codes of four neighbouring bytes as f16, exactly: byte + 128 under the exponent of 1024, minus 1152.
 __device__ __forceinline__ h2 codes_lo(uint32_t u) { return __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - h2{(f16)1152, (f16)1152}; }
@@ -88,15 +135,16 @@ __device__ __forceinline__ Raw<BYTES> load_raw(const void *p) {
   return r;
 }
 
-// What a wave keeps in LDS of a tile: where its 32 rows begin, in elements, and (8-bit caches) the scales of its keys and the
-// logarithms of its values'.
+// What a wave keeps in LDS of a tile: where its 32 rows begin, in elements, and (8-bit caches) the scales of its keys, those of its
+// values and their logarithms.
 struct TileRows {
   int64_t at[TILE];
-  float scale[2 * TILE];
+  float scale[3 * TILE];
 };
 
+// (two waves to a SIMD: the second workgroup of a CU works while the first one looks up its pair or joins its waves)
 template <typename C, typename Q, int DP>
-__global__ __launch_bounds__(64 * WAVES) void attend_kernel(AttendParams p) {
+__global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void attend_kernel(AttendParams p) {
   typedef Operand<C> Op;
   typedef typename Op::t H;
   constexpr bool S8 = sizeof(C) == 1;
@@ -105,286 +153,423 @@ __global__ __launch_bounds__(64 * WAVES) void attend_kernel(AttendParams p) {
   constexpr int KS = DP / 32;                             // products per block of 16 scores
   __shared__ TileRows rows[WAVES][2];
   __shared__ float part[WAVES][HEADS][DP + 1], ml[WAVES][HEADS][2];
+  __shared__ int64_t scan[WAVES][2], before;
+  __shared__ int from;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
-  const int chunks = (p.group + HEADS - 1) / HEADS;
-  const int kvh = blockIdx.x / chunks, qc = blockIdx.x % chunks, split = blockIdx.y, b = blockIdx.z;
-  const int len = min(max(p.lens[b], 0), p.max_len), first = split * p.chunk, end = min(len, first + p.chunk);
-  if (split > 0 && first >= len) return;
-  const int heads = min(HEADS, p.group - qc * HEADS), hq0 = kvh * p.group + qc * HEADS;
-  const int32_t *table = p.table + b * p.table_ld;
-
-  // Q^T as the right operand: the lane's head, the dimensions that its loads of K bring
-  v4i q[KS];
-  float q_scale = p.scale;
-  {
-    const Q *src = static_cast<const Q *>(p.q) + b * p.qt + (hq0 + min(c16, heads - 1)) * p.qh;
-    float f[KS][8];
-    uint32_t top = 0;
+  const int per_b = p.kv_heads * p.chunks, group_rows = min(p.group, HEADS);
+  int b, hc, unit, units, slot = 0;
+  int64_t left;                               // units of this workgroup's run
+  if (p.wgs == 0) {
+    b = blockIdx.x / per_b, hc = blockIdx.x % per_b, unit = 0, units = units_of(p, b), left = units;
+  } else {
+    // The request that holds the run's first unit: the units of 256 requests at a time, added up from the front.  (The sum of all
+    // of them comes with it where there are no more requests than that.)
+    int64_t total = -1, start = 0, done = 0;
+    if (p.batch > 64 * WAVES) {
+      int64_t sum[2] = {0, 0};
+      for (int i = threadIdx.x; i < p.batch; i += 64 * WAVES) sum[0] += units_of(p, i);
+      wg_sum<WAVES>(sum, scan);
+      total = sum[0] * per_b;
+    }
+    for (int i0 = 0;; i0 += 64 * WAVES) {
+      const int i = i0 + (int)threadIdx.x;
+      const int64_t mine = i < p.batch ? (int64_t)units_of(p, i) * per_b : 0;
+      int64_t upto = mine;
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int d = S8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 + j : s * 32 + g * 8 + j;
-        f[s][j] = c16 < heads && d < p.dim ? (float)src[d] : 0.0f;
-        top = max(top, magnitude(f[s][j]));
+      for (int d = 1; d < 64; d <<= 1) {
+        const int64_t o = __shfl_up((long long)upto, d);
+        if (lane >= d) upto += o;
       }
-    if (S8) {
-      // a power of two brings the largest element of the head into [1, 2): f16 then holds what the 16-bit q had, elements
-      // 2^-14 below the largest excepted
-      top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-      const int ex = (int)(top >> 23);
-      const bool plain = ex > 0 && ex < 254;
-      q_scale *= plain ? __int_as_float(ex << 23) : 1.0f;
-      const float inv = plain ? __int_as_float((254 - ex) << 23) : 1.0f;
+      if (lane == 63) scan[wave][0] = upto;
+      __syncthreads();
+      int64_t at = done, all = 0;
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[s][j] *= inv;
+      for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) at += scan[w][0];
+        all += scan[w][0];
+      }
+      at += upto - mine;
+      if (i0 == 0) {
+        const Runs runs(uniform64(total < 0 ? all : total), p.wgs);
+        start = runs.start(blockIdx.x);
+        left = runs.start(blockIdx.x + 1) - start;
+        if (left == 0) return;
+      }
+      if (mine > 0 && at <= start && start < at + mine) from = i, before = at;
+      __syncthreads();
+      done += all;
+      if (start < done) break;
     }
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      typedef H t8 __attribute__((ext_vector_type(8)));
-      t8 o;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = (H)f[s][j];
-      q[s] = __builtin_bit_cast(v4i, o);
-    }
+    b = from;
+    units = units_of(p, b);
+    const int64_t in = start - before;
+    hc = (int)(in / units), unit = (int)(in - (int64_t)hc * units);
   }
+  b = __builtin_amdgcn_readfirstlane(b), hc = __builtin_amdgcn_readfirstlane(hc);
+  unit = __builtin_amdgcn_readfirstlane(unit), units = __builtin_amdgcn_readfirstlane(units), left = uniform64(left);
+  for (bool more = true; more;) {
+    const int kvh = hc / p.chunks, qc = hc % p.chunks, len = len_of(p, b);
+    const int last = (int)min((int64_t)units, unit + left), first = unit * UNIT, end = min(len, last * UNIT);
+    const int heads = min(HEADS, p.group - qc * HEADS), hq0 = kvh * p.group + qc * HEADS;
+    const int32_t *table = p.table + b * p.table_ld;
 
-  v4f o[E];
+    // Q^T as the right operand: the lane's head, the dimensions that its loads of K bring
+    v4i q[KS];
+    float q_scale = p.scale;
+    {
+      const Q *src = static_cast<const Q *>(p.q) + b * p.qt + (hq0 + min(c16, heads - 1)) * p.qh;
+      float f[KS][8];
+      v4i raw[KS];
+      uint32_t top = 0;
+      // (8 neighbours at a time, all loads in flight; dimensions past the head's and heads past the group's become 0 afterwards)
 #pragma unroll
-  for (int n = 0; n < E; ++n) o[n] = v4f{0, 0, 0, 0};
-  float m = -INFINITY, l = 0.0f;
-
-  struct Tile {
-    Raw<16> k[2][KL];
-    Raw<VB> v[8];
-    v4f ks[2], vs[2];
-    uint32_t there;
-  };
-  // The rows of the tile at `t0`: lane l looks up token l % 32, and everybody fetches what is theirs.
-  auto fetch = [&](int t0, int buf, Tile &x) {
-    TileRows &r = rows[wave][buf];
-    const int tok = t0 + (lane & 31);
-    const uint32_t pg = p.page_size.div((uint32_t)tok), place = (uint32_t)tok - pg * p.page_size.d;
-    const int page = tok < end ? table[pg] : -1;
-    const bool there = (uint32_t)page < (uint32_t)p.pages;
-    x.there = (uint32_t)__ballot(there);
-    const int64_t at = there ? page * p.page + place * p.token : 0;
-    if (lane < 32) r.at[lane] = at;
-    if constexpr (S8) {
-      const float *src = lane < 32 ? p.k_scale : p.v_scale;
-      const float s = there ? src[page * p.spage + place * p.stoken + kvh * p.shead] : 1.0f;
-      r.scale[lane] = lane < 32 ? s : __log2f(s);
-    }
-    lanes_meet();
-    const C *k = static_cast<const C *>(p.k) + kvh * p.head, *v = static_cast<const C *>(p.v) + kvh * p.head;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const C *row = k + r.at[16 * h + c16];
-#pragma unroll
-      for (int i = 0; i < KL; ++i) {
-        const int d = (i * 4 + g) * (16 / (int)sizeof(C));
-        x.k[h][i] = load_raw<16>(row + (d < p.dim ? d : 0));
+      for (int s = 0; s < KS; ++s) {
+        const int d = S8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
+        __builtin_memcpy(&raw[s], src + (d < p.dim ? d : 0), 16);
       }
-    }
-    const int dv = c16 * E < p.dim ? c16 * E : 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int s = 0; s < KS; ++s) {
+        const int d = S8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
+        unpack8<Q>(&raw[s], f[s]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x.v[4 * h + j] = load_raw<VB>(v + r.at[16 * h + 4 * g + j] + dv);
-    if constexpr (S8) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        x.ks[h] = *reinterpret_cast<const v4f *>(&r.scale[16 * h + 4 * g]);
-        x.vs[h] = *reinterpret_cast<const v4f *>(&r.scale[32 + 16 * h + 4 * g]);
-      }
-    }
-  };
-
-  auto attend = [&](Tile &x) {
-    // scores of the lane's head at its 8 tokens
-    float s[8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      v4f acc{0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < KL; ++i) {
-        const bool real = (i * 4 + g) * (16 / (int)sizeof(C)) < p.dim;
-        uint32_t d[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) d[j] = real ? x.k[h][i].d[j] : 0u;
-        if constexpr (S8) {
-          h8 lo, hi;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t u = d[j] ^ 0x80808080u;
-            const h2 a = codes_lo(u), e = codes_hi(u);
-            h8 &to = j < 2 ? lo : hi;
-            to[4 * (j & 1)] = a[0], to[4 * (j & 1) + 1] = a[1], to[4 * (j & 1) + 2] = e[0], to[4 * (j & 1) + 3] = e[1];
-          }
-          acc = Op::mfma(__builtin_bit_cast(v4i, lo), q[2 * i], acc);
-          acc = Op::mfma(__builtin_bit_cast(v4i, hi), q[2 * i + 1], acc);
-        } else {
-          acc = Op::mfma(v4i{(int)d[0], (int)d[1], (int)d[2], (int)d[3]}, q[i], acc);
+        for (int j = 0; j < 8; ++j) {
+          f[s][j] = c16 < heads && d < p.dim ? f[s][j] : 0.0f;
+          top = max(top, magnitude(f[s][j]));
         }
       }
+      if (S8) {
+        // a power of two brings the largest element of the head into [1, 2): f16 then holds what the 16-bit q had, elements
+        // 2^-14 below the largest excepted
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        const int ex = (int)(top >> 23);
+        const bool plain = ex > 0 && ex < 254;
+        q_scale *= plain ? __int_as_float(ex << 23) : 1.0f;
+        const float inv = plain ? __int_as_float((254 - ex) << 23) : 1.0f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[4 * h + j] = acc[j] * (S8 ? q_scale * x.ks[h][j] : q_scale);
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[s][j] *= inv;
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        typedef H t8 __attribute__((ext_vector_type(8)));
+        t8 o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = (H)f[s][j];
+        q[s] = __builtin_bit_cast(v4i, o);
+      }
     }
-    if (x.there != 0xffffffffu) {
+
+    v4f o[E];
+#pragma unroll
+    for (int n = 0; n < E; ++n) o[n] = v4f{0, 0, 0, 0};
+    float m = -INFINITY, l = 0.0f;
+
+    // A tile on its way: while one is attended to, the next one's rows are in flight, and the table entries of the one after.
+    struct Tile {
+      Raw<16> k[2][KL];
+      Raw<VB> v[8];
+      float scale;                            // lanes 0..31: of the key of token `lane`, 32..63: of the value of token `lane - 32`
+      uint32_t there;                         // its tokens that exist
+    };
+    const C *const kbase = static_cast<const C *>(p.k) + kvh * p.head, *const vbase = static_cast<const C *>(p.v) + kvh * p.head;
+    const int dv = c16 * E < p.dim ? c16 * E : 0;
+    auto look_up = [&](int t0) {              // page of token lane % 32 of the tile at t0
+      const int tok = t0 + (lane & 31);
+      return tok < end ? table[p.page_size.div((uint32_t)tok)] : -1;
+    };
+    auto fetch = [&](int t0, int page, int64_t (&at_lds)[TILE], Tile &x) {
+      const uint32_t tok = (uint32_t)(t0 + (lane & 31)), place = tok - p.page_size.div(tok) * p.page_size.d;
+      const bool there = (uint32_t)page < (uint32_t)p.pages;
+      x.there = (uint32_t)__ballot(there);
+      const int64_t at = there ? page * p.page + place * p.token : 0;
+      if (lane < 32) at_lds[lane] = at;
+      lanes_meet();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const C *row = kbase + at_lds[16 * h + c16];
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+          const int d = (i * 4 + g) * (16 / (int)sizeof(C));
+          x.k[h][i] = load_raw<16>(row + (d < p.dim ? d : 0));
+        }
+      }
+      if constexpr (S8) {
+        const float *src = lane < 32 ? p.k_scale : p.v_scale;
+        x.scale = there ? src[page * p.spage + place * p.stoken + kvh * p.shead] : 1.0f;
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool there = x.there >> (16 * h + 4 * g + j) & 1;
-          if (!there) s[4 * h + j] = -INFINITY;
-#pragma unroll
-          for (int n = 0; n < VB / 4; ++n) x.v[4 * h + j].d[n] = there ? x.v[4 * h + j].d[n] : 0u;   // (0 * NaN is NaN)
-        }
-    }
-    float w[8], top = m;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      w[j] = S8 ? s[j] + x.vs[j >> 2][j & 3] : s[j];
-      top = fmaxf(top, w[j]);
-    }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float base = top == -INFINITY ? 0.0f : top, shrink = __builtin_amdgcn_exp2f(m - base);
-    m = top;
-    float sum = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      sum += __builtin_amdgcn_exp2f(s[j] - base);
-      w[j] = __builtin_amdgcn_exp2f(w[j] - base);
-    }
-    l = l * shrink + sum;
-    typedef H t8 __attribute__((ext_vector_type(8)));
-    t8 wh;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) wh[j] = (H)w[j];
-    const v4i pt = __builtin_bit_cast(v4i, wh);
-#pragma unroll
-    for (int n = 0; n < E; ++n) {
-      v4i a;
+        for (int j = 0; j < 4; ++j) x.v[4 * h + j] = load_raw<VB>(vbase + at_lds[16 * h + 4 * g + j] + dv);
+    };
+
+    auto attend = [&](Tile &x, float *scale_lds) {
+      v4f ks[2], vs[2], vl[2];
       if constexpr (S8) {
-        const uint32_t sel = 0x0c000c00u | (uint32_t)(n & 3) | (uint32_t)(4 + (n & 3)) << 16;
+        scale_lds[lane] = x.scale;
+        if (lane >= 32) scale_lds[32 + lane] = __log2f(x.scale);
+        lanes_meet();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t u = __builtin_amdgcn_perm(x.v[2 * j + 1].d[n >> 2], x.v[2 * j].d[n >> 2], sel) ^ 0x64806480u;
-          a[j] = __builtin_bit_cast(int, __builtin_bit_cast(h2, u) - h2{(f16)1152, (f16)1152});
+        for (int h = 0; h < 2; ++h) {
+          ks[h] = *reinterpret_cast<const v4f *>(scale_lds + 16 * h + 4 * g);
+          vs[h] = *reinterpret_cast<const v4f *>(scale_lds + 32 + 16 * h + 4 * g);
+          vl[h] = *reinterpret_cast<const v4f *>(scale_lds + 64 + 16 * h + 4 * g);
         }
-      } else {
-        const uint32_t sel = n & 1 ? 0x07060302u : 0x05040100u;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = (int)__builtin_amdgcn_perm(x.v[2 * j + 1].d[n >> 1], x.v[2 * j].d[n >> 1], sel);
       }
+      // scores of the lane's head at its 8 tokens
+      float s[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[n][j] *= shrink;
-      o[n] = Op::mfma(a, pt, o[n]);
-    }
-  };
+      for (int h = 0; h < 2; ++h) {
+        v4f acc{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+          const bool real = (i * 4 + g) * (16 / (int)sizeof(C)) < p.dim;
+          uint32_t d[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) d[j] = real ? x.k[h][i].d[j] : 0u;
+          if constexpr (S8) {
+            h8 lo, hi;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t u = d[j] ^ 0x80808080u;
+              const h2 a = codes_lo(u), e = codes_hi(u);
+              h8 &to = j < 2 ? lo : hi;
+              to[4 * (j & 1)] = a[0], to[4 * (j & 1) + 1] = a[1], to[4 * (j & 1) + 2] = e[0], to[4 * (j & 1) + 3] = e[1];
+            }
+            acc = Op::mfma(__builtin_bit_cast(v4i, lo), q[2 * i], acc);
+            acc = Op::mfma(__builtin_bit_cast(v4i, hi), q[2 * i + 1], acc);
+          } else {
+            acc = Op::mfma(v4i{(int)d[0], (int)d[1], (int)d[2], (int)d[3]}, q[i], acc);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[4 * h + j] = acc[j] * (S8 ? q_scale * ks[h][j] : q_scale);
+      }
+      if (x.there != 0xffffffffu) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const bool there = x.there >> (16 * h + 4 * g + j) & 1;
+            if (!there) s[4 * h + j] = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < VB / 4; ++n) x.v[4 * h + j].d[n] = there ? x.v[4 * h + j].d[n] : 0u;   // (0 * NaN is NaN)
+          }
+      }
+      float top = m;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, S8 ? s[j] + vl[j >> 2][j & 3] : s[j]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float base = top == -INFINITY ? 0.0f : top;
+      if (__any(top > m)) {                   // (seldom in a long context)
+        const float shrink = __builtin_amdgcn_exp2f(m - base);
+        l *= shrink;
+#pragma unroll
+        for (int n = 0; n < E; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[n][j] *= shrink;
+        m = top;
+      }
+      typedef H t8 __attribute__((ext_vector_type(8)));
+      t8 wh;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float w = __builtin_amdgcn_exp2f(s[j] - base);
+        l += w;
+        wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : w);
+      }
+      const v4i pt = __builtin_bit_cast(v4i, wh);
+#pragma unroll
+      for (int n = 0; n < E; ++n) {
+        v4i a;
+        if constexpr (S8) {
+          const uint32_t sel = 0x0c000c00u | (uint32_t)(n & 3) | (uint32_t)(4 + (n & 3)) << 16;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t u = __builtin_amdgcn_perm(x.v[2 * j + 1].d[n >> 2], x.v[2 * j].d[n >> 2], sel) ^ 0x64806480u;
+            a[j] = __builtin_bit_cast(int, __builtin_bit_cast(h2, u) - h2{(f16)1152, (f16)1152});
+          }
+        } else {
+          const uint32_t sel = n & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) a[j] = (int)__builtin_amdgcn_perm(x.v[2 * j + 1].d[n >> 1], x.v[2 * j].d[n >> 1], sel);
+        }
+        o[n] = Op::mfma(a, pt, o[n]);
+      }
+    };
 
-  for (int t0 = first + wave * TILE; t0 < end; t0 += WAVES * TILE) {
-    Tile x;
-    fetch(t0, 0, x);
-    attend(x);
-  }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-
-  // the four waves join in LDS
-  if (g == 0) ml[wave][c16][0] = m, ml[wave][c16][1] = l;
-  __syncthreads();
-  float top = ml[0][c16][0];
-#pragma unroll
-  for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ml[w][c16][0]);
-  const float shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
-#pragma unroll
-  for (int n = 0; n < E; ++n)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) part[wave][c16][(4 * g + j) * E + n] = o[n][j] * shrink;
-  __syncthreads();
-  for (int i = threadIdx.x; i < heads * DP; i += 64 * WAVES) {
-    const int h = i / DP, d = i % DP;
-    float mh = ml[0][h][0], sum = 0.0f, of = 0.0f;
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) mh = fmaxf(mh, ml[w][h][0]);
-    const float base = mh == -INFINITY ? 0.0f : mh;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      sum += ml[w][h][1] * __builtin_amdgcn_exp2f(ml[w][h][0] - base);
-      of += part[w][h][d];
+    constexpr int NEXT = WAVES * TILE;
+    int t0 = first + wave * TILE;
+    if (t0 < end) {
+      Tile x, y;
+      fetch(t0, look_up(t0), rows[wave][0].at, x);
+      int page = look_up(t0 + NEXT);
+      auto turn = [&](Tile &now, Tile &then, int buf) {
+        if (t0 + NEXT < end) {
+          const int ahead = look_up(t0 + 2 * NEXT);
+          fetch(t0 + NEXT, page, rows[wave][buf ^ 1].at, then);
+          page = ahead;
+        }
+        attend(now, rows[wave][buf].scale);
+        t0 += NEXT;
+        return t0 < end;
+      };
+      while (turn(x, y, 0) && turn(y, x, 1)) {
+      }
     }
-    if (d >= p.dim) continue;
-    if (p.splits == 1) {
-      static_cast<Q *>(p.out)[b * p.ot + (hq0 + h) * p.oh + d] = (Q)(sum == 0.0f ? 0.0f : of / sum);
-    } else {
-      const int64_t at = ((int64_t)b * p.q_heads + hq0 + h) * p.splits + split;
-      p.part_o[at * p.dim + d] = of;
-      if (d == 0) p.part_ml[2 * at] = mh, p.part_ml[2 * at + 1] = sum;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+
+    // the four waves join in LDS
+    if (g == 0) ml[wave][c16][0] = m, ml[wave][c16][1] = l;
+    __syncthreads();
+    float top = ml[0][c16][0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ml[w][c16][0]);
+    const float shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
+#pragma unroll
+    for (int n = 0; n < E; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) part[wave][c16][(4 * g + j) * E + n] = o[n][j] * shrink;
+    __syncthreads();
+    for (int i = threadIdx.x; i < heads * DP; i += 64 * WAVES) {
+      const int h = i / DP, d = i % DP;
+      float mh = ml[0][h][0], sum = 0.0f, of = 0.0f;
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) mh = fmaxf(mh, ml[w][h][0]);
+      const float base = mh == -INFINITY ? 0.0f : mh;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        sum += ml[w][h][1] * __builtin_amdgcn_exp2f(ml[w][h][0] - base);
+        of += part[w][h][d];
+      }
+      if (d >= p.dim) continue;
+      if (unit == 0 && last == units) {
+        static_cast<Q *>(p.out)[b * p.ot + (hq0 + h) * p.oh + d] = (Q)(sum == 0.0f ? 0.0f : of / sum);
+      } else {
+        const int64_t at = (2 * (int64_t)blockIdx.x + slot) * group_rows + h;
+        p.part_o[at * p.dim + d] = of;
+        if (d == 0) p.part_ml[2 * at] = mh, p.part_ml[2 * at + 1] = sum;
+      }
+    }
+    left -= last - unit;
+    more = left > 0;
+    if (more) {                                 // the next pair that has tokens
+      __syncthreads();
+      slot = 1, unit = 0;
+      if (++hc == per_b) {
+        hc = 0;
+        do units = __builtin_amdgcn_readfirstlane(units_of(p, ++b));
+        while (units == 0);
+      }
     }
   }
 }
 
-// The stretches of a request and head, in their order: 4 groups of 64 lanes take every fourth.
+// The pairs that lie in pieces, and the requests without tokens.  A workgroup takes JOIN_PART elements (heads by dimensions) of a
+// pair, 4 neighbours a thread and as many pieces at a time as threads are left; the pieces are added up in a fixed order.
+constexpr int JOINERS = 8, JOIN_PART = 256, JOIN_VECS = JOIN_PART / 4, JOIN_AT_ONCE = 64 * JOINERS / JOIN_VECS;
+
 template <typename Q>
-__global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
-  __shared__ float part[4][256], sums[4];
-  const int hq = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int len = min(max(p.lens[b], 0), p.max_len), n = (len + p.chunk - 1) / p.chunk;
-  const int64_t at = ((int64_t)b * p.q_heads + hq) * p.splits;
-  float top = -INFINITY;
-  for (int i = lane; i < n; i += 64) top = fmaxf(top, p.part_ml[2 * (at + i)]);
+__global__ __launch_bounds__(64 * JOINERS) void join_kernel(AttendParams p) {
+  __shared__ v4f part[JOIN_AT_ONCE][JOIN_VECS];
+  __shared__ float sums[JOIN_AT_ONCE][JOIN_VECS];
+  __shared__ int64_t scan[JOINERS][2];
+  const int per_b = p.kv_heads * p.chunks, b = blockIdx.x / per_b, hc = blockIdx.x % per_b, kvh = hc / p.chunks, qc = hc % p.chunks;
+  const int heads = min(HEADS, p.group - qc * HEADS), hq0 = kvh * p.group + qc * HEADS, rows = min(p.group, HEADS), units = units_of(p, b);
+  const int vec = (int)threadIdx.x % JOIN_VECS, mine = (int)threadIdx.x / JOIN_VECS;
+  // (dim is a multiple of 16: four neighbours belong to one head)
+  const int e = blockIdx.y * JOIN_PART + vec * 4, h = e / p.dim, d = e - h * p.dim;
+  const bool real = h < heads;
+  Q *out = static_cast<Q *>(p.out) + b * p.ot + (hq0 + h) * p.oh + d;
+  if (units == 0) {
+    if (mine == 0 && real)
+      for (int k = 0; k < 4; ++k) out[k] = (Q)0.0f;
+    return;
+  }
+  int64_t all[2] = {0, 0};                    // units of all requests, and of those in front of this one
+  for (int i = threadIdx.x; i < p.batch; i += 64 * JOINERS) {
+    const int u = units_of(p, i);
+    all[0] += u;
+    if (i < b) all[1] += u;
+  }
+  wg_sum<JOINERS>(all, scan);
+  const Runs runs(uniform64(all[0] * per_b), p.wgs);
+  const int64_t at = uniform64(all[1] * per_b + (int64_t)hc * units), i0 = runs.of(at), i1 = runs.of(at + units - 1);
+  if (i0 == i1) return;                       // whole in one run
+  // piece i lies in slot 0 of workgroup i, but the pair may begin behind others in the first one (runs in between are not empty:
+  // with fewer units than workgroups the first ones have one each)
+  const int64_t row0 = (2 * i0 + (runs.start(i0) < at ? 1 : 0)) * rows, step = 2 * rows;
+  const int n = (int)(i1 - i0) + 1, hr = real ? h : 0;
+  const float2 *ml = reinterpret_cast<const float2 *>(p.part_ml) + hr;
+  const float *po = p.part_o + hr * p.dim + (real ? d : 0);
+  auto row_of = [&](int i) { return i == 0 ? row0 : (2 * i0) * rows + i * step; };
+  // running maximum, as in the kernel above; four pieces on their way at a time
+  float top = -INFINITY, sum = 0.0f;
+  v4f o{0, 0, 0, 0};
+  for (int i = mine; i < n; i += 4 * JOIN_AT_ONCE) {
+    float2 s[4];
+    v4f v[4];
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    for (int u = 0; u < 4; ++u) {
+      const int64_t r = row_of(min(i + u * JOIN_AT_ONCE, n - 1));
+      s[u] = ml[r];
+      v[u] = *reinterpret_cast<const v4f *>(po + r * p.dim);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (i + u * JOIN_AT_ONCE >= n) break;
+      const float now = fmaxf(top, s[u].x), base = now == -INFINITY ? 0.0f : now;
+      const float was = __builtin_amdgcn_exp2f(top - base), is = __builtin_amdgcn_exp2f(s[u].x - base);
+      top = now;
+      sum = sum * was + s[u].y * is;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = o[k] * was + v[u][k] * is;
+    }
+  }
+  __shared__ float tops[JOIN_AT_ONCE][JOIN_VECS];
+  part[mine][vec] = o, sums[mine][vec] = sum, tops[mine][vec] = top;
+  __syncthreads();
+  if (mine != 0 || !real) return;
+  for (int w = 1; w < JOIN_AT_ONCE; ++w) top = fmaxf(top, tops[w][vec]);
   const float base = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f, o[4] = {0, 0, 0, 0};
-#pragma unroll 4
-  for (int i = wave; i < n; i += 4) {
-    const float f = __builtin_amdgcn_exp2f(p.part_ml[2 * (at + i)] - base);
-    sum += f * p.part_ml[2 * (at + i) + 1];
+  sum = 0.0f, o = v4f{0, 0, 0, 0};
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (lane + 64 * k < p.dim) o[k] = __builtin_fmaf(f, p.part_o[(at + i) * p.dim + lane + 64 * k], o[k]);
+  for (int w = 0; w < JOIN_AT_ONCE; ++w) {
+    const float f = __builtin_amdgcn_exp2f(tops[w][vec] - base);
+    sum += sums[w][vec] * f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] += part[w][vec][k] * f;
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k) part[wave][lane + 64 * k] = o[k];
-  if (lane == 0) sums[wave] = sum;
-  __syncthreads();
-  const int d = threadIdx.x;
-  if (d >= p.dim) return;
-  const float total = sums[0] + sums[1] + sums[2] + sums[3], of = part[0][d] + part[1][d] + part[2][d] + part[3][d];
-  static_cast<Q *>(p.out)[b * p.ot + hq * p.oh + d] = (Q)(total == 0.0f ? 0.0f : of / total);
+  for (int k = 0; k < 4; ++k) out[k] = (Q)(sum == 0.0f ? 0.0f : o[k] / sum);
 }
 
 template <typename C, typename Q>
-f8_status launch(const AttendParams &p, int batch, int kv_heads, hipStream_t s) {
-  const int chunks = (p.group + HEADS - 1) / HEADS;
-  const dim3 grid(kv_heads * chunks, p.splits, batch), block(64 * WAVES);
+f8_status launch(const AttendParams &p, hipStream_t s) {
+  const dim3 grid(p.wgs ? p.wgs : p.batch * p.kv_heads * p.chunks), block(64 * WAVES);
   if (p.dim <= 64) hipLaunchKernelGGL((attend_kernel<C, Q, 64>), grid, block, 0, s, p);
   else if (p.dim <= 128) hipLaunchKernelGGL((attend_kernel<C, Q, 128>), grid, block, 0, s, p);
   else hipLaunchKernelGGL((attend_kernel<C, Q, 256>), grid, block, 0, s, p);
   f8_status st = launch_status();
-  if (st != F8_OK || p.splits == 1) return st;
-  hipLaunchKernelGGL(join_kernel<Q>, dim3(p.q_heads, batch), dim3(256), 0, s, p);
+  if (st != F8_OK || p.wgs == 0) return st;
+  const int elements = (p.group < HEADS ? p.group : HEADS) * p.dim;
+  hipLaunchKernelGGL(join_kernel<Q>, dim3(p.batch * p.kv_heads * p.chunks, (elements + JOIN_PART - 1) / JOIN_PART), dim3(64 * JOINERS), 0, s, p);
   return launch_status();
 }
 
-struct Split {
-  int splits, chunk;
-};
-// Stretches of whole rounds of the four waves (128 tokens), as many as give the chip some workgroups per CU.
-Split split_of(int batch, int kv_heads, int group, int max_len) {
-  const int64_t wgs = (int64_t)batch * kv_heads * ((group + HEADS - 1) / HEADS);
-  const int64_t rounds = (max_len + WAVES * TILE - 1) / (WAVES * TILE);
-  int64_t want = wgs > 0 ? (2048 + wgs - 1) / wgs : 1;
-  want = want < rounds ? want : rounds;
-  if (want < 1) want = 1;
-  const int64_t per = rounds ? (rounds + want - 1) / want : 1;
-  return Split{(int)(rounds ? (rounds + per - 1) / per : 1), (int)per * WAVES * TILE};
+// Workgroups among which the units are dealt out, or 0: a workgroup to each pair and no second launch, up to 4 units (300 tokens,
+// 32 pairs: 5.7 us against 7.1).  Otherwise as many as are resident at once, two to a CU, one with more than 128 dimensions: a
+// workgroup's way to its first rows is 5 us that only its neighbour hides (131072 tokens, 8 pairs: 67 us with 512, 72 with 1024, 81
+// with 256; dim 256, 16 pairs of up to 16384 tokens: 39 us with 256, 45 with 512), and at most 256 to a pair, whose pieces the
+// second launch adds up (one pair of 131072 tokens: 26 us with 256, 33 with 512).
+int wgs_of(int64_t pairs, int dim, int max_len) {
+  const int64_t units = (max_len + UNIT - 1) / UNIT, most = dim > 128 || pairs == 1 ? 256 : 512;
+  if (units <= 4) return 0;
+  return (int)(pairs * units < most ? pairs * units : most);
 }
 
 }  // namespace
@@ -396,8 +581,8 @@ extern "C" {
 
 size_t f8_attend_workspace_bytes(int batch, int q_heads, int kv_heads, int dim, int max_len) {
   if (batch < 1 || q_heads < 1 || kv_heads < 1 || dim < 1 || max_len < 1 || q_heads % kv_heads != 0) return 0;
-  const Split s = split_of(batch, kv_heads, q_heads / kv_heads, max_len);
-  return s.splits == 1 ? 0 : (size_t)batch * q_heads * s.splits * (dim + 2) * sizeof(float);
+  const int group = q_heads / kv_heads, wgs = wgs_of((int64_t)batch * kv_heads * ((group + HEADS - 1) / HEADS), dim, max_len);
+  return (size_t)2 * wgs * (group < HEADS ? group : HEADS) * (dim + 2) * sizeof(float);
 }
 
 f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cache, const float *k_scale, const float *v_scale,
@@ -417,23 +602,23 @@ f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cach
   if (!aligned_to(q, 2) || !aligned_to(out, 2) || !aligned_to(table, 4) || !aligned_to(lens, 4) || !aligned_to(k_scale, 4) || !aligned_to(v_scale, 4) ||
       !aligned_to(k_cache, 16) || !aligned_to(v_cache, 16) || c->page_stride * e % 16 || c->token_stride * e % 16 || c->head_stride * e % 16)
     return F8_ERR_ALIGN;
-  const int group = d->q_heads / c->heads;
-  const Split s = split_of(d->batch, c->heads, group, d->max_len);
-  if (s.splits > 65535) return F8_ERR_UNSUPPORTED;
-  const size_t rows = (size_t)d->batch * d->q_heads * s.splits;
-  if (s.splits > 1) {
+  const int group = d->q_heads / c->heads, chunks = (group + HEADS - 1) / HEADS, row = group < HEADS ? group : HEADS;
+  const int64_t pairs = (int64_t)d->batch * c->heads * chunks;
+  if (pairs > 0x7fffffffLL) return F8_ERR_UNSUPPORTED;
+  const int wgs = wgs_of(pairs, c->dim, d->max_len);
+  if (wgs) {
     if (!workspace) return F8_ERR_NULL;
     if (!aligned_to(workspace, 16)) return F8_ERR_ALIGN;
-    if (workspace_bytes < rows * (c->dim + 2) * sizeof(float)) return F8_ERR_SHAPE;
+    if (workspace_bytes < f8_attend_workspace_bytes(d->batch, d->q_heads, c->heads, c->dim, d->max_len)) return F8_ERR_SHAPE;
   }
   float *ws = static_cast<float *>(workspace);
-  const AttendParams p{q, k_cache, v_cache, k_scale, v_scale, table, lens, out, ws, ws ? ws + rows * c->dim : nullptr,
+  const AttendParams p{q, k_cache, v_cache, k_scale, v_scale, table, lens, out, ws, wgs ? ws + (size_t)2 * wgs * row * c->dim : nullptr,
                        d->q_token, d->q_head, d->o_token, d->o_head, c->page_stride, c->token_stride, c->head_stride,
-                       c->scale_page, c->scale_token, c->scale_head, d->table_ld, d->q_heads, group, c->dim, c->pages, d->max_len,
-                       s.splits, s.chunk, FastDiv((uint32_t)c->page_size), d->scale * LOG2E};
+                       c->scale_page, c->scale_token, c->scale_head, d->table_ld, d->batch, c->heads, group, chunks, c->dim, c->pages, d->max_len,
+                       wgs, FastDiv((uint32_t)c->page_size), d->scale * LOG2E};
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  if (codes) return d->type == F8_F16 ? launch<int8_t, f16>(p, d->batch, c->heads, hs) : launch<int8_t, bf16>(p, d->batch, c->heads, hs);
-  return d->type == F8_F16 ? launch<f16, f16>(p, d->batch, c->heads, hs) : launch<bf16, bf16>(p, d->batch, c->heads, hs);
+  if (codes) return d->type == F8_F16 ? launch<int8_t, f16>(p, hs) : launch<int8_t, bf16>(p, hs);
+  return d->type == F8_F16 ? launch<f16, f16>(p, hs) : launch<bf16, bf16>(p, hs);
 }
 
 }  // extern "C"

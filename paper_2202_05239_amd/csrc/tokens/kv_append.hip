@@ -21,9 +21,9 @@ struct AppendParams {
   int page_size;
 };
 
-template <typename T, typename C, int NV, bool VEC>
+template <typename T, typename C, int NV>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p) {
-  typedef RowMap<LANES, NV, VEC> Map;
+  typedef RowMap<LANES, NV> Map;
   const int row = blockIdx.x * (256 / LANES) + (int)threadIdx.x / LANES, l = (int)threadIdx.x % LANES, kv = blockIdx.y;
   if (row >= p.rows) return;
   const int token = (int)p.heads.div((uint32_t)row), head = row - token * (int)p.heads.d;
@@ -32,7 +32,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p) {
   float v[NV][8];
   const T *x = static_cast<const T *>(p.x[kv]) + token * p.xt[kv] + head * p.xh[kv];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) load_piece<T, Map, VEC>(x, i, l, p.dim, v[i]);
+  for (int i = 0; i < NV; ++i) load_piece<T, Map>(x, i, l, p.dim, v[i]);
   const int64_t page = there ? slot / p.page_size : 0, place = there ? slot - page * p.page_size : 0;
   C *to = static_cast<C *>(p.cache[kv]) + page * p.page + place * p.token + head * p.head;
   if constexpr (sizeof(C) == 1) {
@@ -51,31 +51,26 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p) {
       int q[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) q[j] = code_of(v[i][j], s);
-      store_codes<Map, VEC>(reinterpret_cast<int8_t *>(to), i, l, p.dim, q);
+      store_codes<Map>(reinterpret_cast<int8_t *>(to), i, l, p.dim, q);
     }
   } else {
     if (!there) return;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) store_piece<C, Map, VEC>(to, i, l, p.dim, v[i]);
+    for (int i = 0; i < NV; ++i) store_piece<C, Map>(to, i, l, p.dim, v[i]);
   }
 }
 
 template <typename T, typename C>
-f8_status launch(const AppendParams &p, bool vec, hipStream_t s) {
+f8_status launch(const AppendParams &p, hipStream_t s) {
   const dim3 grid((p.rows + 256 / LANES - 1) / (256 / LANES), 2), block(256);
-  if (p.dim <= LANES * 8) {
-    if (vec) hipLaunchKernelGGL((kv_append_kernel<T, C, 1, true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((kv_append_kernel<T, C, 1, false>), grid, block, 0, s, p);
-  } else {
-    if (vec) hipLaunchKernelGGL((kv_append_kernel<T, C, 2, true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((kv_append_kernel<T, C, 2, false>), grid, block, 0, s, p);
-  }
+  if (p.dim <= LANES * 8) hipLaunchKernelGGL((kv_append_kernel<T, C, 1>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((kv_append_kernel<T, C, 2>), grid, block, 0, s, p);
   return launch_status();
 }
 
 template <typename T>
-f8_status launch_cache(const AppendParams &p, int cache, bool vec, hipStream_t s) {
-  return cache == F8_S8 ? launch<T, int8_t>(p, vec, s) : cache == F8_F16 ? launch<T, f16>(p, vec, s) : launch<T, bf16>(p, vec, s);
+f8_status launch_cache(const AppendParams &p, int cache, hipStream_t s) {
+  return cache == F8_S8 ? launch<T, int8_t>(p, s) : cache == F8_F16 ? launch<T, f16>(p, s) : launch<T, bf16>(p, s);
 }
 
 }  // namespace
@@ -93,18 +88,14 @@ extern "C" f8_status f8_kv_append(const void *k, const void *v, const int64_t *s
   if (d->tokens == 0) return F8_OK;
   const bool codes = c->type == F8_S8;
   if (!k || !v || !slots || !k_cache || !v_cache || (codes && (!k_scale || !v_scale))) return F8_ERR_NULL;
-  const size_t e = bytes_of(d->type), o = bytes_of(c->type), og = codes ? 8 : 16;
-  const int64_t strides[] = {d->k_token, d->k_head, d->v_token, d->v_head}, places[] = {c->page_stride, c->token_stride, c->head_stride};
+  const size_t e = bytes_of(d->type), o = bytes_of(c->type);
   if (!aligned_to(k, e) || !aligned_to(v, e) || !aligned_to(slots, 8) || !aligned_to(k_cache, o) || !aligned_to(v_cache, o) ||
       !aligned_to(k_scale, 4) || !aligned_to(v_scale, 4))
     return F8_ERR_ALIGN;
-  bool vec = aligned_to(k, 16) && aligned_to(v, 16) && aligned_to(k_cache, og) && aligned_to(v_cache, og);
-  for (int64_t n : strides) vec = vec && n * (int64_t)e % 16 == 0;
-  for (int64_t n : places) vec = vec && n * (int64_t)o % (int64_t)og == 0;
   const AppendParams p{{k, v}, slots, {k_cache, v_cache}, {k_scale, v_scale}, {d->k_token, d->v_token}, {d->k_head, d->v_head},
                        c->page_stride, c->token_stride, c->head_stride, c->scale_page, c->scale_token, c->scale_head,
                        (int64_t)c->pages * c->page_size, d->tokens * c->heads, c->dim, FastDiv((uint32_t)c->heads), c->page_size};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return d->type == F8_F32 ? launch_cache<float>(p, c->type, vec, s)
-                           : d->type == F8_F16 ? launch_cache<f16>(p, c->type, vec, s) : launch_cache<bf16>(p, c->type, vec, s);
+  return d->type == F8_F32 ? launch_cache<float>(p, c->type, s)
+                           : d->type == F8_F16 ? launch_cache<f16>(p, c->type, s) : launch_cache<bf16>(p, c->type, s);
 }

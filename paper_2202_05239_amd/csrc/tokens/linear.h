@@ -12,7 +12,6 @@ struct LinearParams {
   void *y;
   int64_t ldx, ldw, ldy;
   int M, N, K;
-  int x_vec;                          // real tokens' rows start on 16 bytes
 };
 
 typedef int v16i __attribute__((ext_vector_type(16)));
@@ -33,11 +32,10 @@ __device__ __forceinline__ v4i load_row16(const int8_t *row, bool real, int k, i
 
 // 8 real elements of a row from column k on (a multiple of 8); past the row's end zeros.
 template <typename X>
-__device__ __forceinline__ void load_row8(const X *row, int k, int K, int vec, float (&v)[8]) {
-  if (vec && k + 8 <= K) {
+__device__ __forceinline__ void load_row8(const X *row, int k, int K, float (&v)[8]) {
+  if (k + 8 <= K) {
     v4i raw[2];
-    raw[0] = *reinterpret_cast<const v4i *>(row + k);
-    if (sizeof(X) == 4) raw[1] = *reinterpret_cast<const v4i *>(row + k + 4);
+    __builtin_memcpy(raw, row + k, 8 * sizeof(X));
     unpack8<X>(raw, v);
   } else {
 #pragma unroll
@@ -45,30 +43,40 @@ __device__ __forceinline__ void load_row8(const X *row, int k, int K, int vec, f
   }
 }
 
-// The 16 channels n .. n + 15 of token m (n a multiple of 16).  VEC: y, its rows, sw and bias start on 16 bytes.
+// The 16 channels n .. n + 15 of token m from a lane's registers (n a multiple of 16), at any address.
 template <typename T>
-__device__ __forceinline__ void store_scaled(const LinearParams &p, const v16i &acc, int m, int n, bool vec) {
-  if (m >= p.M || n >= p.N) return;
-  const float sx = p.sx[m];
-  T *y = static_cast<T *>(p.y) + m * p.ldy + n;
-  if (vec && n + 16 <= p.N) {
-    typedef T t16 __attribute__((ext_vector_type(16)));
-    t16 o;
+__device__ __forceinline__ void scale16(const LinearParams &p, const v16i &acc, float sx, int n, T (&o)[16]) {
+  float s[16], b[16];
+  if (n + 16 <= p.N) {
+    __builtin_memcpy(s, p.sw + n, 64);
+    if (p.bias) __builtin_memcpy(b, p.bias + n, 64);
+  } else {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float4 s = reinterpret_cast<const float4 *>(p.sw + n)[q];
-      const float4 b = p.bias ? reinterpret_cast<const float4 *>(p.bias + n)[q] : make_float4(0, 0, 0, 0);
-      o[4 * q] = (T)__builtin_fmaf((float)acc[4 * q] * sx, s.x, b.x);
-      o[4 * q + 1] = (T)__builtin_fmaf((float)acc[4 * q + 1] * sx, s.y, b.y);
-      o[4 * q + 2] = (T)__builtin_fmaf((float)acc[4 * q + 2] * sx, s.z, b.z);
-      o[4 * q + 3] = (T)__builtin_fmaf((float)acc[4 * q + 3] * sx, s.w, b.w);
+    for (int i = 0; i < 16; ++i) {
+      s[i] = n + i < p.N ? p.sw[n + i] : 0.0f;
+      if (p.bias) b[i] = n + i < p.N ? p.bias[n + i] : 0.0f;
     }
+  }
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<v4i *>(y)[i] = reinterpret_cast<const v4i *>(&o)[i];
+  for (int i = 0; i < 16; ++i) o[i] = (T)__builtin_fmaf((float)acc[i] * sx, s[i], p.bias ? b[i] : 0.0f);
+}
+template <typename T>
+__device__ __forceinline__ void store_scaled(const LinearParams &p, const v16i &acc, int m, int n) {
+  if (m >= p.M || n >= p.N) return;
+  T o[16];
+  scale16(p, acc, p.sx[m], n, o);
+  T *y = static_cast<T *>(p.y) + m * p.ldy + n;
+  if (n + 16 <= p.N) {
+#pragma unroll
+    for (int q = 0; q < (int)sizeof(T); ++q) {
+      v4i v;
+      __builtin_memcpy(&v, o + q * (16 / sizeof(T)), 16);
+      reinterpret_cast<v4i_any *>(y)[q] = v;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      if (n + i < p.N) y[i] = (T)__builtin_fmaf((float)acc[i] * sx, p.sw[n + i], p.bias ? p.bias[n + i] : 0.0f);
+      if (n + i < p.N) y[i] = o[i];
   }
 }
 

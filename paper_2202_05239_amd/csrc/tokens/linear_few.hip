@@ -51,7 +51,7 @@ __global__ __launch_bounds__(THREADS) void linear_few_kernel(LinearParams p) {
       const int task = wave + WAVES * h;
       if (task >= tasks) break;
       const int r = task / stretches, k = (task - r * stretches) * 512 + lane * 8;
-      load_row8(x + r * p.ldx, k, p.K, p.x_vec, v[h]);
+      load_row8(x + r * p.ldx, k, p.K, v[h]);
     }
 #pragma unroll
     for (int h = 0; h < HELD; ++h) {

@@ -28,7 +28,7 @@ __device__ __forceinline__ v4i lds_read(uint32_t at, const int imm) {
 }
 
 template <typename T, int WN, int WM, int NB, int MB, int RING, int KG>
-__global__ __launch_bounds__(64 * WN * WM * KG) void linear_tile_kernel(LinearParams p, int tiles_m, int tiles_n, int vec) {
+__global__ __launch_bounds__(64 * WN * WM * KG) void linear_tile_kernel(LinearParams p, int tiles_m, int tiles_n) {
   constexpr int BN = 32 * NB * WN, BM = 32 * MB * WM, W = WN * WM, BUF = (BN + BM) * KS, LOADS = (BN + BM) / 8 / W, GROUP = 8;
   static_assert(W % 2 == 0 && BN / 8 % W == 0 && BM / 8 % W == 0, "an instruction's rows are all weights or all tokens");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[KG * RING * BUF];
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(64 * WN * WM * KG) void linear_tile_kernel(LinearPa
 #pragma unroll
   for (int j = 0; j < MB; ++j)
 #pragma unroll
-    for (int i = 0; i < NB; ++i) store_scaled<T>(p, acc[i][j], m0 + wm + 32 * j + l32, n0 + wn + 32 * i + 16 * half, vec);
+    for (int i = 0; i < NB; ++i) store_scaled<T>(p, acc[i][j], m0 + wm + 32 * j + l32, n0 + wn + 32 * i + 16 * half);
 }
 
 template <typename T, int WN, int WM, int NB, int MB, int RING, int KG>
@@ -193,8 +193,7 @@ f8_status launch(const LinearParams &p, hipStream_t s) {
   constexpr int BN = 32 * NB * WN, BM = 32 * MB * WM;
   const int64_t tn = (p.N + BN - 1) / BN, tm = (p.M + BM - 1) / BM;
   if (tn * tm > 0x7fffffff) return F8_ERR_UNSUPPORTED;
-  const int vec = aligned_to(p.y, 16) && p.ldy * sizeof(T) % 16 == 0 && aligned_to(p.sw, 16) && aligned_to(p.bias, 16);
-  hipLaunchKernelGGL((linear_tile_kernel<T, WN, WM, NB, MB, RING, KG>), dim3((unsigned)(tn * tm)), dim3(64 * WN * WM * KG), 0, s, p, (int)tm, (int)tn, vec);
+  hipLaunchKernelGGL((linear_tile_kernel<T, WN, WM, NB, MB, RING, KG>), dim3((unsigned)(tn * tm)), dim3(64 * WN * WM * KG), 0, s, p, (int)tm, (int)tn);
   return launch_status();
 }
 

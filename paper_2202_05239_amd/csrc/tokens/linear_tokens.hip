@@ -18,7 +18,7 @@ namespace {
 constexpr int ANY_TILE = 128, ANY_K = 64, ANY_PITCH = ANY_K + 16;
 
 template <typename T>
-__global__ __launch_bounds__(256) void linear_any_kernel(LinearParams p, int tiles_m, int vec) {
+__global__ __launch_bounds__(256) void linear_any_kernel(LinearParams p, int tiles_m) {
   __shared__ uint8_t lds[2][2 * ANY_TILE * ANY_PITCH];
   const int tile = (int)xcd_remap(blockIdx.x, gridDim.x);
   const int m0 = tile % tiles_m * ANY_TILE, n0 = tile / tiles_m * ANY_TILE;
@@ -64,15 +64,14 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearParams p, int til
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) store_scaled<T>(p, acc[i][j], m0 + wm + 32 * j + l32, n0 + wn + 32 * i + 16 * half, vec);
+    for (int j = 0; j < 2; ++j) store_scaled<T>(p, acc[i][j], m0 + wm + 32 * j + l32, n0 + wn + 32 * i + 16 * half);
 }
 
 template <typename T>
 f8_status launch_any(const LinearParams &p, hipStream_t s) {
-  const bool vec = aligned_to(p.y, 16) && p.ldy * sizeof(T) % 16 == 0 && aligned_to(p.sw, 16) && aligned_to(p.bias, 16);
   const int64_t tm = (p.M + ANY_TILE - 1) / ANY_TILE, tn = (p.N + ANY_TILE - 1) / ANY_TILE;
   if (tm * tn > 0x7fffffff) return F8_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(linear_any_kernel<T>, dim3((unsigned)(tm * tn)), dim3(256), 0, s, p, (int)tm, vec);
+  hipLaunchKernelGGL(linear_any_kernel<T>, dim3((unsigned)(tm * tn)), dim3(256), 0, s, p, (int)tm);
   return launch_status();
 }
 
@@ -136,7 +135,7 @@ f8_status f8_linear_scaled(const int8_t *x, const float *sx, const int8_t *w, co
   if (st != F8_OK) return st;
   if (!sx) return F8_ERR_NULL;
   if (!aligned_to(sx, 4)) return F8_ERR_ALIGN;
-  const LinearParams p{x, w, sx, sw, bias, y, d->ldx, d->ldw, d->ldy, d->M, d->N, d->K, 0};
+  const LinearParams p{x, w, sx, sw, bias, y, d->ldx, d->ldw, d->ldy, d->M, d->N, d->K};
   return enqueue_linear(p, d->y_type, static_cast<hipStream_t>(stream));
 }
 
@@ -157,8 +156,7 @@ f8_status f8_linear_tokens(const void *x, const int8_t *w, const float *sw, cons
   if (!aligned_to(x, bytes_of(d->x_type)) || !aligned_to(workspace, 16)) return F8_ERR_ALIGN;
   if (workspace_bytes < f8_linear_workspace_bytes(d->M, d->K)) return F8_ERR_SHAPE;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  LinearParams p{static_cast<const int8_t *>(x), w, nullptr, sw, bias, y, d->ldx, d->ldw, d->ldy, d->M, d->N, d->K,
-                 aligned_to(x, 16) && d->ldx * bytes_of(d->x_type) % 16 == 0};
+  LinearParams p{static_cast<const int8_t *>(x), w, nullptr, sw, bias, y, d->ldx, d->ldw, d->ldy, d->M, d->N, d->K};
   if (few_quantises(d->M, d->N, d->K)) return launch_linear_few(p, d->x_type, d->y_type, s);
   const int64_t pitch = code_pitch(d->K);
   int8_t *codes = static_cast<int8_t *>(workspace);

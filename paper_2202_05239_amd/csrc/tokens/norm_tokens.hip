@@ -24,16 +24,16 @@ struct NormParams {
 };
 
 // The weights are vectors of `cols` in the type of the rows or in 32 bits, read by every row (from cache).
-template <typename T, typename Map, bool VEC>
+template <typename T, typename Map>
 __device__ __forceinline__ void load_weight(const void *w, int w_f32, int i, int t, int cols, float (&v)[8]) {
-  if (w_f32) load_piece<float, Map, VEC>(static_cast<const float *>(w), i, t, cols, v);
-  else load_piece<T, Map, VEC>(static_cast<const T *>(w), i, t, cols, v);
+  if (w_f32) load_piece<float, Map>(static_cast<const float *>(w), i, t, cols, v);
+  else load_piece<T, Map>(static_cast<const T *>(w), i, t, cols, v);
 }
 
-template <typename T, int TPR, int NV, bool VEC>
+template <typename T, int TPR, int NV>
 __device__ __forceinline__ void normalise(float (&v)[NV][8], int form, float eps, const void *w, const void *b, const NormParams &p, int t,
                                           float *lds) {
-  typedef RowMap<TPR, NV, VEC> Map;
+  typedef RowMap<TPR, NV> Map;
   constexpr int W = TPR / 64;
   float mean = 0.0f;
   if (form == F8_NORM_LAYER) {
@@ -60,35 +60,35 @@ __device__ __forceinline__ void normalise(float (&v)[NV][8], int form, float eps
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[i][j] *= r;
     if (w) {
-      load_weight<T, Map, VEC>(w, p.w_f32, i, t, p.cols, g);
+      load_weight<T, Map>(w, p.w_f32, i, t, p.cols, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] *= g[j];
     }
     if (b) {
-      load_weight<T, Map, VEC>(b, p.w_f32, i, t, p.cols, g);
+      load_weight<T, Map>(b, p.w_f32, i, t, p.cols, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] += g[j];
     }
   }
 }
 
-template <typename T, int TPR, int NV, bool VEC>
+template <typename T, int TPR, int NV>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_tokens_kernel(NormParams p) {
-  typedef RowMap<TPR, NV, VEC> Map;
+  typedef RowMap<TPR, NV> Map;
   constexpr int THREADS = TPR < 256 ? 256 : TPR, RPB = THREADS / TPR, W = TPR / 64;
   __shared__ float lds[5 * (THREADS / 64)];          // a set of words for each of the five reductions of a row
   const int row = blockIdx.x * RPB + (int)threadIdx.x / TPR, t = (int)threadIdx.x % TPR;
   if (RPB > 1 && row >= p.rows) return;              // (waves on their own: no barrier below)
   float v[NV][8];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) load_piece<T, Map, VEC>(static_cast<const T *>(p.a) + row * p.lda, i, t, p.cols, v[i]);
-  if (p.post != F8_NORM_NONE) normalise<T, TPR, NV, VEC>(v, p.post, p.post_eps, p.post_w, p.post_b, p, t, lds);
+  for (int i = 0; i < NV; ++i) load_piece<T, Map>(static_cast<const T *>(p.a) + row * p.lda, i, t, p.cols, v[i]);
+  if (p.post != F8_NORM_NONE) normalise<T, TPR, NV>(v, p.post, p.post_eps, p.post_w, p.post_b, p, t, lds);
   if (p.gate) {
     const T *gate = static_cast<const T *>(p.gate) + p.gate_rows.div((uint32_t)row) * p.ldg;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       float g[8];
-      load_piece<T, Map, VEC>(gate, i, t, p.cols, g);
+      load_piece<T, Map>(gate, i, t, p.cols, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] *= g[j];
     }
@@ -97,20 +97,20 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_tokens_kernel(Norm
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       float g[8];
-      load_piece<T, Map, VEC>(static_cast<const T *>(p.res) + row * p.ldr, i, t, p.cols, g);
+      load_piece<T, Map>(static_cast<const T *>(p.res) + row * p.ldr, i, t, p.cols, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = __builtin_fmaf(p.res_scale, g[j], v[i][j]);
     }
   }
   if (p.res_out) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) store_piece<T, Map, VEC>(static_cast<T *>(p.res_out) + row * p.ldo, i, t, p.cols, v[i]);
+    for (int i = 0; i < NV; ++i) store_piece<T, Map>(static_cast<T *>(p.res_out) + row * p.ldo, i, t, p.cols, v[i]);
   }
   if (!p.y) return;
-  if (p.pre != F8_NORM_NONE) normalise<T, TPR, NV, VEC>(v, p.pre, p.pre_eps, p.pre_w, p.pre_b, p, t, lds + 2 * W);
+  if (p.pre != F8_NORM_NONE) normalise<T, TPR, NV>(v, p.pre, p.pre_eps, p.pre_w, p.pre_b, p, t, lds + 2 * W);
   if (!p.codes) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) store_piece<T, Map, VEC>(static_cast<T *>(p.y) + row * p.ldy, i, t, p.cols, v[i]);
+    for (int i = 0; i < NV; ++i) store_piece<T, Map>(static_cast<T *>(p.y) + row * p.ldy, i, t, p.cols, v[i]);
     return;
   }
   uint32_t top = 0;
@@ -125,32 +125,28 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_tokens_kernel(Norm
     int q[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) q[j] = code_of(v[i][j], s);
-    store_codes<Map, VEC>(static_cast<int8_t *>(p.y) + row * p.ldy, i, t, p.cols, q);
+    store_codes<Map>(static_cast<int8_t *>(p.y) + row * p.ldy, i, t, p.cols, q);
   }
 }
 
-template <typename T, int TPR, int NV, bool VEC>
+template <typename T, int TPR, int NV>
 void launch(const NormParams &p, hipStream_t s) {
   constexpr int THREADS = TPR < 256 ? 256 : TPR, RPB = THREADS / TPR;
-  hipLaunchKernelGGL((norm_tokens_kernel<T, TPR, NV, VEC>), dim3((p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
-}
-
-template <typename T, bool VEC>
-void launch_row(const NormParams &p, hipStream_t s) {
-  if (p.cols <= 512) launch<T, 64, 1, VEC>(p, s);
-  else if (p.cols <= 1024) launch<T, 64, 2, VEC>(p, s);
-  else if (p.cols <= 2048) launch<T, 256, 1, VEC>(p, s);
-  else if (p.cols <= 4096) launch<T, 256, 2, VEC>(p, s);
-  else if (p.cols <= 8192) launch<T, 256, 4, VEC>(p, s);
-  else if (p.cols <= 16384) launch<T, 1024, 2, VEC>(p, s);
-  else launch<T, 1024, 8, VEC>(p, s);
+  hipLaunchKernelGGL((norm_tokens_kernel<T, TPR, NV>), dim3((p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
 }
 
 template <typename T>
-f8_status launch_type(const NormParams &p, bool vec, hipStream_t s) {
-  vec ? launch_row<T, true>(p, s) : launch_row<T, false>(p, s);
+f8_status launch_row(const NormParams &p, hipStream_t s) {
+  if (p.cols <= 512) launch<T, 64, 1>(p, s);
+  else if (p.cols <= 1024) launch<T, 64, 2>(p, s);
+  else if (p.cols <= 2048) launch<T, 256, 1>(p, s);
+  else if (p.cols <= 4096) launch<T, 256, 2>(p, s);
+  else if (p.cols <= 8192) launch<T, 256, 4>(p, s);
+  else if (p.cols <= 16384) launch<T, 1024, 2>(p, s);
+  else launch<T, 1024, 8>(p, s);
   return launch_status();
 }
+
 
 bool norm_form(int f) { return f == F8_NORM_NONE || f == F8_NORM_RMS || f == F8_NORM_LAYER; }
 
@@ -171,18 +167,15 @@ extern "C" f8_status f8_norm_tokens(const void *a, const void *res, const void *
   if (d->rows == 0) return F8_OK;
   const bool codes = y && d->y_type == F8_S8;
   if (!a || (!y && !res_out) || (codes && !scale)) return F8_ERR_NULL;
-  const size_t e = bytes_of(d->type), we = bytes_of(d->w_type), o = codes ? 1 : e, og = codes ? 8 : 16;
-  const void *rows[] = {a, res, gate, res_out}, *weights[] = {post_w, post_b, pre_w, pre_b};
-  const int64_t lds[] = {d->lda, d->ldr, d->ldg, d->ldo};
-  bool vec = aligned_to(y, og) && (!y || d->ldy * o % og == 0);
-  if (!aligned_to(y, o) || !aligned_to(scale, 4)) return F8_ERR_ALIGN;
-  for (int i = 0; i < 4; ++i) {
-    if (!aligned_to(rows[i], e) || !aligned_to(weights[i], we)) return F8_ERR_ALIGN;
-    vec = vec && aligned_to(rows[i], 16) && (!rows[i] || lds[i] * e % 16 == 0) && aligned_to(weights[i], 16);
-  }
+  const size_t e = bytes_of(d->type), we = bytes_of(d->w_type);
+  for (const void *t : {a, res, gate, static_cast<const void *>(res_out)})
+    if (!aligned_to(t, e)) return F8_ERR_ALIGN;
+  for (const void *t : {post_w, post_b, pre_w, pre_b})
+    if (!aligned_to(t, we)) return F8_ERR_ALIGN;
+  if (!aligned_to(y, codes ? 1 : e) || !aligned_to(scale, 4)) return F8_ERR_ALIGN;
   const NormParams p{a, res, post_w, post_b, gate, pre_w, pre_b, res_out, y, scale, d->lda, d->ldr, d->ldg, d->ldo, d->ldy,
                      d->rows, d->cols, d->post, d->pre, codes, d->w_type == F8_F32, d->post_eps, d->pre_eps, d->res_scale,
                      1.0f / (float)d->cols, FastDiv((uint32_t)(gate ? d->gate_rows : 1))};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return d->type == F8_F32 ? launch_type<float>(p, vec, s) : d->type == F8_F16 ? launch_type<f16>(p, vec, s) : launch_type<bf16>(p, vec, s);
+  return d->type == F8_F32 ? launch_row<float>(p, s) : d->type == F8_F16 ? launch_row<f16>(p, s) : launch_row<bf16>(p, s);
 }

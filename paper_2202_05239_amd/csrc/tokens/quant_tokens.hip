@@ -29,9 +29,9 @@ __device__ __forceinline__ float act_of(int act, float g) {
   return g / (1.0f + expf(-u));
 }
 
-template <typename T, int TPR, int NV, bool VEC>
+template <typename T, int TPR, int NV>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quant_tokens_kernel(QuantParams p) {
-  typedef RowMap<TPR, NV, VEC> Map;
+  typedef RowMap<TPR, NV> Map;
   constexpr int THREADS = TPR < 256 ? 256 : TPR, RPB = THREADS / TPR;
   __shared__ float lds[THREADS / 64];
   const int row = blockIdx.x * RPB + (int)threadIdx.x / TPR, t = (int)threadIdx.x % TPR;
@@ -40,13 +40,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quant_tokens_kernel(Qua
   float v[NV][8];
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) load_piece<T, Map, VEC>(x, i, t, p.cols, v[i]);
+  for (int i = 0; i < NV; ++i) load_piece<T, Map>(x, i, t, p.cols, v[i]);
   if (p.gate) {
     const T *gate = static_cast<const T *>(p.gate) + row * p.ldg;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       float g[8];
-      load_piece<T, Map, VEC>(gate, i, t, p.cols, g);
+      load_piece<T, Map>(gate, i, t, p.cols, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] *= act_of(p.act, g[j]);
     }
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quant_tokens_kernel(Qua
       int q[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) q[j] = code_of(v[i][j], s);
-      store_codes<Map, VEC>(y, i, t, p.pad, q);
+      store_codes<Map>(y, i, t, p.pad, q);
     }
   } else {
     T *y = static_cast<T *>(p.y) + row * p.ldy;
@@ -73,44 +73,39 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quant_tokens_kernel(Qua
       float o[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) o[j] = (float)code_of(v[i][j], s) * s.scale;
-      store_piece<T, Map, VEC>(y, i, t, p.cols, o);
+      store_piece<T, Map>(y, i, t, p.cols, o);
     }
   }
 }
 
-template <typename T, int TPR, int NV, bool VEC>
+template <typename T, int TPR, int NV>
 void launch(const QuantParams &p, hipStream_t s) {
   constexpr int THREADS = TPR < 256 ? 256 : TPR, RPB = THREADS / TPR;
-  hipLaunchKernelGGL((quant_tokens_kernel<T, TPR, NV, VEC>), dim3((p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
-}
-
-template <typename T, bool VEC>
-void launch_row(const QuantParams &p, hipStream_t s) {
-  if (p.pad <= 512) launch<T, 64, 1, VEC>(p, s);
-  else if (p.pad <= 1024) launch<T, 64, 2, VEC>(p, s);
-  else if (p.pad <= 2048) launch<T, 256, 1, VEC>(p, s);
-  else if (p.pad <= 4096) launch<T, 256, 2, VEC>(p, s);
-  else if (p.pad <= 8192) launch<T, 256, 4, VEC>(p, s);
-  else if (p.pad <= 16384) launch<T, 1024, 2, VEC>(p, s);
-  else launch<T, 1024, 8, VEC>(p, s);
+  hipLaunchKernelGGL((quant_tokens_kernel<T, TPR, NV>), dim3((p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
 }
 
 template <typename T>
-f8_status launch_type(const QuantParams &p, bool vec, hipStream_t s) {
-  vec ? launch_row<T, true>(p, s) : launch_row<T, false>(p, s);
+f8_status launch_row(const QuantParams &p, hipStream_t s) {
+  if (p.pad <= 512) launch<T, 64, 1>(p, s);
+  else if (p.pad <= 1024) launch<T, 64, 2>(p, s);
+  else if (p.pad <= 2048) launch<T, 256, 1>(p, s);
+  else if (p.pad <= 4096) launch<T, 256, 2>(p, s);
+  else if (p.pad <= 8192) launch<T, 256, 4>(p, s);
+  else if (p.pad <= 16384) launch<T, 1024, 2>(p, s);
+  else launch<T, 1024, 8>(p, s);
   return launch_status();
 }
 
-f8_status enqueue(const QuantParams &p, int x_type, bool vec, hipStream_t s) {
-  return x_type == F8_F32 ? launch_type<float>(p, vec, s) : x_type == F8_F16 ? launch_type<f16>(p, vec, s) : launch_type<bf16>(p, vec, s);
+
+f8_status enqueue(const QuantParams &p, int x_type, hipStream_t s) {
+  return x_type == F8_F32 ? launch_row<float>(p, s) : x_type == F8_F16 ? launch_row<f16>(p, s) : launch_row<bf16>(p, s);
 }
 
 }  // namespace
 
 f8_status enqueue_quant_tokens(const void *x, int64_t ldx, int x_type, int8_t *codes, int64_t ld, int pad, float *scale, int rows, int cols,
                                hipStream_t s) {
-  const bool vec = aligned_to(x, 16) && ldx * bytes_of(x_type) % 16 == 0 && aligned_to(codes, 8) && ld % 8 == 0;
-  return enqueue(QuantParams{x, nullptr, codes, scale, ldx, 0, ld, rows, cols, F8_ACT_NONE, 1, pad}, x_type, vec, s);
+  return enqueue(QuantParams{x, nullptr, codes, scale, ldx, 0, ld, rows, cols, F8_ACT_NONE, 1, pad}, x_type, s);
 }
 
 }  // namespace f8
@@ -128,9 +123,6 @@ extern "C" f8_status f8_quant_tokens(const void *x, const void *gate, void *y, f
   if (!x || !y || (codes && !scale) || (d->act != F8_ACT_NONE && !gate)) return F8_ERR_NULL;
   const size_t e = bytes_of(d->x_type), o = codes ? 1 : e;
   if (!aligned_to(x, e) || !aligned_to(y, o) || !aligned_to(gate, e) || !aligned_to(scale, 4)) return F8_ERR_ALIGN;
-  const size_t og = codes ? 8 : 16;                  // a piece of 8 is one access of 8 codes, or of 16 bytes
-  const bool vec = aligned_to(x, 16) && d->ldx * e % 16 == 0 && aligned_to(y, og) && d->ldy * o % og == 0 &&
-                   (!gate || (aligned_to(gate, 16) && d->ldg * e % 16 == 0));
   const QuantParams p{x, gate, y, scale, d->ldx, d->ldg, d->ldy, d->rows, d->cols, d->act, codes, d->cols};
-  return enqueue(p, d->x_type, vec, static_cast<hipStream_t>(stream));
+  return enqueue(p, d->x_type, static_cast<hipStream_t>(stream));
 }

@@ -18,15 +18,18 @@ namespace f8 {
 typedef _Float16 f16;
 typedef __bf16 bf16;
 
+// 16 bytes at any address (a vector store of its own type: as elements the compiler would split it where another branch stores some)
+typedef int v4i_any __attribute__((ext_vector_type(4), aligned(1), may_alias));
+
 constexpr int ROW_MOST = 65536;   // columns of a row that a workgroup holds in registers
 
-// How the elements of a row lie in its threads.  `TPR` threads share a row, each has NV pieces of 8.  VEC: the rows start on
-// 16 bytes, a piece is 8 neighbours (one or two 16-byte accesses).  Otherwise the 8 elements of a piece are TPR apart, so
-// that each access of a wave is one run of neighbours whatever the row's address.
-template <int TPR, int NV, bool VEC>
+// How the elements of a row lie in its threads: `TPR` threads share a row, each has NV pieces of 8 neighbours, one or two 16-byte
+// accesses.  The accesses are taken at any address an element may have: this chip's loads and stores do not need alignment, a row
+// off the 16-byte grid costs up to a second line per access.
+template <int TPR, int NV>
 struct RowMap {
   static constexpr int most = TPR * NV * 8;
-  static __device__ __forceinline__ int col(int i, int j, int t) { return VEC ? (i * TPR + t) * 8 + j : (i * 8 + j) * TPR + t; }
+  static __device__ __forceinline__ int col(int i, int j, int t) { return (i * TPR + t) * 8 + j; }
 };
 
 template <typename T>
@@ -49,13 +52,12 @@ __device__ __forceinline__ void unpack8(const v4i *raw, float (&v)[8]) {
 }
 
 // 8 elements of piece i of a row into v; what lies past the row's end reads as 0.
-template <typename T, typename Map, bool VEC>
+template <typename T, typename Map>
 __device__ __forceinline__ void load_piece(const T *row, int i, int t, int cols, float (&v)[8]) {
   const int c = Map::col(i, 0, t);
-  if (VEC && c + 8 <= cols) {
+  if (c + 8 <= cols) {
     v4i raw[2];
-    raw[0] = *reinterpret_cast<const v4i *>(row + c);
-    if (sizeof(T) == 4) raw[1] = *reinterpret_cast<const v4i *>(row + c + 4);
+    __builtin_memcpy(raw, row + c, 8 * sizeof(T));
     unpack8<T>(raw, v);
   } else {
 #pragma unroll
@@ -66,21 +68,16 @@ __device__ __forceinline__ void load_piece(const T *row, int i, int t, int cols,
   }
 }
 
-template <typename T, typename Map, bool VEC>
+template <typename T, typename Map>
 __device__ __forceinline__ void store_piece(T *row, int i, int t, int cols, const float (&v)[8]) {
   const int c = Map::col(i, 0, t);
-  if (VEC && c + 8 <= cols) {
+  if (c + 8 <= cols) {
     typedef T t8 __attribute__((ext_vector_type(8)));
     t8 o;
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = (T)v[j];
-    if constexpr (sizeof(T) == 4) {
-      const v4i *r = reinterpret_cast<const v4i *>(&o);
-      *reinterpret_cast<v4i *>(row + c) = r[0];
-      *reinterpret_cast<v4i *>(row + c + 4) = r[1];
-    } else {
-      *reinterpret_cast<v4i *>(row + c) = __builtin_bit_cast(v4i, o);
-    }
+#pragma unroll
+    for (int q = 0; q < (int)sizeof(T) / 2; ++q) reinterpret_cast<v4i_any *>(row + c)[q] = reinterpret_cast<const v4i *>(&o)[q];
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -90,12 +87,12 @@ __device__ __forceinline__ void store_piece(T *row, int i, int t, int cols, cons
   }
 }
 
-template <typename Map, bool VEC>
+template <typename Map>
 __device__ __forceinline__ void store_codes(int8_t *row, int i, int t, int cols, const int (&q)[8]) {
   const int c = Map::col(i, 0, t);
-  if (VEC && c + 8 <= cols) {
+  if (c + 8 <= cols) {
     const v2i o{(int)pack4(q[0], q[1], q[2], q[3]), (int)pack4(q[4], q[5], q[6], q[7])};
-    *reinterpret_cast<v2i *>(row + c) = o;
+    __builtin_memcpy(row + c, &o, 8);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
