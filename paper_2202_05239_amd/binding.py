@@ -460,17 +460,21 @@ def _real(t):
     return kind
 
 
+# The small calls of a decoding step are bound by this file, not by the GPU: tensors that a call makes itself are not checked, and
+# an attribute of a tensor is read once.
+
 def _matrix(t, shape=None):
     """The row stride of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError("expected a matrix with contiguous rows, got shape %s, strides %s" % (tuple(t.shape), t.stride()))
-    if shape is not None and t.shape != shape:
-        raise ValueError("expected shape %s, got %s" % (tuple(shape), tuple(t.shape)))
-    # (a single row may report any stride)
-    return max(t.stride(0), t.shape[1])
+    have, st = t.shape, t.stride()
+    if len(have) != 2 or (st[1] != 1 and have[1] > 1):
+        raise ValueError("expected a matrix with contiguous rows, got shape %s, strides %s" % (tuple(have), st))
+    if shape is not None and have != shape:
+        raise ValueError("expected shape %s, got %s" % (tuple(shape), tuple(have)))
+    return st[0] if st[0] >= have[1] else have[1]        # (a single row may report any stride)
 
 
 def _vector(t, n, dtype=None):
+    """Address of a contiguous vector of n elements, or None."""
     if t is None:
         return None
     if t.numel() != n or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
@@ -479,31 +483,41 @@ def _vector(t, n, dtype=None):
 
 
 def _scratch(workspace, n, device):
-    """(tensor, its bytes) of at least n bytes; a tensor made here goes back to torch's allocator after the launch, which hands it
+    """(address, bytes, tensor) of at least n bytes; a tensor made here goes back to torch's allocator after the launch, which hands it
     on in the order of the stream."""
-    if n == 0:
-        return None, 0
     if workspace is None:
+        if n == 0:
+            return None, 0, None
         workspace = torch.empty(n, dtype=torch.uint8, device=device)
-    return workspace, workspace.numel() * workspace.element_size()
+        return workspace.data_ptr(), n, workspace
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def f8_quant_tokens(x, gate=None, act=None, values=False, out=None, scale=None):
     """Tokens x [rows][cols] (times act(gate)) into 8 bits with a scale each: (codes int8, scale), or with values=True what the
     codes stand for, in x's type: (values, scale)."""
-    rows, cols = x.shape
-    kind = _real(x)
+    kind, ldx, shape, dtype = _real(x), _matrix(x), x.shape, x.dtype
+    rows, cols = shape
     if out is None:
-        out = torch.empty(rows, cols, dtype=x.dtype if values else torch.int8, device=x.device)
-    elif out.dtype != (x.dtype if values else torch.int8):
-        raise TypeError("out has to be %s" % (x.dtype if values else torch.int8))
+        out, ldy = torch.empty(shape, dtype=dtype if values else torch.int8, device=x.device), cols
+    else:
+        ldy = _matrix(out, shape)
+        if out.dtype != (dtype if values else torch.int8):
+            raise TypeError("out has to be %s" % (dtype if values else torch.int8))
     if scale is None:
         scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-    if gate is not None and gate.dtype != x.dtype:
-        raise TypeError("gate has to be in the type of x")
-    d = f8_quant_tokens_desc(rows, cols, kind, kind if values else F8_S8, _ACT[act], _matrix(x), 0 if gate is None else _matrix(gate, x.shape),
-                             _matrix(out, x.shape))
-    _check(lib().f8_quant_tokens(x.data_ptr(), _ptr(gate), out.data_ptr(), _vector(scale, rows, torch.float32), d, _stream()), "f8_quant_tokens")
+        at_scale = scale.data_ptr()
+    else:
+        at_scale = _vector(scale, rows, torch.float32)
+    ldg, at_gate = 0, None
+    if gate is not None:
+        if gate.dtype != dtype:
+            raise TypeError("gate has to be in the type of x")
+        ldg, at_gate = _matrix(gate, shape), gate.data_ptr()
+    d = f8_quant_tokens_desc(rows, cols, kind, kind if values else F8_S8, _ACT[act], ldx, ldg, ldy)
+    rc = (_lib or lib()).f8_quant_tokens(x.data_ptr(), at_gate, out.data_ptr(), at_scale, d, _stream())
+    if rc:
+        raise F8Error(rc, "f8_quant_tokens")
     return out, scale
 
 
@@ -511,116 +525,141 @@ def f8_norm_tokens(a, res=None, post=None, post_w=None, post_b=None, gate=None, 
                    pre_b=None, eps=1e-6, post_eps=None, codes=False, keep_res=True, res_out=None, out=None, scale=None):
     """r = res_scale * res + gate * post(a), y = pre(r) over rows [rows][cols].  post, pre: None, "rms" or "layer".  Returns
     (r, y), or with codes=True (r, codes, scale); r is None with keep_res=False.  gate [n][cols]: gate_rows rows share a row of it."""
-    rows, cols = a.shape
-    kind = _real(a)
-    w = next((t for t in (post_w, post_b, pre_w, pre_b) if t is not None), a)
-    w_kind = _real(w)
-    for t in (post_w, post_b, pre_w, pre_b):
-        if t is not None and t.dtype != w.dtype:
-            raise TypeError("the weights have to be of one type")
-    for t in (res, gate, res_out, None if codes else out):
-        if t is not None and t.dtype != a.dtype:
-            raise TypeError("a, res, gate and the results have to be of one type")
-    ldg = 0
+    kind, lda, shape, dtype = _real(a), _matrix(a), a.shape, a.dtype
+    rows, cols = shape
+    w_type, at_w = None, [None] * 4
+    for i, t in enumerate((post_w, post_b, pre_w, pre_b)):
+        if t is not None:
+            w_type = w_type or t.dtype
+            at_w[i] = _vector(t, cols, w_type)
+    ldr = ldg = ldo = 0
+    if res is not None:
+        ldr = _matrix(res, shape)
+        if res.dtype != dtype:
+            raise TypeError("res has to be in the type of a")
     if gate is not None:
         gate_rows = rows if gate_rows is None else int(gate_rows)
         ldg = _matrix(gate)
+        if gate.dtype != dtype:
+            raise TypeError("gate has to be in the type of a")
         if gate_rows < 1 or gate.shape[1] != cols or gate.shape[0] * gate_rows < rows:
             raise ValueError("gate %s does not cover %d rows of %d, %d to a row of it" % (tuple(gate.shape), rows, cols, gate_rows))
-    if keep_res and res_out is None:
-        res_out = torch.empty(rows, cols, dtype=a.dtype, device=a.device)
-    if out is None:
-        out = torch.empty(rows, cols, dtype=torch.int8 if codes else a.dtype, device=a.device)
-    elif codes and out.dtype != torch.int8:
-        raise TypeError("out has to be int8")
+    if res_out is not None:
+        ldo = _matrix(res_out, shape)
+        if res_out.dtype != dtype:
+            raise TypeError("res_out has to be in the type of a")
+    elif keep_res:
+        res_out, ldo = torch.empty(shape, dtype=dtype, device=a.device), cols
+    if out is not None:
+        ldy = _matrix(out, shape)
+        if out.dtype != (torch.int8 if codes else dtype):
+            raise TypeError("out has to be %s" % (torch.int8 if codes else dtype))
+    else:
+        out, ldy = torch.empty(shape, dtype=torch.int8 if codes else dtype, device=a.device), cols
     if codes and scale is None:
         scale = torch.empty(rows, dtype=torch.float32, device=a.device)
-    d = f8_norm_tokens_desc(rows, cols, kind, F8_S8 if codes else kind, w_kind, _NORM[post], _NORM[pre], gate_rows or 0,
-                            eps if post_eps is None else post_eps, eps, res_scale, _matrix(a), 0 if res is None else _matrix(res, a.shape),
-                            ldg, 0 if res_out is None else _matrix(res_out, a.shape), _matrix(out, a.shape))
-    _check(lib().f8_norm_tokens(a.data_ptr(), _ptr(res), _vector(post_w, cols), _vector(post_b, cols), _ptr(gate), _vector(pre_w, cols),
-                                _vector(pre_b, cols), _ptr(res_out), out.data_ptr(), _vector(scale, rows, torch.float32) if codes else None,
-                                d, _stream()), "f8_norm_tokens")
+    d = f8_norm_tokens_desc(rows, cols, kind, F8_S8 if codes else kind, _REAL.get(w_type, F8_S8) if w_type else kind, _NORM[post], _NORM[pre],
+                            gate_rows or 0, eps if post_eps is None else post_eps, eps, res_scale, lda, ldr, ldg, ldo, ldy)
+    rc = (_lib or lib()).f8_norm_tokens(a.data_ptr(), _ptr(res), at_w[0], at_w[1], _ptr(gate), at_w[2], at_w[3], _ptr(res_out), out.data_ptr(),
+                                        _vector(scale, rows, torch.float32) if codes else None, d, _stream())
+    if rc:
+        raise F8Error(rc, "f8_norm_tokens")
     return (res_out, out, scale) if codes else (res_out, out)
 
 
-def _linear_desc(x, w, y, y_dtype):
-    (M, K), N = x.shape, w.shape[0]
+def _linear_desc(x, x_type, w, y, y_dtype):
+    ldx, (M, K), (N, Kw) = _matrix(x), x.shape, w.shape
     if w.dtype != torch.int8:
         raise TypeError("the weights have to be int8")
+    if Kw != K:
+        raise ValueError("tokens of %d columns and weights of %d" % (K, Kw))
     if y is None:
-        y = torch.empty(M, N, dtype=y_dtype or torch.bfloat16, device=x.device)
-    d = f8_linear_desc(M, N, K, F8_S8 if x.dtype == torch.int8 else _real(x), _real(y), _matrix(x), _matrix(w, (N, K)), _matrix(y, (M, N)))
-    return d, y
+        y, ldy = torch.empty((M, N), dtype=y_dtype, device=x.device), N
+    else:
+        ldy = _matrix(y, (M, N))
+    return f8_linear_desc(M, N, K, x_type, _real(y), ldx, _matrix(w), ldy), y, M, N
 
 
 def f8_linear_scaled(x, sx, w, sw, bias=None, y=None, y_dtype=None):
-    """y[m][n] = sx[m] sw[n] sum_k x[m][k] w[n][k] (+ bias[n]) from int8 tokens x [M][K] and weights w [N][K]."""
+    """y[m][n] = sx[m] sw[n] sum_k x[m][k] w[n][k] (+ bias[n]) from int8 tokens x [M][K] and weights w [N][K], in bfloat16 if
+    nothing else is asked for."""
     if x.dtype != torch.int8:
         raise TypeError("the tokens have to be int8")
-    d, y = _linear_desc(x, w, y, y_dtype)
-    _check(lib().f8_linear_scaled(x.data_ptr(), _vector(sx, d.M, torch.float32), w.data_ptr(), _vector(sw, d.N, torch.float32),
-                                  _vector(bias, d.N, torch.float32), y.data_ptr(), d, _stream()), "f8_linear_scaled")
+    d, y, M, N = _linear_desc(x, F8_S8, w, y, y_dtype or torch.bfloat16)
+    rc = (_lib or lib()).f8_linear_scaled(x.data_ptr(), _vector(sx, M, torch.float32), w.data_ptr(), _vector(sw, N, torch.float32),
+                                          _vector(bias, N, torch.float32), y.data_ptr(), d, _stream())
+    if rc:
+        raise F8Error(rc, "f8_linear_scaled")
     return y
 
 
 def f8_linear_tokens(x, w, sw, bias=None, y=None, y_dtype=None, workspace=None):
     """The same from real tokens, which are quantised on the way; y in x's type if nothing else is asked for."""
-    d, y = _linear_desc(x, w, y, y_dtype or x.dtype)
-    workspace, n = _scratch(workspace, lib().f8_linear_workspace_bytes(d.M, d.K), x.device)
-    _check(lib().f8_linear_tokens(x.data_ptr(), w.data_ptr(), _vector(sw, d.N, torch.float32), _vector(bias, d.N, torch.float32), y.data_ptr(),
-                                  d, _ptr(workspace), n, _stream()), "f8_linear_tokens")
+    d, y, M, N = _linear_desc(x, _real(x), w, y, y_dtype or x.dtype)
+    L = _lib or lib()
+    at_ws, n, _keep = _scratch(workspace, L.f8_linear_workspace_bytes(M, d.K), x.device)
+    rc = L.f8_linear_tokens(x.data_ptr(), w.data_ptr(), _vector(sw, N, torch.float32), _vector(bias, N, torch.float32), y.data_ptr(), d, at_ws, n,
+                            _stream())
+    if rc:
+        raise F8Error(rc, "f8_linear_tokens")
     return y
 
 
 def _kv_layout(k, v, k_scale, v_scale):
     """Layout of a cache given as arrays [pages][page_size][heads][dim] (any strides with dim contiguous)."""
-    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or (k.stride(3) != 1 and k.shape[3] > 1):
+    shape, st, dtype = k.shape, k.stride(), k.dtype
+    if len(shape) != 4 or v.shape != shape or v.dtype != dtype or v.stride() != st or st[3] != 1:
         raise ValueError("keys and values have to be two arrays [pages][page_size][heads][dim] of one layout, dim contiguous")
-    s = (0, 0, 0)
-    if k.dtype == torch.int8:
-        if k_scale is None or v_scale is None or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
-            raise TypeError("an 8-bit cache has float32 scales")
-        if k_scale.shape != k.shape[:3] or v_scale.shape != k.shape[:3] or k_scale.stride() != v_scale.stride():
-            raise ValueError("the scales have to be two arrays [pages][page_size][heads] of one layout")
-        s, kind = k_scale.stride(), F8_S8
-    else:
-        kind = _real(k)
-    return f8_kv_layout(kind, *k.shape, *k.stride()[:3], *s)
+    if dtype != torch.int8:
+        return f8_kv_layout(_real(k), *shape, *st[:3], 0, 0, 0)
+    if k_scale is None or v_scale is None or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+        raise TypeError("an 8-bit cache has float32 scales")
+    s = k_scale.stride()
+    if k_scale.shape != shape[:3] or v_scale.shape != shape[:3] or v_scale.stride() != s:
+        raise ValueError("the scales have to be two arrays [pages][page_size][heads] of one layout")
+    return f8_kv_layout(F8_S8, *shape, *st[:3], *s)
 
 
 def f8_kv_append(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None):
     """Keys and values of new tokens, [tokens][heads][dim], into the cache's slots (page * page_size + place; negative: skipped)."""
     c = _kv_layout(k_cache, v_cache, k_scale, v_scale)
-    if k.shape != v.shape or k.dtype != v.dtype or tuple(k.shape[1:]) != (c.heads, c.dim) or (c.dim > 1 and (k.stride(2) != 1 or v.stride(2) != 1)):
+    shape, ks, vs = k.shape, k.stride(), v.stride()
+    if v.shape != shape or k.dtype != v.dtype or shape[1:] != (c.heads, c.dim) or ks[2] != 1 or vs[2] != 1:
         raise ValueError("k and v have to be [tokens][%d][%d] of one type, the last dimension contiguous" % (c.heads, c.dim))
-    d = f8_kv_append_desc(k.shape[0], _real(k), k.stride(0), k.stride(1), v.stride(0), v.stride(1))
-    _check(lib().f8_kv_append(k.data_ptr(), v.data_ptr(), _vector(slots, k.shape[0], torch.int64), k_cache.data_ptr(), v_cache.data_ptr(),
-                              _ptr(k_scale), _ptr(v_scale), c, d, _stream()), "f8_kv_append")
+    tokens = shape[0]
+    d = f8_kv_append_desc(tokens, _real(k), ks[0], ks[1], vs[0], vs[1])
+    rc = (_lib or lib()).f8_kv_append(k.data_ptr(), v.data_ptr(), _vector(slots, tokens, torch.int64), k_cache.data_ptr(), v_cache.data_ptr(),
+                                      _ptr(k_scale), _ptr(v_scale), c, d, _stream())
+    if rc:
+        raise F8Error(rc, "f8_kv_append")
 
 
 def f8_attend_paged(q, k_cache, v_cache, table, lens, k_scale=None, v_scale=None, scale=None, max_len=None, out=None, workspace=None):
     """One new token per request, q [batch][q_heads][dim], over its lens[b] cached tokens, whose pages table [batch][cols] lists.
     scale: of the scores (1 / sqrt(dim)); max_len: no request is longer (as long as the table allows)."""
     c = _kv_layout(k_cache, v_cache, k_scale, v_scale)
-    B, H, D = q.shape
-    if D != c.dim or (D > 1 and q.stride(2) != 1):
+    shape, qs = q.shape, q.stride()
+    B, H, D = shape
+    if D != c.dim or qs[2] != 1:
         raise ValueError("q has to be [batch][q_heads][%d], the last dimension contiguous" % c.dim)
-    if table.dtype != torch.int32 or table.shape[0] != B:
+    rows, cols = table.shape
+    if table.dtype != torch.int32 or rows != B:
         raise ValueError("the table has to be an int32 matrix [batch][cols]")
     if out is None:
-        out = torch.empty(B, H, D, dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape or out.dtype != q.dtype or (D > 1 and out.stride(2) != 1):
-        raise ValueError("out has to be like q")
-    cols = table.shape[1]
+        out, os = torch.empty(shape, dtype=q.dtype, device=q.device), (H * D, D)
+    else:
+        os = out.stride()
+        if out.shape != shape or out.dtype != q.dtype or os[2] != 1:
+            raise ValueError("out has to be like q")
     if max_len is None:
         max_len = min(cols * c.page_size, 0x7fff0000)
-    L = lib()
-    workspace, n = _scratch(workspace, L.f8_attend_workspace_bytes(B, H, c.heads, D, max_len), q.device)
-    d = f8_attend_desc(B, H, _real(q), max_len, cols, D ** -0.5 if scale is None else scale, _matrix(table), q.stride(0), q.stride(1),
-                       out.stride(0), out.stride(1))
-    _check(L.f8_attend_paged(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), table.data_ptr(),
-                             _vector(lens, B, torch.int32), out.data_ptr(), c, d, _ptr(workspace), n, _stream()), "f8_attend_paged")
+    L = _lib or lib()
+    at_ws, n, _keep = _scratch(workspace, L.f8_attend_workspace_bytes(B, H, c.heads, D, max_len), q.device)
+    d = f8_attend_desc(B, H, _real(q), max_len, cols, D ** -0.5 if scale is None else scale, _matrix(table), qs[0], qs[1], os[0], os[1])
+    rc = L.f8_attend_paged(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), table.data_ptr(),
+                           _vector(lens, B, torch.int32), out.data_ptr(), c, d, at_ws, n, _stream())
+    if rc:
+        raise F8Error(rc, "f8_attend_paged")
     return out
 
 

@@ -73,9 +73,9 @@ __device__ __forceinline__ void normalise(float (&v)[NV][8], int form, float eps
 }
 
 template <typename T, int TPR, int NV>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_tokens_kernel(NormParams p) {
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_tokens_kernel(NormParams p) {
   typedef RowMap<TPR, NV> Map;
-  constexpr int THREADS = TPR < 256 ? 256 : TPR, RPB = THREADS / TPR, W = TPR / 64;
+  constexpr int THREADS = TPR == 64 ? 256 : TPR, RPB = THREADS / TPR, W = TPR / 64;
   __shared__ float lds[5 * (THREADS / 64)];          // a set of words for each of the five reductions of a row
   const int row = blockIdx.x * RPB + (int)threadIdx.x / TPR, t = (int)threadIdx.x % TPR;
   if (RPB > 1 && row >= p.rows) return;              // (waves on their own: no barrier below)
@@ -131,17 +131,21 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_tokens_kernel(Norm
 
 template <typename T, int TPR, int NV>
 void launch(const NormParams &p, hipStream_t s) {
-  constexpr int THREADS = TPR < 256 ? 256 : TPR, RPB = THREADS / TPR;
+  constexpr int THREADS = TPR == 64 ? 256 : TPR, RPB = THREADS / TPR;
   hipLaunchKernelGGL((norm_tokens_kernel<T, TPR, NV>), dim3((p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
 }
 
+// Threads to a row: as many as leave each one or two pieces (registers, and so workgroups to a CU, are what counts: 4096 columns with
+// 64 threads of 8 pieces 164 us where 512 of one take 90).  With a norm in front there are two reductions, which fewer threads pass
+// faster: 256 of two pieces 101 us, 512 of one 105.
 template <typename T>
 f8_status launch_row(const NormParams &p, hipStream_t s) {
   if (p.cols <= 512) launch<T, 64, 1>(p, s);
   else if (p.cols <= 1024) launch<T, 64, 2>(p, s);
   else if (p.cols <= 2048) launch<T, 256, 1>(p, s);
+  else if (p.cols <= 4096 && p.post == F8_NORM_NONE) launch<T, 512, 1>(p, s);
   else if (p.cols <= 4096) launch<T, 256, 2>(p, s);
-  else if (p.cols <= 8192) launch<T, 256, 4>(p, s);
+  else if (p.cols <= 8192) launch<T, 512, 2>(p, s);
   else if (p.cols <= 16384) launch<T, 1024, 2>(p, s);
   else launch<T, 1024, 8>(p, s);
   return launch_status();

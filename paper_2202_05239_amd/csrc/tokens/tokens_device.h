@@ -131,11 +131,12 @@ __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(
 
 struct TokenScale {
   float scale, inv;
+  uint32_t real;                          // all bits set where the scale is finite, else 0
 };
 __device__ __forceinline__ TokenScale token_scale(float amax) {
   float s = amax / 127.0f;
   s = s < 1.17549435e-38f ? 1.17549435e-38f : s;   // (false for a NaN, which stays)
-  return TokenScale{s, 1.0f / s};
+  return TokenScale{s, 1.0f / s, s < __builtin_inff() ? 0xffffffffu : 0u};
 }
 // v / scale, correctly rounded without a division for each element: the product with the reciprocal, corrected by its exact
 // remainder.  (One operation off in the last place would turn codes at ties.)
@@ -143,9 +144,12 @@ __device__ __forceinline__ float over_scale(float v, const TokenScale &s) {
   const float q = v * s.inv;
   return __builtin_fmaf(__builtin_fmaf(-q, s.scale, v), s.inv, q);
 }
+// The code in the low byte: at 1.5 * 2^23 the unit of the sum is 1, so the addition rounds half to even and leaves the integer in
+// the low bits.  Codes of a row whose scale is not finite are 0.
 __device__ __forceinline__ int code_of(float v, const TokenScale &s) {
-  const float q = __builtin_rintf(over_scale(v, s));
-  return q == q ? (int)q : 0;
+  return (int)(__float_as_uint(over_scale(v, s) + 12582912.0f) & s.real);
 }
+// The value that the code stands for; NaN where the scale is not finite (an infinite one times 0, or what is no number itself).
+__device__ __forceinline__ float value_of(float v, const TokenScale &s) { return __builtin_rintf(over_scale(v, s)) * s.scale; }
 
 }  // namespace f8
