@@ -82,7 +82,12 @@ __device__ __forceinline__ void store_scaled(const LinearParams &p, const v16i &
 
 // Tiles through LDS by its own loads, for operands whose rows start on 4 bytes.  `tile`: which (linear_tile.hip).
 f8_status launch_linear_tile(const LinearParams &p, int y_type, int tile, hipStream_t s);
-int linear_tile_of(int M, int N, int K, float *us);   // the tile that takes least, and its estimated microseconds
+// What takes least, by estimate: `tile` over tokens 0 .. M1 - 1 and channels 0 .. N1 - 1, and if that is not all, `tile2` over the rest.
+struct LinearPlan {
+  int tile, M1, N1, tile2;
+  float us;
+};
+LinearPlan linear_plan(int M, int N, int K);
 
 // At most LINEAR_FEW tokens, any strides and alignment (linear_few.hip).  x_type F8_S8: codes with scales sx; real: p.x points to the
 // tokens themselves, p.sx is not read, M * ceil(K / 512) at most LINEAR_FEW_HELD.

@@ -108,10 +108,23 @@ bool few_quantises(int M, int N, int K) {
 f8_status enqueue_linear(const LinearParams &p, int y_type, hipStream_t s) {
   // tiles: rows on 4 bytes, and within reach of 31-bit offsets inside a tile
   const bool tiles = aligned_to(p.x, 4) && aligned_to(p.w, 4) && p.ldx % 4 == 0 && p.ldw % 4 == 0 && p.ldx < (1 << 22) && p.ldw < (1 << 22);
-  float us = 0.0f;
-  const int tile = linear_tile_of(p.M, p.N, p.K, &us);
-  if (p.M <= LINEAR_FEW && (!tiles || few_us(p) < us)) return launch_linear_few(p, F8_S8, y_type, s);
-  if (tiles) return launch_linear_tile(p, y_type, tile, s);
+  const LinearPlan plan = linear_plan(p.M, p.N, p.K);
+  if (p.M <= LINEAR_FEW && (!tiles || few_us(p) < plan.us)) return launch_linear_few(p, F8_S8, y_type, s);
+  if (tiles) {
+    LinearParams part = p;
+    part.M = plan.M1, part.N = plan.N1;
+    const f8_status st = launch_linear_tile(part, y_type, plan.tile, s);
+    if (st != F8_OK || (plan.M1 == p.M && plan.N1 == p.N)) return st;
+    part = p;
+    char *y = static_cast<char *>(p.y);
+    if (plan.N1 < p.N) {
+      part.N -= plan.N1, part.w += plan.N1 * p.ldw, part.sw += plan.N1, part.y = y + plan.N1 * bytes_of(y_type);
+      if (p.bias) part.bias += plan.N1;
+    } else {
+      part.M -= plan.M1, part.x += plan.M1 * p.ldx, part.sx += plan.M1, part.y = y + plan.M1 * p.ldy * bytes_of(y_type);
+    }
+    return launch_linear_tile(part, y_type, plan.tile2, s);
+  }
   return y_type == F8_F32 ? launch_any<float>(p, s) : y_type == F8_F16 ? launch_any<f16>(p, s) : launch_any<bf16>(p, s);
 }
 

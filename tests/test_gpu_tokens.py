@@ -256,6 +256,18 @@ def test_products_of_real_tokens_are_those_of_their_codes(M, K, N):
             assert torch.equal(y, f8.f8_linear_scaled(codes, scale, wt, sw.to(DEV), y_dtype=torch.float32)), (dtype, pad)
 
 
+@pytest.mark.parametrize("M,K,N", [(4096, 1024, 5000), (5231, 1024, 6386), (5000, 2048, 4096), (7275, 512, 5251), (2570, 528, 8450)])
+def test_products_in_two_parts(M, K, N):
+    # sizes that leave a thin last round of tiles: whole rounds of one tile and a second launch over the rest, with bias and pads
+    g = torch.Generator(device=DEV).manual_seed(M)
+    x, w = (torch.randint(-128, 128, s, generator=g, device=DEV, dtype=torch.int32).to(torch.int8) for s in ((M, K), (N, K)))
+    sx, sw, b = (torch.rand(n, generator=g, device=DEV) for n in (M, N, N))
+    want = linear_ref(x, sx, w, sw, b)
+    big = torch.full((M, N + 3), 7.0, device=DEV)
+    y = f8.f8_linear_scaled(x, sx, w, sw, bias=b, y=big[:, :N])
+    assert ((y.double() - want).abs() <= 5 * U32 * (want.abs() + b.double())).all() and (big[:, N:] == 7).all()
+
+
 def test_largest_sums_are_exact():
     K = 131071
     x, w = torch.full((3, K), -128, dtype=torch.int8), torch.full((40, K), -128, dtype=torch.int8)
