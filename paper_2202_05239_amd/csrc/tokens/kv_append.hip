@@ -17,8 +17,7 @@ struct AppendParams {
   int64_t xt[2], xh[2];
   int64_t page, token, head, spage, stoken, shead, slot_count;
   int rows, dim;
-  FastDiv heads;
-  int page_size;
+  FastDiv heads, page_size;
 };
 
 template <typename T, typename C, int NV>
@@ -33,7 +32,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p) {
   const T *x = static_cast<const T *>(p.x[kv]) + token * p.xt[kv] + head * p.xh[kv];
 #pragma unroll
   for (int i = 0; i < NV; ++i) load_piece<T, Map>(x, i, l, p.dim, v[i]);
-  const int64_t page = there ? slot / p.page_size : 0, place = there ? slot - page * p.page_size : 0;
+  // (a division in 64 bits is half of this kernel: only for slots beyond 31)
+  const int64_t page = !there ? 0 : slot <= 0x7fffffff ? (int64_t)p.page_size.div((uint32_t)slot) : slot / (int64_t)p.page_size.d;
+  const int64_t place = there ? slot - page * (int64_t)p.page_size.d : 0;
   C *to = static_cast<C *>(p.cache[kv]) + page * p.page + place * p.token + head * p.head;
   if constexpr (sizeof(C) == 1) {
     uint32_t top = 0;
@@ -94,7 +95,7 @@ extern "C" f8_status f8_kv_append(const void *k, const void *v, const int64_t *s
     return F8_ERR_ALIGN;
   const AppendParams p{{k, v}, slots, {k_cache, v_cache}, {k_scale, v_scale}, {d->k_token, d->v_token}, {d->k_head, d->v_head},
                        c->page_stride, c->token_stride, c->head_stride, c->scale_page, c->scale_token, c->scale_head,
-                       (int64_t)c->pages * c->page_size, d->tokens * c->heads, c->dim, FastDiv((uint32_t)c->heads), c->page_size};
+                       (int64_t)c->pages * c->page_size, d->tokens * c->heads, c->dim, FastDiv((uint32_t)c->heads), FastDiv((uint32_t)c->page_size)};
   hipStream_t s = static_cast<hipStream_t>(stream);
   return d->type == F8_F32 ? launch_cache<float>(p, c->type, s)
                            : d->type == F8_F16 ? launch_cache<f16>(p, c->type, s) : launch_cache<bf16>(p, c->type, s);

@@ -16,18 +16,20 @@ struct LinearParams {
 
 typedef int v16i __attribute__((ext_vector_type(16)));
 
-// 16 bytes of a row from column k on, at any address; past the row's end zeros.
+// 16 bytes of a row from column k on, at any address; past the row's end zeros (there the row's last 16 bytes, shifted down).
 __device__ __forceinline__ v4i load_row16(const int8_t *row, bool real, int k, int K) {
-  v4i v{0, 0, 0, 0};
-  if (real && k + 16 <= K) {
-    __builtin_memcpy(&v, row + k, 16);
-  } else if (real) {
-    int8_t b[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) b[i] = k + i < K ? row[k + i] : 0;
-    __builtin_memcpy(&v, b, 16);
+  unsigned __int128 v = 0;
+  if (real && k < K) {
+    if (K >= 16) {
+      const int over = max(k + 16 - K, 0);
+      __builtin_memcpy(&v, row + k - over, 16);
+      v >>= 8 * over;
+    } else {
+#pragma nounroll
+      for (int i = k; i < K; ++i) v |= (unsigned __int128)(uint8_t)row[i] << (8 * (i - k));
+    }
   }
-  return v;
+  return __builtin_bit_cast(v4i, v);
 }
 
 // 8 real elements of a row from column k on (a multiple of 8); past the row's end zeros.
@@ -89,9 +91,10 @@ struct LinearPlan {
 };
 LinearPlan linear_plan(int M, int N, int K);
 
-// At most LINEAR_FEW tokens, any strides and alignment (linear_few.hip).  x_type F8_S8: codes with scales sx; real: p.x points to the
-// tokens themselves, p.sx is not read, M * ceil(K / 512) at most LINEAR_FEW_HELD.
+// LINEAR_FEW tokens to a workgroup, any strides and alignment (linear_few.hip).  x_type F8_S8: codes with scales sx; real: p.x points to the
+// tokens themselves, p.sx is not read, M at most
+// LINEAR_FEW, M * ceil(K / 512) at most LINEAR_FEW_HELD.
 f8_status launch_linear_few(const LinearParams &p, int x_type, int y_type, hipStream_t s);
-constexpr int LINEAR_FEW = 16, LINEAR_FEW_HELD = 16;
+constexpr int LINEAR_FEW = 16, LINEAR_FEW_HELD = 16, LINEAR_FEW_MOST = 64;
 
 }  // namespace f8

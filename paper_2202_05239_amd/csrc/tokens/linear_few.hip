@@ -1,6 +1,6 @@
-// Products of at most 16 tokens: the weights are the traffic, each byte of them is needed once.
+// Products of few tokens: the weights are the traffic, each byte of them is needed once.
 //
-// A workgroup takes 16 output channels, its eight waves a contiguous share of K each.  Weights go from memory straight into the
+// A workgroup takes 16 output channels and up to 16 tokens, its eight waves a contiguous share of K each.  Weights go from memory straight into the
 // registers that are the row operand of the 16 x 16 x 64 matrix instruction (lane l: channel l % 16, 16 bytes of K), U slices of 64
 // columns in flight per wave; the tokens are the column operand, from L2 or, where they come as real numbers, from LDS: every
 // workgroup then quantises them itself while its first weights are on their way, which saves a launch.  The waves' 32-bit sums meet
@@ -10,17 +10,31 @@
 namespace f8 {
 namespace {
 
+typedef int v4i_dword __attribute__((ext_vector_type(4), aligned(4), may_alias));
+
 constexpr int WAVES = 8, THREADS = 64 * WAVES, U = 8, HELD = LINEAR_FEW_HELD / WAVES;
 
+// 16 bytes at any address, from the dwords that cover them (each of those holds a byte that is asked for).  Sixteen rows an
+// instruction at odd addresses are what the load unit is slow at: 5 x 4467 x 4886 17.4 us with plain loads.
+template <bool ODD>
 __device__ __forceinline__ v4i load16(const int8_t *p) {
-  v4i v;
-  __builtin_memcpy(&v, p, 16);
-  return v;
+  if constexpr (!ODD) {
+    return *reinterpret_cast<const v4i_dword *>(p);
+  } else {
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
+    const int8_t *q = p - off;
+    const v4i v = *reinterpret_cast<const v4i_dword *>(q);
+    const int last = *reinterpret_cast<const int *>(q + (off ? 16 : 12));
+    return v4i{(int)__builtin_amdgcn_alignbyte(v[1], v[0], off), (int)__builtin_amdgcn_alignbyte(v[2], v[1], off),
+               (int)__builtin_amdgcn_alignbyte(v[3], v[2], off), (int)__builtin_amdgcn_alignbyte(last, v[3], off)};
+  }
 }
 
-// X: int8_t, or the real type of tokens that are quantised here.
-template <typename T, typename X>
+// X: int8_t, or the real type of tokens that are quantised here.  ODD: rows that do not all start on 4 bytes.
+template <typename T, typename X, bool ODD>
 __global__ __launch_bounds__(THREADS) void linear_few_kernel(LinearParams p) {
+  const int m0 = blockIdx.y * LINEAR_FEW;
+  p.M = min(p.M - m0, LINEAR_FEW);
   constexpr bool REAL = sizeof(X) > 1;
   __shared__ int sums[256];
   __shared__ uint32_t tops[LINEAR_FEW];
@@ -37,7 +51,7 @@ __global__ __launch_bounds__(THREADS) void linear_few_kernel(LinearParams p) {
   v4i fw[U];
   if (whole(first)) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) fw[u] = load16(w + (first + u) * 64);
+    for (int u = 0; u < U; ++u) fw[u] = load16<ODD>(w + (first + u) * 64);
   }
   if constexpr (REAL) {
     const X *x = reinterpret_cast<const X *>(p.x);
@@ -79,19 +93,19 @@ __global__ __launch_bounds__(THREADS) void linear_few_kernel(LinearParams p) {
     }
   }
   __syncthreads();
-  const int8_t *x = REAL ? codes + m * pitch + g * 16 : p.x + m * p.ldx + g * 16;
+  const int8_t *x = REAL ? codes + m * pitch + g * 16 : p.x + (m0 + m) * p.ldx + g * 16;
   v4i acc{0, 0, 0, 0};
   int t = first;
   while (whole(t)) {
     v4i fx[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) fx[u] = REAL ? *reinterpret_cast<const v4i *>(x + (t + u) * 64) : load16(x + (t + u) * 64);
+    for (int u = 0; u < U; ++u) fx[u] = REAL ? *reinterpret_cast<const v4i *>(x + (t + u) * 64) : load16<ODD>(x + (t + u) * 64);
 #pragma unroll
     for (int u = 0; u < U; ++u) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u], fx[u], acc, 0, 0, 0);
     t += U;
     if (whole(t)) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) fw[u] = load16(w + (t + u) * 64);
+      for (int u = 0; u < U; ++u) fw[u] = load16<ODD>(w + (t + u) * 64);
     }
   }
   for (; t < last; ++t) {
@@ -105,15 +119,18 @@ __global__ __launch_bounds__(THREADS) void linear_few_kernel(LinearParams p) {
   if (threadIdx.x < 256) {
     const int row = threadIdx.x / 16, n = n0 + threadIdx.x % 16;
     if (row < p.M && n < p.N)
-      static_cast<T *>(p.y)[row * p.ldy + n] =
-          (T)__builtin_fmaf((float)sums[threadIdx.x] * (REAL ? scales[row] : p.sx[row]), p.sw[n], p.bias ? p.bias[n] : 0.0f);
+      static_cast<T *>(p.y)[(m0 + row) * p.ldy + n] =
+          (T)__builtin_fmaf((float)sums[threadIdx.x] * (REAL ? scales[row] : p.sx[m0 + row]), p.sw[n], p.bias ? p.bias[n] : 0.0f);
   }
 }
 
 template <typename T, typename X>
 f8_status launch(const LinearParams &p, hipStream_t s) {
   const size_t lds = sizeof(X) > 1 ? (size_t)p.M * ((p.K + 63) / 64 * 64 + 16) : 0;
-  hipLaunchKernelGGL((linear_few_kernel<T, X>), dim3((p.N + 15) / 16), dim3(THREADS), lds, s, p);
+  const dim3 grid((p.N + 15) / 16, (p.M + LINEAR_FEW - 1) / LINEAR_FEW);
+  const bool even = aligned_to(p.w, 4) && p.ldw % 4 == 0 && (sizeof(X) > 1 || (aligned_to(p.x, 4) && p.ldx % 4 == 0));
+  if (even) hipLaunchKernelGGL((linear_few_kernel<T, X, false>), grid, dim3(THREADS), lds, s, p);
+  else hipLaunchKernelGGL((linear_few_kernel<T, X, true>), grid, dim3(THREADS), lds, s, p);
   return launch_status();
 }
 

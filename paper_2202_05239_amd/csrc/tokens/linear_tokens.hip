@@ -4,75 +4,99 @@
 //
 // scaled in 32-bit floating point and rounded once to the type of y.
 //
-// Three kernels: at most 16 tokens, where the weights are the traffic (linear_few.hip); tiles through LDS for rows that start on 4
-// bytes (linear_tile.hip); and linear_any_kernel here for any stride and alignment: 128 x 128 outputs per workgroup, weights as the
-// row operand of the 32 x 32 x 32 matrix instruction in the channel order of f8_device.h (weight_row), so that a lane ends with 16
-// neighbouring channels of one token and stores them from its registers; operands go through registers into two LDS buffers.  It
-// takes 1.4 to 2.6 times as long as the tiles (1531 x 4096 x 5008 49 us against 35.5, 64 x 4096 x 4096 37 against 8.6, 8192 x 8192 x
-// 8192 857 against 462): unaligned 16-byte pieces, one K step of 64 ahead.
+// Three kernels: few tokens, where the weights are the traffic (linear_few.hip); tiles through LDS for rows that start on 4 bytes
+// (linear_tile.hip); and linear_any_kernel here for any stride and alignment: 128 x 128 or 64 x 64 outputs per workgroup, weights as
+// the row operand of the 32 x 32 x 32 matrix instruction in the channel order of f8_device.h (weight_row), so that a lane ends with
+// 16 neighbouring channels of one token and stores them from its registers; operands go through two sets of registers into two LDS
+// buffers, two steps of 128 columns ahead.  Every 16-byte piece off the grid is two lines: 4096 x 4097 x 4096 takes 141 us, 4096 x
+// 4096 x 4096 on tiles 65; 1531 x 4097 x 5001 73 us, 1531 x 4100 x 5001 43.
 #include "linear.h"
 
 namespace f8 {
 namespace {
 
-constexpr int ANY_TILE = 128, ANY_K = 64, ANY_PITCH = ANY_K + 16;
+constexpr int ANY_K = 128, ANY_PITCH = ANY_K + 16;       // (rows 36 words apart: sixteen neighbours' pieces lie on all 64 banks)
 
-template <typename T>
-__global__ __launch_bounds__(256) void linear_any_kernel(LinearParams p, int tiles_m) {
-  __shared__ uint8_t lds[2][2 * ANY_TILE * ANY_PITCH];
+template <typename T, int TILE>
+__global__ __launch_bounds__(256, 2) void linear_any_kernel(LinearParams p, int tiles_m) {
+  constexpr int WT = TILE / 2, BL = WT / 32, PIECES = TILE * ANY_K / 16 / 256;      // a wave's share of a side, its blocks, 16-byte pieces per thread
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2][2 * TILE * ANY_PITCH];
   const int tile = (int)xcd_remap(blockIdx.x, gridDim.x);
-  const int m0 = tile % tiles_m * ANY_TILE, n0 = tile / tiles_m * ANY_TILE;
+  const int m0 = tile % tiles_m * TILE, n0 = tile / tiles_m * TILE;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
-  const int wn = (wave & 1) * 64, wm = (wave >> 1) * 64;
-  const int row = threadIdx.x >> 2, piece = threadIdx.x & 3;    // 64 rows x 4 pieces of 16 bytes at a time
-  v4i st[4];
-  auto load = [&](int k0) {
+  const int wn = (wave & 1) * WT, wm = (wave >> 1) * WT;
+  const int row = threadIdx.x >> 3, piece = (threadIdx.x & 7) * 16;               // 32 rows at a time
+  // (rows past the end read the last one's; their results are not stored)
+  const int8_t *w[PIECES], *x[PIECES];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int n = n0 + row + 64 * h, m = m0 + row + 64 * h, k = k0 + piece * 16;
-      st[h] = load_row16(p.w + n * p.ldw, n < p.N, k, p.K);
-      st[2 + h] = load_row16(p.x + m * p.ldx, m < p.M, k, p.K);
+  for (int h = 0; h < PIECES; ++h) w[h] = p.w + min(n0 + row + 32 * h, p.N - 1) * p.ldw, x[h] = p.x + min(m0 + row + 32 * h, p.M - 1) * p.ldx;
+  v4i st[2][2 * PIECES];
+  auto load = [&](int set, int k0) {
+    if (k0 + ANY_K <= p.K) {
+#pragma unroll
+      for (int h = 0; h < PIECES; ++h) {
+        __builtin_memcpy(&st[set][h], w[h] + k0 + piece, 16);
+        __builtin_memcpy(&st[set][PIECES + h], x[h] + k0 + piece, 16);
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < PIECES; ++h) {
+        st[set][h] = load_row16(w[h], true, k0 + piece, p.K);
+        st[set][PIECES + h] = load_row16(x[h], true, k0 + piece, p.K);
+      }
     }
   };
-  auto put = [&](int buf) {
+  auto put = [&](int set) {
 #pragma unroll
-    for (int h = 0; h < 4; ++h) *reinterpret_cast<v4i *>(&lds[buf][((h & 1) * 64 + row + (h >> 1) * ANY_TILE) * ANY_PITCH + piece * 16]) = st[h];
+    for (int h = 0; h < 2 * PIECES; ++h)
+      *reinterpret_cast<v4i *>(&lds[set][(h % PIECES * 32 + row + h / PIECES * TILE) * ANY_PITCH + piece]) = st[set][h];
   };
-  v16i acc[2][2] = {};
-  const int steps = (p.K + ANY_K - 1) / ANY_K;
-  load(0);
-  put(0);
-  for (int s = 0; s < steps; ++s) {
-    if (s + 1 < steps) load((s + 1) * ANY_K);
+  v16i acc[BL][BL] = {};
+  auto step = [&](int set, int k0) {      // the operands of k0 lie in LDS, those of the next step are in the registers of the other set
+    load(set, k0 + 2 * ANY_K);
     __syncthreads();
-    const uint8_t *b = lds[s & 1];
+    const uint8_t *b = lds[set];
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      v4i fw[2], fx[2];
+    for (int ks = 0; ks < ANY_K / 32; ++ks) {
+      v4i fw[BL], fx[BL];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < BL; ++i) {
         fw[i] = *reinterpret_cast<const v4i *>(b + (wn + 32 * i + weight_row(l32)) * ANY_PITCH + ks * 32 + half * 16);
-        fx[i] = *reinterpret_cast<const v4i *>(b + (ANY_TILE + wm + 32 * i + l32) * ANY_PITCH + ks * 32 + half * 16);
+        fx[i] = *reinterpret_cast<const v4i *>(b + (TILE + wm + 32 * i + l32) * ANY_PITCH + ks * 32 + half * 16);
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < BL; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[i], fx[j], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < BL; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[i], fx[j], acc[i][j], 0, 0, 0);
     }
-    if (s + 1 < steps) put((s + 1) & 1);
+    put(set ^ 1);
+  };
+  load(0, 0);
+  load(1, ANY_K);
+  put(0);
+  for (int k = 0; k < p.K; k += 2 * ANY_K) {
+    step(0, k);
+    if (k + ANY_K < p.K) step(1, k + ANY_K);
   }
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < BL; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) store_scaled<T>(p, acc[i][j], m0 + wm + 32 * j + l32, n0 + wn + 32 * i + 16 * half);
+    for (int j = 0; j < BL; ++j) store_scaled<T>(p, acc[i][j], m0 + wm + 32 * j + l32, n0 + wn + 32 * i + 16 * half);
 }
 
+template <typename T, int TILE>
+f8_status launch_any_tile(const LinearParams &p, hipStream_t s) {
+  const int64_t tm = (p.M + TILE - 1) / TILE, tn = (p.N + TILE - 1) / TILE;
+  if (tm * tn > 0x7fffffff) return F8_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((linear_any_kernel<T, TILE>), dim3((unsigned)(tm * tn)), dim3(256), 0, s, p, (int)tm);
+  return launch_status();
+}
+
+// Tiles of 64 where those of 128 would leave CUs without one.
 template <typename T>
 f8_status launch_any(const LinearParams &p, hipStream_t s) {
-  const int64_t tm = (p.M + ANY_TILE - 1) / ANY_TILE, tn = (p.N + ANY_TILE - 1) / ANY_TILE;
-  if (tm * tn > 0x7fffffff) return F8_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL(linear_any_kernel<T>, dim3((unsigned)(tm * tn)), dim3(256), 0, s, p, (int)tm);
-  return launch_status();
+  const int64_t tiles = (int64_t)((p.M + 127) / 128) * ((p.N + 127) / 128);
+  return tiles < 256 ? launch_any_tile<T, 64>(p, s) : launch_any_tile<T, 128>(p, s);
 }
 
 f8_status check(const f8_linear_desc *d) {
@@ -89,11 +113,14 @@ f8_status check_pointers(const void *x, const void *w, const float *sw, const fl
   return F8_OK;
 }
 
-// What linear_few_kernel takes: its weights at 5.9 TB/s, and every workgroup's reads of the tokens from L2 at 20.  Measured (us):
-// 1 x 4096 x 4096 5.5, 16 x 4096 x 4096 6.5, 1 x 16384 x 4096 13.8, 16 x 4096 x 16384 17.2; the best tile takes 8.0, 8.2, 18.5 and 12.6.
+// What linear_few_kernel takes: its weights at 5.9 TB/s (once more from L2 for every further 16 tokens), every workgroup's reads of
+// the tokens from L2, and at least a memory latency for each batch of 8 slices that a wave walks through.  Measured (us): 1 x 4096 x
+// 4096 5.5, 16 x 4096 x 4096 6.5, 1 x 16384 x 4096 13.8, 16 x 4096 x 16384 17.2; the best tile takes 8.0, 8.2, 18.5 and 12.6.
 float few_us(const LinearParams &p) {
-  const float bytes = (float)p.N * (float)p.K;
-  return 2.5f + bytes / 5.9e6f + bytes * (float)p.M / 16.0f / 20e6f;
+  const float bytes = (float)p.N * (float)p.K, blocks = (float)((p.M + LINEAR_FEW - 1) / LINEAR_FEW);
+  const float traffic = bytes / 5.9e6f + bytes * (blocks - 1.0f) / 12e6f + bytes * (float)p.M / 16.0f / 20e6f;
+  const float batches = 0.9f * (float)((p.K + 4095) / 4096);
+  return 2.5f + (traffic > batches ? traffic : batches);
 }
 
 // Whether linear_few_kernel also quantises the tokens.  A launch less is 2.3 us; every workgroup repeating the work costs about half of
@@ -109,7 +136,7 @@ f8_status enqueue_linear(const LinearParams &p, int y_type, hipStream_t s) {
   // tiles: rows on 4 bytes, and within reach of 31-bit offsets inside a tile
   const bool tiles = aligned_to(p.x, 4) && aligned_to(p.w, 4) && p.ldx % 4 == 0 && p.ldw % 4 == 0 && p.ldx < (1 << 22) && p.ldw < (1 << 22);
   const LinearPlan plan = linear_plan(p.M, p.N, p.K);
-  if (p.M <= LINEAR_FEW && (!tiles || few_us(p) < plan.us)) return launch_linear_few(p, F8_S8, y_type, s);
+  if (tiles ? p.M <= LINEAR_FEW_MOST && few_us(p) < plan.us : p.M <= LINEAR_FEW) return launch_linear_few(p, F8_S8, y_type, s);
   if (tiles) {
     LinearParams part = p;
     part.M = plan.M1, part.N = plan.N1;
