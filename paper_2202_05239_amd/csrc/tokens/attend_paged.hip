@@ -604,7 +604,7 @@ f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cach
     return F8_ERR_ALIGN;
   const int group = d->q_heads / c->heads, chunks = (group + HEADS - 1) / HEADS, row = group < HEADS ? group : HEADS;
   const int64_t pairs = (int64_t)d->batch * c->heads * chunks;
-  if (pairs > 0x7fffffffLL) return F8_ERR_UNSUPPORTED;
+  if (pairs > 1 << 22) return F8_ERR_UNSUPPORTED;          // (workgroups of a launch)
   const int wgs = wgs_of(pairs, c->dim, d->max_len);
   if (wgs) {
     if (!workspace) return F8_ERR_NULL;

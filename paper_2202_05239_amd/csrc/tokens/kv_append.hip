@@ -23,9 +23,10 @@ struct AppendParams {
 template <typename T, typename C, int NV>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p) {
   typedef RowMap<LANES, NV> Map;
-  const int row = blockIdx.x * (256 / LANES) + (int)threadIdx.x / LANES, l = (int)threadIdx.x % LANES, kv = blockIdx.y;
+  const int64_t row = row_block() * (256 / LANES) + (int)threadIdx.x / LANES;
+  const int l = (int)threadIdx.x % LANES, kv = blockIdx.z;
   if (row >= p.rows) return;
-  const int token = (int)p.heads.div((uint32_t)row), head = row - token * (int)p.heads.d;
+  const int token = (int)p.heads.div((uint32_t)row), head = (int)row - token * (int)p.heads.d;
   const int64_t slot = p.slots[token];
   const bool there = slot >= 0 && slot < p.slot_count;
   float v[NV][8];
@@ -63,7 +64,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p) {
 
 template <typename T, typename C>
 f8_status launch(const AppendParams &p, hipStream_t s) {
-  const dim3 grid((p.rows + 256 / LANES - 1) / (256 / LANES), 2), block(256);
+  dim3 grid = block_grid(((int64_t)p.rows + 256 / LANES - 1) / (256 / LANES));
+  const dim3 block(256);
+  grid.z = 2;
   if (p.dim <= LANES * 8) hipLaunchKernelGGL((kv_append_kernel<T, C, 1>), grid, block, 0, s, p);
   else hipLaunchKernelGGL((kv_append_kernel<T, C, 2>), grid, block, 0, s, p);
   return launch_status();

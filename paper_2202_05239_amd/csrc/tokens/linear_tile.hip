@@ -199,7 +199,7 @@ template <typename T, int WN, int WM, int NB, int MB, int RING, int KG>
 f8_status launch(const LinearParams &p, hipStream_t s) {
   constexpr int BN = 32 * NB * WN, BM = 32 * MB * WM;
   const int64_t tn = (p.N + BN - 1) / BN, tm = (p.M + BM - 1) / BM;
-  if (tn * tm > 0x7fffffff) return F8_ERR_UNSUPPORTED;
+  if (tn * tm > LINEAR_TILES_MOST) return F8_ERR_UNSUPPORTED;
   hipLaunchKernelGGL((linear_tile_kernel<T, WN, WM, NB, MB, RING, KG>), dim3((unsigned)(tn * tm)), dim3(64 * WN * WM * KG), 0, s, p, (int)tm, (int)tn);
   return launch_status();
 }

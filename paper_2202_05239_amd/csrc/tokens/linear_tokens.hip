@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256, 2) void linear_any_kernel(LinearParams p, int 
 template <typename T, int TILE>
 f8_status launch_any_tile(const LinearParams &p, hipStream_t s) {
   const int64_t tm = (p.M + TILE - 1) / TILE, tn = (p.N + TILE - 1) / TILE;
-  if (tm * tn > 0x7fffffff) return F8_ERR_UNSUPPORTED;
+  if (tm * tn > LINEAR_TILES_MOST) return F8_ERR_UNSUPPORTED;
   hipLaunchKernelGGL((linear_any_kernel<T, TILE>), dim3((unsigned)(tm * tn)), dim3(256), 0, s, p, (int)tm);
   return launch_status();
 }
@@ -101,7 +101,7 @@ f8_status launch_any(const LinearParams &p, hipStream_t s) {
 
 f8_status check(const f8_linear_desc *d) {
   if (!d) return F8_ERR_NULL;
-  if (d->M < 0 || d->N < 0 || d->K < 1 || d->K > F8_LINEAR_MAX_K) return F8_ERR_SHAPE;
+  if (d->M < 0 || d->N < 0 || d->M > F8_LINEAR_MAX_ROWS || d->N > F8_LINEAR_MAX_ROWS || d->K < 1 || d->K > F8_LINEAR_MAX_K) return F8_ERR_SHAPE;
   if (!real_type(d->y_type)) return F8_ERR_DTYPE;
   if (d->ldx < d->K || d->ldw < d->K || d->ldy < d->N) return F8_ERR_SHAPE;
   return F8_OK;

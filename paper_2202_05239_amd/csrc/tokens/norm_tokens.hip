@@ -77,8 +77,9 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_tokens_kernel(Norm
   typedef RowMap<TPR, NV> Map;
   constexpr int THREADS = TPR == 64 ? 256 : TPR, RPB = THREADS / TPR, W = TPR / 64;
   __shared__ float lds[5 * (THREADS / 64)];          // a set of words for each of the five reductions of a row
-  const int row = blockIdx.x * RPB + (int)threadIdx.x / TPR, t = (int)threadIdx.x % TPR;
-  if (RPB > 1 && row >= p.rows) return;              // (waves on their own: no barrier below)
+  const int64_t row = row_block() * RPB + (int)threadIdx.x / TPR;
+  const int t = (int)threadIdx.x % TPR;
+  if (row >= p.rows) return;                         // (a whole workgroup, or waves on their own: no barrier below)
   float v[NV][8];
 #pragma unroll
   for (int i = 0; i < NV; ++i) load_piece<T, Map>(static_cast<const T *>(p.a) + row * p.lda, i, t, p.cols, v[i]);
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_tokens_kernel(Norm
 template <typename T, int TPR, int NV>
 void launch(const NormParams &p, hipStream_t s) {
   constexpr int THREADS = TPR == 64 ? 256 : TPR, RPB = THREADS / TPR;
-  hipLaunchKernelGGL((norm_tokens_kernel<T, TPR, NV>), dim3((p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
+  hipLaunchKernelGGL((norm_tokens_kernel<T, TPR, NV>), block_grid(((int64_t)p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
 }
 
 // Threads to a row: as many as leave each one or two pieces (registers, and so workgroups to a CU, are what counts: 4096 columns with

@@ -36,8 +36,9 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void quant_tokens_kernel(Qua
   typedef RowMap<TPR, NV> Map;
   constexpr int THREADS = TPR == 64 ? 256 : TPR, RPB = THREADS / TPR;
   __shared__ float lds[THREADS / 64];
-  const int row = blockIdx.x * RPB + (int)threadIdx.x / TPR, t = (int)threadIdx.x % TPR;
-  if (RPB > 1 && row >= p.rows) return;             // (waves on their own: no barrier below)
+  const int64_t row = row_block() * RPB + (int)threadIdx.x / TPR;
+  const int t = (int)threadIdx.x % TPR;
+  if (row >= p.rows) return;                         // (a whole workgroup, or waves on their own: no barrier below)
   const T *x = static_cast<const T *>(p.x) + row * p.ldx;
   float v[NV][8];
   uint32_t top = 0;
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void quant_tokens_kernel(Qua
 template <typename T, int TPR, int NV>
 void launch(const QuantParams &p, hipStream_t s) {
   constexpr int THREADS = TPR == 64 ? 256 : TPR, RPB = THREADS / TPR;
-  hipLaunchKernelGGL((quant_tokens_kernel<T, TPR, NV>), dim3((p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
+  hipLaunchKernelGGL((quant_tokens_kernel<T, TPR, NV>), block_grid(((int64_t)p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
 }
 
 // Threads to a row: as many as leave each one or two pieces, up to 1024 (16384 gated columns, 8192 rows, us: 1024 threads of two pieces

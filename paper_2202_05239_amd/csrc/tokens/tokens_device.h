@@ -23,6 +23,8 @@ typedef int v4i_any __attribute__((ext_vector_type(4), aligned(1), may_alias));
 
 constexpr int ROW_MOST = 65536;   // columns of a row that a workgroup holds in registers
 
+__device__ __forceinline__ int64_t row_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }   // see block_grid
+
 // How the elements of a row lie in its threads: `TPR` threads share a row, each has NV pieces of 8 neighbours, one or two 16-byte
 // accesses.  The accesses are taken at any address an element may have: this chip's loads and stores do not need alignment, a row
 // off the 16-byte grid costs up to a second line per access.

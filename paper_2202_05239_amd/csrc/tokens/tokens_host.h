@@ -13,6 +13,12 @@ inline bool real_type(int t) { return t == F8_F32 || t == F8_F16 || t == F8_BF16
 inline size_t bytes_of(int t) { return t == F8_F32 ? 4 : t == F8_F16 || t == F8_BF16 ? 2 : 1; }
 inline f8_status launch_status() { return hipGetLastError() == hipSuccess ? F8_OK : F8_ERR_DEVICE; }
 
+// A grid of `blocks` workgroups whose extents stay below 2^32 threads: kernels number them by row_block() and turn away the surplus.
+inline dim3 block_grid(int64_t blocks) {
+  const int64_t x = blocks < (1 << 21) ? blocks : 1 << 21;
+  return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+
 inline f8_status check_kv_layout(const f8_kv_layout &c) {
   if (c.type != F8_S8 && c.type != F8_F16 && c.type != F8_BF16) return F8_ERR_DTYPE;
   if (c.pages < 1 || c.page_size < 1 || c.heads < 1 || c.dim < 16 || c.dim > 256 || c.dim % 16 != 0) return F8_ERR_SHAPE;

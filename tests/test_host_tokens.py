@@ -68,7 +68,7 @@ def test_products():
     assert scaled(None) == 1
     for k in ("x", "sx", "w", "sw", "y"):
         assert scaled(l_desc(), **{k: None}) == 1, k
-    for bad in (dict(M=-1), dict(N=-1), dict(K=0), dict(K=131072, ldx=131072, ldw=131072), dict(ldx=31), dict(ldw=31), dict(ldy=7)):
+    for bad in (dict(M=-1), dict(N=-1), dict(M=(1 << 26) + 1), dict(N=(1 << 26) + 1, ldy=1 << 27), dict(K=0), dict(K=131072, ldx=131072, ldw=131072), dict(ldx=31), dict(ldw=31), dict(ldy=7)):
         assert scaled(l_desc(**bad)) == 2, bad
     assert scaled(l_desc(x_type=f8.F8_F32)) == 5 and scaled(l_desc(y_type=f8.F8_S8)) == 5
     assert scaled(l_desc(), y=ODD) == 7 and scaled(l_desc(), sx=ODD) == 7 and scaled(l_desc(), b=ODD) == 7
@@ -130,6 +130,7 @@ def test_attention():
     long = a_desc(max_len=4096, table_cols=256, table_ld=256)
     need = L.f8_attend_workspace_bytes(2, 4, 2, 64, 4096)
     assert need > 0 and att(d=long, ws=None) == 1 and att(d=long, n=need - 1) == 2 and att(d=long, ws=ctypes.c_void_p(0x1008)) == 7
+    assert att(layout(heads=512), d=a_desc(batch=65535, q_heads=512)) == 8            # more pairs than a launch has workgroups
     assert att(d=a_desc(batch=0), q=None) == 0
     assert L.f8_attend_workspace_bytes(2, 5, 2, 64, 4096) == 0 and L.f8_attend_workspace_bytes(0, 4, 2, 64, 4096) == 0
 
