@@ -20,7 +20,7 @@
 // below the rounding of the 16-bit result.  Scores, maxima, sums and outputs are 32 bits.
 //
 // Bound by HBM: every cached byte is read once, in whole rows, one tile ahead per wave (131072 tokens of 8 heads, 277 MB: 67 us with
-// the second launch, 4.2 TB/s; 64 requests of up to 8192 tokens, 491 MB: 120 us, 4.1 TB/s; a large copy reaches 5.5).  The vector units
+// the second launch, 4.2 TB/s; 64 requests of up to 8192 tokens, 491 MB: 117 us, 4.2 TB/s; a large copy reaches 5.5).  The vector units
 // are a third busy (350 instructions a tile, most of them codes into f16).  Without the tile ahead the two took 97 and 239 us; with
 // the requests' lengths cut into equal stretches, a workgroup each, instead of units dealt out evenly, 68 and 167.
 #include <math.h>
@@ -157,10 +157,14 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void attend_kernel(At
   __shared__ int from;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
   const int per_b = p.kv_heads * p.chunks, group_rows = min(p.group, HEADS);
+  // Runs that follow one another lie on one XCD, so that the heads of a request, whose scales share lines, share an L2 (64 requests of up
+  // to 8192 tokens, 491 MB: 592 MB fetched otherwise and 122 us, 563 and 117 with it).  With few requests a head is many runs, and those of the same tokens meet on
+  // an XCD by themselves.
+  const uint32_t run = p.batch >= 8 ? xcd_remap(blockIdx.x, gridDim.x) : blockIdx.x;
   int b, hc, unit, units, slot = 0;
   int64_t left;                               // units of this workgroup's run
   if (p.wgs == 0) {
-    b = blockIdx.x / per_b, hc = blockIdx.x % per_b, unit = 0, units = units_of(p, b), left = units;
+    b = (int)run / per_b, hc = (int)run % per_b, unit = 0, units = units_of(p, b), left = units;
   } else {
     // The request that holds the run's first unit: the units of 256 requests at a time, added up from the front.  (The sum of all
     // of them comes with it where there are no more requests than that.)
@@ -191,8 +195,8 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void attend_kernel(At
       at += upto - mine;
       if (i0 == 0) {
         const Runs runs(uniform64(total < 0 ? all : total), p.wgs);
-        start = runs.start(blockIdx.x);
-        left = runs.start(blockIdx.x + 1) - start;
+        start = runs.start(run);
+        left = runs.start((int64_t)run + 1) - start;
         if (left == 0) return;
       }
       if (mine > 0 && at <= start && start < at + mine) from = i, before = at;
@@ -450,7 +454,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void attend_kernel(At
       if (unit == 0 && last == units) {
         static_cast<Q *>(p.out)[b * p.ot + (hq0 + h) * p.oh + d] = (Q)(sum == 0.0f ? 0.0f : of / sum);
       } else {
-        const int64_t at = (2 * (int64_t)blockIdx.x + slot) * group_rows + h;
+        const int64_t at = (2 * (int64_t)run + slot) * group_rows + h;
         p.part_o[at * p.dim + d] = of;
         if (d == 0) p.part_ml[2 * at] = mh, p.part_ml[2 * at + 1] = sum;
       }
