@@ -97,6 +97,6 @@ LinearPlan linear_plan(int M, int N, int K);
 // tokens themselves, p.sx is not read, M at most
 // LINEAR_FEW, M * ceil(K / 512) at most LINEAR_FEW_HELD.
 f8_status launch_linear_few(const LinearParams &p, int x_type, int y_type, hipStream_t s);
-constexpr int LINEAR_FEW = 16, LINEAR_FEW_HELD = 16, LINEAR_FEW_MOST = 64;
+constexpr int LINEAR_FEW = 16, LINEAR_FEW_HELD = 16, LINEAR_FEW_MOST = 512;
 
 }  // namespace f8

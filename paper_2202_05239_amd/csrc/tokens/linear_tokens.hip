@@ -10,6 +10,8 @@
 // 16 neighbouring channels of one token and stores them from its registers; operands go through two sets of registers into two LDS
 // buffers, two steps of 128 columns ahead.  Every 16-byte piece off the grid is two lines: 4096 x 4097 x 4096 takes 141 us, 4096 x
 // 4096 x 4096 on tiles 65; 1531 x 4097 x 5001 73 us, 1531 x 4100 x 5001 43.
+#include <math.h>
+
 #include "linear.h"
 
 namespace f8 {
@@ -114,13 +116,22 @@ f8_status check_pointers(const void *x, const void *w, const float *sw, const fl
 }
 
 // What linear_few_kernel takes: its weights at 5.9 TB/s (once more from L2 for every further 16 tokens), every workgroup's reads of
-// the tokens from L2, and at least a memory latency for each batch of 8 slices that a wave walks through.  Measured (us): 1 x 4096 x
-// 4096 5.5, 16 x 4096 x 4096 6.5, 1 x 16384 x 4096 13.8, 16 x 4096 x 16384 17.2; the best tile takes 8.0, 8.2, 18.5 and 12.6.
-float few_us(const LinearParams &p) {
+// the tokens from L2, and at least a memory latency for each batch of 8 slices that a wave walks through; rows at odd addresses cost
+// 3.5 and 1.5 times that.  Measured (us), and the best tile: 1 x 4096 x 4096 5.5 | 8.0, 16 x 4096 x 4096 6.5 | 8.2, 1 x 16384 x 4096
+// 13.8 | 18.5, 65 x 6144 x 432 7.8 | 9.5, 163 x 528 x 449 3.7 | 5.2, but 16 x 4096 x 16384 17.2 | 12.6 and 130 x 9712 x 1198 28.4 | 13.8; at odd
+// addresses, and linear_any_kernel: 9 x 10123 x 2476 15 | 29, 189 x 13017 x 275 21 | 43, but 95 x 849 x 2742 12.9 | 7.0.
+float few_us(const LinearParams &p, bool odd) {
   const float bytes = (float)p.N * (float)p.K, blocks = (float)((p.M + LINEAR_FEW - 1) / LINEAR_FEW);
   const float traffic = bytes / 5.9e6f + bytes * (blocks - 1.0f) / 12e6f + bytes * (float)p.M / 16.0f / 20e6f;
-  const float batches = 0.9f * (float)((p.K + 4095) / 4096);
-  return 2.5f + (traffic > batches ? traffic : batches);
+  const float batches = 0.9f * (float)((p.K + 4095) / 4096), t = odd ? 3.5f * traffic : traffic, l = odd ? 1.5f * batches : batches;
+  return 2.5f + (t > l ? t : l);
+}
+
+// The same of linear_any_kernel: rounds of two workgroups to a CU, a step of the small or the large tile.
+float any_us(const LinearParams &p) {
+  const float large = (float)((p.M + 127) / 128) * (float)((p.N + 127) / 128), steps = (float)((p.K + ANY_K - 1) / ANY_K);
+  if (large >= 256.0f) return 4.0f + ceilf(large / 512.0f) * steps * 1.3f;
+  return 4.0f + ceilf((float)((p.M + 63) / 64) * (float)((p.N + 63) / 64) / 512.0f) * steps * 0.4f;
 }
 
 // Whether linear_few_kernel also quantises the tokens.  A launch less is 2.3 us; every workgroup repeating the work costs about half of
@@ -136,7 +147,7 @@ f8_status enqueue_linear(const LinearParams &p, int y_type, hipStream_t s) {
   // tiles: rows on 4 bytes, and within reach of 31-bit offsets inside a tile
   const bool tiles = aligned_to(p.x, 4) && aligned_to(p.w, 4) && p.ldx % 4 == 0 && p.ldw % 4 == 0 && p.ldx < (1 << 22) && p.ldw < (1 << 22);
   const LinearPlan plan = linear_plan(p.M, p.N, p.K);
-  if (tiles ? p.M <= LINEAR_FEW_MOST && few_us(p) < plan.us : p.M <= LINEAR_FEW) return launch_linear_few(p, F8_S8, y_type, s);
+  if (p.M <= LINEAR_FEW_MOST && few_us(p, !tiles) < (tiles ? plan.us : any_us(p))) return launch_linear_few(p, F8_S8, y_type, s);
   if (tiles) {
     LinearParams part = p;
     part.M = plan.M1, part.N = plan.N1;
