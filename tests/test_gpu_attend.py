@@ -124,6 +124,24 @@ def test_long_contexts_are_split_and_joined(kind, dtype):
         check(c2, q2, out2, 128 ** -0.5)
 
 
+@pytest.mark.parametrize("B,heads,group,kind", [(257, 1, 2, "s8"), (700, 2, 1, "bf16"), (1100, 1, 17, "s8")])
+def test_many_requests(B, heads, group, kind):
+    # more requests than are looked through at a time, stretches of empty ones among them, some far longer than the others
+    g = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, 90, (B,), generator=g)
+    lens[torch.rand(B, generator=g) < 0.3] = 0
+    lens[B // 3:B // 3 + 100] = 0
+    for i, n in ((0, 700), (B // 2, 1500), (B - 1, 640), (B - 2, 0)):
+        lens[i] = n
+    c = Cache(B, lens.tolist(), heads, 32, 16, kind)
+    dtype = torch.bfloat16 if kind == "bf16" else torch.float16
+    q, out = run(c, B, heads * group, 32, dtype)
+    check(c, q, out, 32 ** -0.5)
+    c.lens = [0] * B                                             # nobody has a token
+    out = f8.f8_attend_paged(q.to(DEV), table=c.table.to(DEV), lens=torch.zeros(B, dtype=torch.int32, device=DEV), **c.args())
+    assert (out == 0).all()
+
+
 def test_scores_far_apart_and_scales_far_apart():
     c = Cache(3, [700, 40], 2, 64, 16, "s8")
     q, out = run(c, 2, 4, 64, torch.float16, scale=4.0)           # one token takes all the weight
