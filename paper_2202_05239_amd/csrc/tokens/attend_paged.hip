@@ -142,9 +142,10 @@ struct TileRows {
   float scale[3 * TILE];
 };
 
-// (two waves to a SIMD: the second workgroup of a CU works while the first one looks up its pair or joins its waves)
+// (two waves to a SIMD where the registers allow it: the second workgroup of a CU works while the first one looks up its pair or joins its
+// waves.  128 dimensions of 16 bits held to that spill 14 words a lane, and their reloads wait for the tile ahead: 57.7 us against 51.1)
 template <typename C, typename Q, int DP>
-__global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void attend_kernel(AttendParams p) {
+__global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void attend_kernel(AttendParams p) {
   typedef Operand<C> Op;
   typedef typename Op::t H;
   constexpr bool S8 = sizeof(C) == 1;
@@ -566,12 +567,13 @@ f8_status launch(const AttendParams &p, hipStream_t s) {
 }
 
 // Workgroups among which the units are dealt out, or 0: a workgroup to each pair and no second launch, up to 4 units (300 tokens,
-// 32 pairs: 5.7 us against 7.1).  Otherwise as many as are resident at once, two to a CU, one with more than 128 dimensions: a
-// workgroup's way to its first rows is 5 us that only its neighbour hides (131072 tokens, 8 pairs: 67 us with 512, 72 with 1024, 81
-// with 256; dim 256, 16 pairs of up to 16384 tokens: 39 us with 256, 45 with 512), and at most 256 to a pair, whose pieces the
-// second launch adds up (one pair of 131072 tokens: 26 us with 256, 33 with 512).
-int wgs_of(int64_t pairs, int dim, int max_len) {
-  const int64_t units = (max_len + UNIT - 1) / UNIT, most = dim > 128 || pairs == 1 ? 256 : 512;
+// 32 pairs: 5.7 us against 7.1).  Otherwise as many as are resident at once, two to a CU, or one where a row is more than 128 bytes
+// (of the kernel's 64, 128 or 256 dimensions): a workgroup's way to its first rows is 5 us that only its neighbour hides (131072 tokens,
+// 8 pairs: 67 us with 512, 72 with 1024, 81 with 256; 256 dimensions, 16 pairs of up to 16384 tokens: 39 us with 256, 45 with 512), and
+// at most 256 to a pair, whose pieces the second launch adds up (one pair of 131072 tokens: 26 us with 256, 33 with 512).
+int wgs_of(int64_t pairs, int dim, int bytes, int max_len) {
+  const int row = (dim <= 64 ? 64 : dim <= 128 ? 128 : 256) * bytes;
+  const int64_t units = (max_len + UNIT - 1) / UNIT, most = row > 128 || pairs == 1 ? 256 : 512;
   if (units <= 4) return 0;
   return (int)(pairs * units < most ? pairs * units : most);
 }
@@ -583,9 +585,10 @@ using namespace f8;
 
 extern "C" {
 
+// (for any type of cache: a 16-bit one may use less)
 size_t f8_attend_workspace_bytes(int batch, int q_heads, int kv_heads, int dim, int max_len) {
   if (batch < 1 || q_heads < 1 || kv_heads < 1 || dim < 1 || max_len < 1 || q_heads % kv_heads != 0) return 0;
-  const int group = q_heads / kv_heads, wgs = wgs_of((int64_t)batch * kv_heads * ((group + HEADS - 1) / HEADS), dim, max_len);
+  const int group = q_heads / kv_heads, wgs = wgs_of((int64_t)batch * kv_heads * ((group + HEADS - 1) / HEADS), dim, 1, max_len);
   return (size_t)2 * wgs * (group < HEADS ? group : HEADS) * (dim + 2) * sizeof(float);
 }
 
@@ -609,7 +612,7 @@ f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cach
   const int group = d->q_heads / c->heads, chunks = (group + HEADS - 1) / HEADS, row = group < HEADS ? group : HEADS;
   const int64_t pairs = (int64_t)d->batch * c->heads * chunks;
   if (pairs > 1 << 22) return F8_ERR_UNSUPPORTED;          // (workgroups of a launch)
-  const int wgs = wgs_of(pairs, c->dim, d->max_len);
+  const int wgs = wgs_of(pairs, c->dim, (int)bytes_of(c->type), d->max_len);
   if (wgs) {
     if (!workspace) return F8_ERR_NULL;
     if (!aligned_to(workspace, 16)) return F8_ERR_ALIGN;
