@@ -2,8 +2,8 @@
 //
 //   s_t = scale * q . k_t,   p = softmax of s over the tokens of the request,   o = sum_t p_t v_t   (0 without tokens),
 //
-// query head h reads cache head h / G.  A workgroup's unit of work is 128 tokens of a request, a cache head and up to 16 of the
-// query heads that share it; the units of all requests are dealt out evenly (see Runs), and a second launch joins the pairs that came
+// query head h reads cache head h / G.  A workgroup's unit of work is 128 tokens of a request (or 64, of two heads), a cache head and
+// up to 16 of the query heads that share it; the units of all requests are dealt out evenly (see Runs), and a second launch joins the pairs that came
 // apart.
 //
 // Inside, a wave walks over tiles of 32 tokens on its own and keeps the running maximum, sum and output of its heads.  Both
@@ -20,7 +20,7 @@
 // below the rounding of the 16-bit result.  Scores, maxima, sums and outputs are 32 bits.
 //
 // Bound by HBM: every cached byte is read once, in whole rows, one tile ahead per wave (131072 tokens of 8 heads, 277 MB: 67 us with
-// the second launch, 4.2 TB/s; 64 requests of up to 8192 tokens, 491 MB: 117 us, 4.2 TB/s; a large copy reaches 5.5).  The vector units
+// the second launch, 4.2 TB/s; 64 requests of up to 8192 tokens, 491 MB: 113 us, 4.35 TB/s; a large copy reaches 5.5).  The vector units
 // are a third busy (350 instructions a tile, most of them codes into f16).  Without the tile ahead the two took 97 and 239 us; with
 // the requests' lengths cut into equal stretches, a workgroup each, instead of units dealt out evenly, 68 and 167.
 #include <math.h>
@@ -47,20 +47,21 @@ struct AttendParams {
   void *out;
   float *part_o, *part_ml;                 // [2 wgs][rows][dim] and [2 wgs][rows][2], rows = min(group, HEADS)
   int64_t qt, qh, ot, oh, page, token, head, spage, stoken, shead, table_ld;
-  int batch, kv_heads, group, chunks, dim, pages, max_len;
+  int batch, hp, kv_groups, group, chunks, dim, pages, max_len;   // kv_groups: of hp heads of the cache
+  int unit_shift;                          // log2 of the tokens of a unit
   int wgs;                                 // 0: a workgroup to each pair
   FastDiv page_size;
   float scale;                             // of the scores, times log2 e
 };
 
-// How the work is dealt out.  A pair is a request and a cache head with up to 16 of its query heads; its units are rounds of a
-// workgroup's four waves over the request's tokens.  All pairs' units lie in a row, request by request, and each workgroup takes
+// How the work is dealt out.  A pair is a request and a cache head (or HP of them) with up to 16 of its query heads; its units are
+// rounds of a workgroup's four waves over the request's tokens.  All pairs' units lie in a row, request by request, and each workgroup takes
 // an equal run of them, whatever the lengths are: a pair that a run does not hold whole is left in pieces for join_kernel, at most
 // two to a workgroup (slot 0 its first pair, slot 1 its last).  The lengths are only known on the device, so every workgroup adds
 // them up itself.
 constexpr int UNIT = WAVES * TILE;
 __device__ __forceinline__ int len_of(const AttendParams &p, int b) { return min(max(p.lens[b], 0), p.max_len); }
-__device__ __forceinline__ int units_of(const AttendParams &p, int b) { return (len_of(p, b) + UNIT - 1) / UNIT; }
+__device__ __forceinline__ int units_of(const AttendParams &p, int b) { return (len_of(p, b) + (1 << p.unit_shift) - 1) >> p.unit_shift; }
 struct Runs {                                // equal runs of `total` units, the first `more` of them one longer
   int64_t per, more;
   __device__ __forceinline__ Runs(int64_t total, int wgs) : per(total / (uint32_t)wgs), more(total - per * wgs) {}
@@ -144,7 +145,7 @@ struct TileRows {
 
 // (two waves to a SIMD where the registers allow it: the second workgroup of a CU works while the first one looks up its pair or joins its
 // waves.  128 dimensions of 16 bits held to that spill 14 words a lane, and their reloads wait for the tile ahead: 57.7 us against 51.1)
-template <typename C, typename Q, int DP>
+template <typename C, typename Q, int DP, int HP>
 __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void attend_kernel(AttendParams p) {
   typedef Operand<C> Op;
   typedef typename Op::t H;
@@ -152,15 +153,16 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
   constexpr int E = DP / 16, VB = E * (int)sizeof(C);     // elements and bytes of a value row per lane
   constexpr int KL = DP * (int)sizeof(C) / 64;            // 16-byte loads of a key row per lane
   constexpr int KS = DP / 32;                             // products per block of 16 scores
+  constexpr int SHARE = WAVES / HP;                       // waves of a head
   __shared__ TileRows rows[WAVES][2];
   __shared__ float part[WAVES][HEADS][DP + 1], ml[WAVES][HEADS][2];
   __shared__ int64_t scan[WAVES][2], before;
   __shared__ int from;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
-  const int per_b = p.kv_heads * p.chunks, group_rows = min(p.group, HEADS);
-  // Runs that follow one another lie on one XCD, so that the heads of a request, whose scales share lines, share an L2 (64 requests of up
-  // to 8192 tokens, 491 MB: 592 MB fetched otherwise and 122 us, 563 and 117 with it).  With few requests a head is many runs, and those of the same tokens meet on
-  // an XCD by themselves.
+  const int per_b = p.kv_groups * p.chunks, group_rows = min(p.group, HEADS), mine = wave % HP;
+  // Runs that follow one another lie on one XCD, so that the heads of a request, whose scales share lines, share an L2 (64 requests of
+  // up to 8192 tokens, 491 MB, one head at a time: 592 MB fetched otherwise and 122 us, 563 and 117 with it).  With few requests a head
+  // is many runs, and those of the same tokens meet on an XCD by themselves.
   const uint32_t run = p.batch >= 8 ? xcd_remap(blockIdx.x, gridDim.x) : blockIdx.x;
   int b, hc, unit, units, slot = 0;
   int64_t left;                               // units of this workgroup's run
@@ -213,8 +215,8 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
   b = __builtin_amdgcn_readfirstlane(b), hc = __builtin_amdgcn_readfirstlane(hc);
   unit = __builtin_amdgcn_readfirstlane(unit), units = __builtin_amdgcn_readfirstlane(units), left = uniform64(left);
   for (bool more = true; more;) {
-    const int kvh = hc / p.chunks, qc = hc % p.chunks, len = len_of(p, b);
-    const int last = (int)min((int64_t)units, unit + left), first = unit * UNIT, end = min(len, last * UNIT);
+    const int kv0 = hc / p.chunks * HP, kvh = kv0 + mine, qc = hc % p.chunks, len = len_of(p, b);
+    const int last = (int)min((int64_t)units, unit + left), first = unit * (UNIT / HP), end = min(len, last * (UNIT / HP));
     const int heads = min(HEADS, p.group - qc * HEADS), hq0 = kvh * p.group + qc * HEADS;
     const int32_t *table = p.table + b * p.table_ld;
 
@@ -406,8 +408,8 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
       }
     };
 
-    constexpr int NEXT = WAVES * TILE;
-    int t0 = first + wave * TILE;
+    constexpr int NEXT = SHARE * TILE;
+    int t0 = first + wave / HP * TILE;
     if (t0 < end) {
       Tile x, y;
       fetch(t0, look_up(t0), rows[wave][0].at, x);
@@ -428,34 +430,34 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
 
-    // the four waves join in LDS
+    // the waves of a head join in LDS
     if (g == 0) ml[wave][c16][0] = m, ml[wave][c16][1] = l;
     __syncthreads();
-    float top = ml[0][c16][0];
+    float top = ml[mine][c16][0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ml[w][c16][0]);
+    for (int w = 1; w < SHARE; ++w) top = fmaxf(top, ml[mine + w * HP][c16][0]);
     const float shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.0f : top));
 #pragma unroll
     for (int n = 0; n < E; ++n)
 #pragma unroll
       for (int j = 0; j < 4; ++j) part[wave][c16][(4 * g + j) * E + n] = o[n][j] * shrink;
     __syncthreads();
-    for (int i = threadIdx.x; i < heads * DP; i += 64 * WAVES) {
-      const int h = i / DP, d = i % DP;
-      float mh = ml[0][h][0], sum = 0.0f, of = 0.0f;
+    for (int i = threadIdx.x; i < HP * heads * DP; i += 64 * WAVES) {
+      const int row = i / DP, d = i % DP, k = row / heads, h = row - k * heads;      // cache head kv0 + k, its query head h
+      float mh = ml[k][h][0], sum = 0.0f, of = 0.0f;
 #pragma unroll
-      for (int w = 1; w < WAVES; ++w) mh = fmaxf(mh, ml[w][h][0]);
+      for (int w = 1; w < SHARE; ++w) mh = fmaxf(mh, ml[k + w * HP][h][0]);
       const float base = mh == -INFINITY ? 0.0f : mh;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        sum += ml[w][h][1] * __builtin_amdgcn_exp2f(ml[w][h][0] - base);
-        of += part[w][h][d];
+      for (int w = 0; w < SHARE; ++w) {
+        sum += ml[k + w * HP][h][1] * __builtin_amdgcn_exp2f(ml[k + w * HP][h][0] - base);
+        of += part[k + w * HP][h][d];
       }
       if (d >= p.dim) continue;
       if (unit == 0 && last == units) {
-        static_cast<Q *>(p.out)[b * p.ot + (hq0 + h) * p.oh + d] = (Q)(sum == 0.0f ? 0.0f : of / sum);
+        static_cast<Q *>(p.out)[b * p.ot + ((kv0 + k) * p.group + qc * HEADS + h) * p.oh + d] = (Q)(sum == 0.0f ? 0.0f : of / sum);
       } else {
-        const int64_t at = (2 * (int64_t)run + slot) * group_rows + h;
+        const int64_t at = ((2 * (int64_t)run + slot) * HP + k) * group_rows + h;
         p.part_o[at * p.dim + d] = of;
         if (d == 0) p.part_ml[2 * at] = mh, p.part_ml[2 * at + 1] = sum;
       }
@@ -483,16 +485,16 @@ __global__ __launch_bounds__(64 * JOINERS) void join_kernel(AttendParams p) {
   __shared__ v4f part[JOIN_AT_ONCE][JOIN_VECS];
   __shared__ float sums[JOIN_AT_ONCE][JOIN_VECS];
   __shared__ int64_t scan[JOINERS][2];
-  const int per_b = p.kv_heads * p.chunks, b = blockIdx.x / per_b, hc = blockIdx.x % per_b, kvh = hc / p.chunks, qc = hc % p.chunks;
-  const int heads = min(HEADS, p.group - qc * HEADS), hq0 = kvh * p.group + qc * HEADS, rows = min(p.group, HEADS), units = units_of(p, b);
+  const int per_b = p.kv_groups * p.chunks, b = blockIdx.x / per_b, hc = blockIdx.x % per_b, kv0 = hc / p.chunks * p.hp, qc = hc % p.chunks;
+  const int heads = min(HEADS, p.group - qc * HEADS), group_rows = min(p.group, HEADS), rows = p.hp * group_rows, units = units_of(p, b);
   const int vec = (int)threadIdx.x % JOIN_VECS, mine = (int)threadIdx.x / JOIN_VECS;
   // (dim is a multiple of 16: four neighbours belong to one head)
-  const int e = blockIdx.y * JOIN_PART + vec * 4, h = e / p.dim, d = e - h * p.dim;
-  const bool real = h < heads;
-  Q *out = static_cast<Q *>(p.out) + b * p.ot + (hq0 + h) * p.oh + d;
+  const int e = blockIdx.y * JOIN_PART + vec * 4, row = e / p.dim, d = e - row * p.dim, k = row / group_rows, h = row - k * group_rows;
+  const bool real = k < p.hp && h < heads;
+  Q *out = static_cast<Q *>(p.out) + b * p.ot + ((kv0 + k) * p.group + qc * HEADS + h) * p.oh + d;
   if (units == 0) {
     if (mine == 0 && real)
-      for (int k = 0; k < 4; ++k) out[k] = (Q)0.0f;
+      for (int j = 0; j < 4; ++j) out[j] = (Q)0.0f;
     return;
   }
   int64_t all[2] = {0, 0};                    // units of all requests, and of those in front of this one
@@ -508,7 +510,7 @@ __global__ __launch_bounds__(64 * JOINERS) void join_kernel(AttendParams p) {
   // piece i lies in slot 0 of workgroup i, but the pair may begin behind others in the first one (runs in between are not empty:
   // with fewer units than workgroups the first ones have one each)
   const int64_t row0 = (2 * i0 + (runs.start(i0) < at ? 1 : 0)) * rows, step = 2 * rows;
-  const int n = (int)(i1 - i0) + 1, hr = real ? h : 0;
+  const int n = (int)(i1 - i0) + 1, hr = real ? row : 0;
   const float2 *ml = reinterpret_cast<const float2 *>(p.part_ml) + hr;
   const float *po = p.part_o + hr * p.dim + (real ? d : 0);
   auto row_of = [&](int i) { return i == 0 ? row0 : (2 * i0) * rows + i * step; };
@@ -555,27 +557,51 @@ __global__ __launch_bounds__(64 * JOINERS) void join_kernel(AttendParams p) {
 
 template <typename C, typename Q>
 f8_status launch(const AttendParams &p, hipStream_t s) {
-  const dim3 grid(p.wgs ? p.wgs : p.batch * p.kv_heads * p.chunks), block(64 * WAVES);
-  if (p.dim <= 64) hipLaunchKernelGGL((attend_kernel<C, Q, 64>), grid, block, 0, s, p);
-  else if (p.dim <= 128) hipLaunchKernelGGL((attend_kernel<C, Q, 128>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((attend_kernel<C, Q, 256>), grid, block, 0, s, p);
+  const int pairs = p.batch * p.kv_groups * p.chunks;
+  const dim3 grid(p.wgs ? p.wgs : pairs);
+  const dim3 block(64 * WAVES);
+  if (sizeof(C) == 1 && p.hp == 2) {
+    if (p.dim <= 64) hipLaunchKernelGGL((attend_kernel<int8_t, Q, 64, 2>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((attend_kernel<int8_t, Q, 128, 2>), grid, block, 0, s, p);
+  } else if (p.dim <= 64) {
+    hipLaunchKernelGGL((attend_kernel<C, Q, 64, 1>), grid, block, 0, s, p);
+  } else if (p.dim <= 128) {
+    hipLaunchKernelGGL((attend_kernel<C, Q, 128, 1>), grid, block, 0, s, p);
+  } else {
+    hipLaunchKernelGGL((attend_kernel<C, Q, 256, 1>), grid, block, 0, s, p);
+  }
   f8_status st = launch_status();
   if (st != F8_OK || p.wgs == 0) return st;
-  const int elements = (p.group < HEADS ? p.group : HEADS) * p.dim;
-  hipLaunchKernelGGL(join_kernel<Q>, dim3(p.batch * p.kv_heads * p.chunks, (elements + JOIN_PART - 1) / JOIN_PART), dim3(64 * JOINERS), 0, s, p);
+  const int elements = p.hp * (p.group < HEADS ? p.group : HEADS) * p.dim;
+  hipLaunchKernelGGL(join_kernel<Q>, dim3(pairs, (elements + JOIN_PART - 1) / JOIN_PART), dim3(64 * JOINERS), 0, s, p);
   return launch_status();
 }
 
-// Workgroups among which the units are dealt out, or 0: a workgroup to each pair and no second launch, up to 4 units (300 tokens,
-// 32 pairs: 5.7 us against 7.1).  Otherwise as many as are resident at once, two to a CU, or one where a row is more than 128 bytes
-// (of the kernel's 64, 128 or 256 dimensions): a workgroup's way to its first rows is 5 us that only its neighbour hides (131072 tokens,
-// 8 pairs: 67 us with 512, 72 with 1024, 81 with 256; 256 dimensions, 16 pairs of up to 16384 tokens: 39 us with 256, 45 with 512), and
+// How a call's work is dealt out.
+// wgs: workgroups among which the units are, or 0: a workgroup to each pair and no second launch, up to 4 units (300 tokens, 32 pairs:
+// 5.7 us against 7.1).  Otherwise as many as are resident at once, two to a CU, or one where a row is more than 128 bytes (of the
+// kernel's 64, 128 or 256 dimensions): a workgroup's way to its first rows is 5 us that only its neighbour hides (131072 tokens, 8
+// pairs: 67 us with 512, 72 with 1024, 81 with 256; 256 dimensions, 16 pairs of up to 16384 tokens: 39 us with 256, 45 with 512), and
 // at most 256 to a pair, whose pieces the second launch adds up (one pair of 131072 tokens: 26 us with 256, 33 with 512).
-int wgs_of(int64_t pairs, int dim, int bytes, int max_len) {
-  const int row = (dim <= 64 ? 64 : dim <= 128 ? 128 : 256) * bytes;
-  const int64_t units = (max_len + UNIT - 1) / UNIT, most = row > 128 || pairs == 1 ? 256 : 512;
-  if (units <= 4) return 0;
-  return (int)(pairs * units < most ? pairs * units : most);
+// hp: heads of the cache that a workgroup reads side by side, half of the waves each.  Two, where rows of 8 bits are at most 128 bytes
+// and there are many requests: their rows are neighbours in a token's memory, and so are their scales (us with one | two: 16 requests of
+// 8192 tokens 73 | 66, 64 of up to 8192 117 | 113, 64 of up to 4096 with 64 dimensions 53 | 48, but 8 of up to 4096 23 | 25 and 2 of up to
+// 65536 30 | 33; 16 of up to 8192 in 16 bits 52 | 53).
+struct Deal {
+  int hp, wgs;
+  size_t rows;                             // of the pieces that the workgroups may leave
+};
+Deal deal_of(int64_t batch, int kv_heads, int group, int dim, int bytes, int max_len) {
+  const int row = (dim <= 64 ? 64 : dim <= 128 ? 128 : 256) * bytes, chunks = (group + HEADS - 1) / HEADS;
+  Deal d{1, 0, 0};
+  if (max_len <= 4 * UNIT) return d;
+  const int64_t rounds = batch * kv_heads * chunks * (((int64_t)max_len + UNIT - 1) / UNIT);
+  if (bytes == 1 && row <= 128 && kv_heads % 2 == 0 && batch >= 16 && rounds >= 2048) d.hp = 2;
+  const int64_t pairs = batch * (kv_heads / d.hp) * chunks, units = ((int64_t)max_len + UNIT / d.hp - 1) / (UNIT / d.hp);
+  const int64_t most = row > 128 || pairs == 1 ? 256 : 512;
+  d.wgs = (int)(pairs * units < most ? pairs * units : most);
+  d.rows = (size_t)2 * d.wgs * d.hp * (group < HEADS ? group : HEADS);
+  return d;
 }
 
 }  // namespace
@@ -585,11 +611,11 @@ using namespace f8;
 
 extern "C" {
 
-// (for any type of cache: a 16-bit one may use less)
+// (for any type of cache)
 size_t f8_attend_workspace_bytes(int batch, int q_heads, int kv_heads, int dim, int max_len) {
   if (batch < 1 || q_heads < 1 || kv_heads < 1 || dim < 1 || max_len < 1 || q_heads % kv_heads != 0) return 0;
-  const int group = q_heads / kv_heads, wgs = wgs_of((int64_t)batch * kv_heads * ((group + HEADS - 1) / HEADS), dim, 1, max_len);
-  return (size_t)2 * wgs * (group < HEADS ? group : HEADS) * (dim + 2) * sizeof(float);
+  const size_t a = deal_of(batch, kv_heads, q_heads / kv_heads, dim, 1, max_len).rows, b = deal_of(batch, kv_heads, q_heads / kv_heads, dim, 2, max_len).rows;
+  return (a > b ? a : b) * (dim + 2) * sizeof(float);
 }
 
 f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cache, const float *k_scale, const float *v_scale,
@@ -609,20 +635,19 @@ f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cach
   if (!aligned_to(q, 2) || !aligned_to(out, 2) || !aligned_to(table, 4) || !aligned_to(lens, 4) || !aligned_to(k_scale, 4) || !aligned_to(v_scale, 4) ||
       !aligned_to(k_cache, 16) || !aligned_to(v_cache, 16) || c->page_stride * e % 16 || c->token_stride * e % 16 || c->head_stride * e % 16)
     return F8_ERR_ALIGN;
-  const int group = d->q_heads / c->heads, chunks = (group + HEADS - 1) / HEADS, row = group < HEADS ? group : HEADS;
-  const int64_t pairs = (int64_t)d->batch * c->heads * chunks;
-  if (pairs > 1 << 22) return F8_ERR_UNSUPPORTED;          // (workgroups of a launch)
-  const int wgs = wgs_of(pairs, c->dim, (int)bytes_of(c->type), d->max_len);
-  if (wgs) {
+  const int group = d->q_heads / c->heads, chunks = (group + HEADS - 1) / HEADS;
+  if ((int64_t)d->batch * c->heads * chunks > 1 << 22) return F8_ERR_UNSUPPORTED;          // (workgroups of a launch)
+  const Deal deal = deal_of(d->batch, c->heads, group, c->dim, (int)bytes_of(c->type), d->max_len);
+  if (deal.wgs) {
     if (!workspace) return F8_ERR_NULL;
     if (!aligned_to(workspace, 16)) return F8_ERR_ALIGN;
     if (workspace_bytes < f8_attend_workspace_bytes(d->batch, d->q_heads, c->heads, c->dim, d->max_len)) return F8_ERR_SHAPE;
   }
   float *ws = static_cast<float *>(workspace);
-  const AttendParams p{q, k_cache, v_cache, k_scale, v_scale, table, lens, out, ws, wgs ? ws + (size_t)2 * wgs * row * c->dim : nullptr,
+  const AttendParams p{q, k_cache, v_cache, k_scale, v_scale, table, lens, out, ws, deal.wgs ? ws + deal.rows * c->dim : nullptr,
                        d->q_token, d->q_head, d->o_token, d->o_head, c->page_stride, c->token_stride, c->head_stride,
-                       c->scale_page, c->scale_token, c->scale_head, d->table_ld, d->batch, c->heads, group, chunks, c->dim, c->pages, d->max_len,
-                       wgs, FastDiv((uint32_t)c->page_size), d->scale * LOG2E};
+                       c->scale_page, c->scale_token, c->scale_head, d->table_ld, d->batch, deal.hp, c->heads / deal.hp, group, chunks, c->dim, c->pages, d->max_len,
+                       deal.hp == 1 ? 7 : 6, deal.wgs, FastDiv((uint32_t)c->page_size), d->scale * LOG2E};
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (codes) return d->type == F8_F16 ? launch<int8_t, f16>(p, hs) : launch<int8_t, bf16>(p, hs);
   return d->type == F8_F16 ? launch<f16, f16>(p, hs) : launch<bf16, bf16>(p, hs);

@@ -142,6 +142,16 @@ def test_many_requests(B, heads, group, kind):
     assert (out == 0).all()
 
 
+@pytest.mark.parametrize("heads,group,D,dtype", [(2, 3, 64, torch.float16), (4, 16, 80, torch.bfloat16), (2, 17, 128, torch.bfloat16), (6, 1, 16, torch.float16)])
+def test_two_heads_side_by_side(heads, group, D, dtype):
+    # enough requests and tokens that a workgroup takes two heads of an 8-bit cache at a time, in either order of the cache
+    lens = [4500, 0, 1, 63, 64, 65, 128, 129, 700, 31, 2, 1000, 96, 0, 33, 640, 5, 3200]
+    for first in (False, True):
+        c = Cache(heads + D, lens, heads, D, 24, "s8", heads_first=first, wide=200)
+        q, out = run(c, len(lens), heads * group, D, dtype)
+        check(c, q, out, D ** -0.5)
+
+
 def test_scores_far_apart_and_scales_far_apart():
     c = Cache(3, [700, 40], 2, 64, 16, "s8")
     q, out = run(c, 2, 4, 64, torch.float16, scale=4.0)           # one token takes all the weight
