@@ -71,6 +71,14 @@ def test_codes_of_plain_rows_are_exact(dtype):
             assert torch.equal(values.cpu(), (want * s).to(dtype)), (cols, pad)
 
 
+@pytest.mark.parametrize("cols", [4097, 4100, 6143, 6144, 6145])
+def test_many_rows_of_middling_width(cols):
+    x = torch.randn(600, cols, generator=gen(cols)).half()
+    codes, scale = f8.f8_quant_tokens(x.to(DEV))
+    want, s = quant_ref(x.float())
+    assert torch.equal(codes.cpu().float(), want) and torch.equal(scale.cpu(), s[:, 0])
+
+
 def test_ties_and_extreme_scales():
     ties = torch.cat([torch.tensor([127.0]), torch.arange(-126, 126) + 0.5])
     rows = torch.stack([ties * f for f in (1.0, 0.37, 2.0 ** -100, 2.0 ** 100, 1e-3)])
