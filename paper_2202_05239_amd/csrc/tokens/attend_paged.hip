@@ -630,7 +630,7 @@ f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cach
   if (d->table_ld < d->table_cols || isnan(d->scale)) return F8_ERR_SHAPE;
   if (d->batch == 0) return F8_OK;
   const bool codes = c->type == F8_S8;
-  if (!q || !k_cache || !v_cache || !table || !lens || !out || (codes && (!k_scale || !v_scale))) return F8_ERR_NULL;
+  if (!q || !k_cache || !v_cache || (!table && d->max_len > 0) || !lens || !out || (codes && (!k_scale || !v_scale))) return F8_ERR_NULL;
   const size_t e = bytes_of(c->type);
   if (!aligned_to(q, 2) || !aligned_to(out, 2) || !aligned_to(table, 4) || !aligned_to(lens, 4) || !aligned_to(k_scale, 4) || !aligned_to(v_scale, 4) ||
       !aligned_to(k_cache, 16) || !aligned_to(v_cache, 16) || c->page_stride * e % 16 || c->token_stride * e % 16 || c->head_stride * e % 16)

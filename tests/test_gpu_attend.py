@@ -212,6 +212,16 @@ def test_lens_beyond_the_bound_are_clamped():
     check(c, q, out, 0.125)
 
 
+def test_a_batch_without_pages():
+    c = Cache(12, [20], 2, 64, 16, "s8")
+    out = f8.f8_attend_paged(torch.randn(3, 4, 64).half().to(DEV), table=torch.zeros(3, 0, dtype=torch.int32, device=DEV),
+                             lens=torch.tensor([0, 5, 0], dtype=torch.int32, device=DEV), **c.args())
+    assert out.shape == (3, 4, 64) and (out == 0).all()
+    none = f8.f8_attend_paged(torch.empty(0, 4, 64, dtype=torch.float16, device=DEV), table=torch.zeros(0, 2, dtype=torch.int32, device=DEV),
+                              lens=torch.zeros(0, dtype=torch.int32, device=DEV), **c.args())
+    assert none.shape == (0, 4, 64)
+
+
 def test_strided_queries_and_results():
     c = Cache(9, [200, 17], 2, 64, 16, "s8")
     big = torch.randn(2, 3, 4, 80, generator=torch.Generator().manual_seed(1)).half().to(DEV)
