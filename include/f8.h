@@ -418,7 +418,7 @@ typedef struct {
 f8_status f8_linear_scaled(const int8_t *x, const float *sx, const int8_t *w, const float *sw, const float *bias, void *y,
                            const f8_linear_desc *d, void *stream);
 /* The same from real tokens x [M][K] (x_type real, K <= 65536), quantised as by f8_quant_tokens.  The workspace holds their codes
- * and scales: f8_linear_workspace_bytes(M, K) bytes. */
+ * and scales: f8_linear_workspace_bytes(M, K) bytes, which may be 0 (few short tokens; then it may be NULL). */
 size_t f8_linear_workspace_bytes(int M, int K);
 f8_status f8_linear_tokens(const void *x, const int8_t *w, const float *sw, const float *bias, void *y, const f8_linear_desc *d,
                            void *workspace, size_t workspace_bytes, void *stream);

@@ -191,7 +191,8 @@ f8_status f8_linear_scaled(const int8_t *x, const float *sx, const int8_t *w, co
 }
 
 size_t f8_linear_workspace_bytes(int M, int K) {
-  return M < 1 || K < 1 ? 0 : (size_t)M * (size_t)code_pitch(K) + (size_t)M * sizeof(float);
+  if (M < 1 || K < 1 || few_quantises(M, INT32_MAX, K)) return 0;
+  return (size_t)M * (size_t)code_pitch(K) + (size_t)M * sizeof(float);
 }
 
 f8_status f8_linear_tokens(const void *x, const int8_t *w, const float *sw, const float *bias, void *y, const f8_linear_desc *d,
@@ -203,9 +204,10 @@ f8_status f8_linear_tokens(const void *x, const int8_t *w, const float *sw, cons
   if (d->M == 0 || d->N == 0) return F8_OK;
   st = check_pointers(x, w, sw, bias, y, d->y_type);
   if (st != F8_OK) return st;
-  if (!workspace) return F8_ERR_NULL;
+  const size_t need = f8_linear_workspace_bytes(d->M, d->K);
+  if (need && !workspace) return F8_ERR_NULL;
   if (!aligned_to(x, bytes_of(d->x_type)) || !aligned_to(workspace, 16)) return F8_ERR_ALIGN;
-  if (workspace_bytes < f8_linear_workspace_bytes(d->M, d->K)) return F8_ERR_SHAPE;
+  if (workspace_bytes < need) return F8_ERR_SHAPE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   LinearParams p{static_cast<const int8_t *>(x), w, nullptr, sw, bias, y, d->ldx, d->ldw, d->ldy, d->M, d->N, d->K};
   if (few_quantises(d->M, d->N, d->K)) return launch_linear_few(p, d->x_type, d->y_type, s);

@@ -305,6 +305,17 @@ def test_products_repeat_and_replay():
         assert torch.equal(y, want)
 
 
+def test_few_short_tokens_need_no_workspace():
+    g = gen(8)
+    for M, K in ((1, 4096), (8, 512), (2, 2048), (3, 1000)):
+        assert f8.lib().f8_linear_workspace_bytes(M, K) == 0
+        x, w, sw = tokens(g, M, K, torch.bfloat16).to(DEV), codes_of(g, 9000, K).to(DEV), torch.rand(9000, generator=g).to(DEV)
+        codes, scale = f8.f8_quant_tokens(x)
+        for n in (100, 9000):
+            y = f8.f8_linear_tokens(x, w[:n], sw[:n], y_dtype=torch.float32)
+            assert torch.equal(y, f8.f8_linear_scaled(codes, scale, w[:n], sw[:n], y_dtype=torch.float32))
+
+
 def test_another_stream():
     g = gen(6)
     x, w, sw = tokens(g, 9, 1024, torch.float16).to(DEV), codes_of(g, 512, 1024).to(DEV), torch.rand(512, generator=g).to(DEV)

@@ -76,9 +76,11 @@ def test_products():
     tokens = lambda d, x=P, ws=P, n=1 << 20: L.f8_linear_tokens(x, P, P, None, P, d, ws, n, None)  # noqa: E731
     real = dict(x_type=f8.F8_BF16)
     assert tokens(l_desc()) == 5 and tokens(l_desc(K=65537, ldx=65537, ldw=65537, **real)) == 2
+    real["M"] = 40
     assert tokens(l_desc(**real), ws=None) == 1 and tokens(l_desc(**real), ws=ODD) == 7 and tokens(l_desc(**real), x=ODD) == 7
-    need = L.f8_linear_workspace_bytes(4, 32)
-    assert need == 4 * 128 + 16 and tokens(l_desc(**real), n=need - 1) == 2
+    need = L.f8_linear_workspace_bytes(40, 32)
+    assert need == 40 * 128 + 160 and tokens(l_desc(**real), n=need - 1) == 2
+    assert L.f8_linear_workspace_bytes(1, 4096) == 0 and L.f8_linear_workspace_bytes(1, 4097) > 0      # the product quantises them itself
     assert L.f8_linear_workspace_bytes(0, 32) == 0
 
 
