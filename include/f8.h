@@ -426,7 +426,7 @@ f8_status f8_linear_tokens(const void *x, const int8_t *w, const float *sw, cons
 /* A cache of keys and values in pages of page_size tokens.  Element (page, place, head, i) lies at page * page_stride + place *
  * token_stride + head * head_stride + i of its array (elements; the strides may order heads and places either way), and in an
  * 8-bit cache its scale at page * scale_page + place * scale_token + head * scale_head.  Keys and values have an array each
- * (and a scale array each, scales not negative) of the same layout.  type F8_S8, F8_F16 or F8_BF16; dim a multiple of 16 up to
+ * (and a scale array each, scales not negative; a row of zeros may have any of them, 0 too) of the same layout.  type F8_S8, F8_F16 or F8_BF16; dim a multiple of 16 up to
  * 256; offsets may pass 32 bits. */
 typedef struct {
   int32_t type;

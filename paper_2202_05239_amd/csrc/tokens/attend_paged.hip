@@ -14,8 +14,10 @@
 // operand of the n-th product is element n of each, which is a byte permutation inside the lane.  Nothing of K or V passes
 // through LDS; what does is where a tile's rows lie (64 bits each: a cache may be larger than 4 GiB) and their scales.
 //
-// Codes are exact in 16-bit floating point.  A key's scale multiplies its score; a value's scale joins the exponent,
-// w_t = exp(s_t + log scale_t - m) with m the maximum of that sum, so that w is in [0, 1] whatever the scales are.  w is rounded
+// Codes are exact in 16-bit floating point.  A key's scale multiplies its score; a value's scale counts in the maximum,
+// m = max(s_t + max(log2 scale_t, SMALL)) (scores as powers of two), so that exp2(s_t - m) scale_t, the weight of a row of codes, is at
+// most 1 whatever the scales are.  The sum of the softmax takes exp2(s_t - m) itself, which a row with a small scale brings up to 2^-SMALL: rows
+// of zeros, whose scale is 2^-126 or 0, are the ones that come.  Weights are rounded
 // to 16 bits for the second product (as P is for 16-bit caches): relative 2^-12 (f16) or 2^-9 (bf16) of each weight, at random,
 // below the rounding of the 16-bit result.  Scores, maxima, sums and outputs are 32 bits.
 //
@@ -39,6 +41,9 @@ typedef long long v2l __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = 4, TILE = 32, HEADS = 16;
 constexpr float LOG2E = 1.4426950408889634f;
+// The least that a value's scale counts for in the maximum, as a power of two: 2^31 tokens of 2^-SMALL each stay below the largest
+// 32-bit number.  Values whose scales all lie below it (1e-24) only lose bits below 2^-94, where their weights leave f16's normal range.
+constexpr float SMALL = -80.0f;
 
 struct AttendParams {
   const void *q, *k, *v;
@@ -137,7 +142,7 @@ __device__ __forceinline__ Raw<BYTES> load_raw(const void *p) {
 }
 
 // What a wave keeps in LDS of a tile: where its 32 rows begin, in elements, and (8-bit caches) the scales of its keys, those of its
-// values and their logarithms.
+// values and their logarithms, SMALL at least.
 struct TileRows {
   int64_t at[TILE];
   float scale[3 * TILE];
@@ -316,7 +321,7 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
       v4f ks[2], vs[2], vl[2];
       if constexpr (S8) {
         scale_lds[lane] = x.scale;
-        if (lane >= 32) scale_lds[32 + lane] = __log2f(x.scale);
+        if (lane >= 32) scale_lds[32 + lane] = fmaxf(__log2f(x.scale), SMALL);
         lanes_meet();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {

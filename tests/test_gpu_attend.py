@@ -308,3 +308,73 @@ def test_repeats_and_replays():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, f8.f8_attend_paged(q, table=table, lens=lens, max_len=5000, **c.args()))
+
+
+def blank_values(c, b, first, last, scale):
+    """Tokens first .. last - 1 of request b have value rows of zeros with the given scale (their keys stay)."""
+    for t in range(first, last):
+        at = (1, c.table[b, t // c.page].long(), t % c.page)
+        c.kv[at], c.scales[at] = 0, scale
+    c.dev[1].copy_(c.kv[1])
+    c.dev_scales[1].copy_(c.scales[1])
+
+
+# a wave's first tile, a tile in the middle, a workgroup's round, several runs of a long context, all but the last token, everything
+BLANK = [(0, 32), (64, 96), (0, 128), (37, 300), (0, 4000), (1024, 3000), (0, -1), (0, None)]
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -126, 0.0])
+@pytest.mark.parametrize("lens,heads,group", [([300, 40], 2, 4), ([513, 1, 129], 1, 1), ([6000, 0, 4097], 2, 8), ([4500, 700] + [300] * 16, 4, 2)])
+def test_stretches_of_zero_values(lens, heads, group, scale):
+    # in one launch, in two, and two heads side by side; scores that are all alike (scale 0) and scores that differ
+    for first, last in BLANK:
+        c = Cache(13 + heads, lens, heads, 64, 16, "s8", wide=200 if len(lens) > 8 else 0)
+        for b, n in enumerate(lens[:3]):
+            end = n if last is None else n + last if last < 0 else min(last, n)
+            blank_values(c, b, min(first, n), max(end, 0), scale)
+        for s in (0.0, 0.125, 1.0):
+            q, out = run(c, len(lens), heads * group, 64, torch.bfloat16, scale=s)
+            assert torch.isfinite(out).all()
+            check(c, q, out, s)
+
+
+def test_values_of_every_size():
+    # scales of values from 2^-80 to 2^100 in one request, each token's weight such that all of them count alike (or, for the second
+    # head, the large ones), and rows of zeros with the largest weights of all
+    n, D = 640, 64
+    c = Cache(14, [n], 1, D, 16, "s8")
+    g = torch.Generator().manual_seed(2)
+    t = torch.arange(n)
+    at = (c.table[0, t // 16].long(), t % 16)
+    size = torch.linspace(-80, 100, n)[torch.randperm(n, generator=g)]
+    none = torch.rand(n, generator=g) < 0.1
+    score = torch.where(none, 200.0, 120 - size)
+    kv, scales = c.kv[:, at[0], at[1], 0], c.scales[:, at[0], at[1], 0]
+    kv[0] = 0
+    kv[0, :, 0] = 127                                             # keys: one element
+    kv[1, none] = 0
+    scales[0] = score / 127
+    scales[1] = torch.where(none, torch.tensor(2.0 ** -126), torch.exp2(size))
+    c.kv[:, at[0], at[1], 0], c.scales[:, at[0], at[1], 0] = kv, scales
+    c.dev.copy_(c.kv)
+    c.dev_scales.copy_(c.scales)
+    q = torch.zeros(1, 2, D)
+    q[0, 0, 0], q[0, 1, 0] = 1, 0.5
+    q = q.bfloat16()
+    out = f8.f8_attend_paged(q.to(DEV), table=c.table.to(DEV), lens=torch.tensor([n], dtype=torch.int32, device=DEV), scale=math.log(2), **c.args()).cpu()
+    k, v = (x[:, 0] for x in c.rows(0))
+    for h in range(2):
+        want = (k @ q[0, h].double() * math.log(2)).softmax(0) @ v
+        assert (out[0, h].double() - want).norm() <= 2.0 ** -7 * want.norm()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_rows_of_an_8_bit_cache_that_are_not_finite(bad):
+    # their scale is not finite: everything of that request is NaN, beside rows of zeros too
+    for n in (40, 3000):
+        c = Cache(17, [n, 33], 1, 64, 16, "s8")
+        blank_values(c, 0, 0, n - 1, 2.0 ** -126)
+        c.dev_scales[1, c.table[0, (n - 1) // 16].item(), (n - 1) % 16] = bad
+        c.dev[1, c.table[0, (n - 1) // 16].item(), (n - 1) % 16] = 0
+        q, out = run(c, 2, 2, 64, torch.bfloat16)
+        assert out[0].isnan().all() and torch.isfinite(out[1]).all()
