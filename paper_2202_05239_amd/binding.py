@@ -470,7 +470,11 @@ def _matrix(t, shape=None):
         raise ValueError("expected a matrix with contiguous rows, got shape %s, strides %s" % (tuple(have), st))
     if shape is not None and have != shape:
         raise ValueError("expected shape %s, got %s" % (tuple(shape), tuple(have)))
-    return st[0] if st[0] >= have[1] else have[1]        # (a single row may report any stride)
+    if st[0] >= have[1]:
+        return st[0]
+    if have[0] > 1:                                      # (expanded or unfolded: the library reads rows that lie apart)
+        raise ValueError("expected rows that do not overlap, got shape %s, strides %s: copy it first" % (tuple(have), st))
+    return have[1]                                       # a single row may report any stride
 
 
 def _vector(t, n, dtype=None):
@@ -651,6 +655,9 @@ def f8_attend_paged(q, k_cache, v_cache, table, lens, k_scale=None, v_scale=None
         os = out.stride()
         if out.shape != shape or out.dtype != q.dtype or os[2] != 1:
             raise ValueError("out has to be like q")
+        (near, n), (far, m) = sorted(((os[0], B), (os[1], H)))
+        if (n > 1 and near < D) or (m > 1 and far < (near * (n - 1) + D if n > 1 else D)):
+            raise ValueError("out overlaps itself: shape %s, strides %s" % (tuple(shape), os))
     if max_len is None:
         max_len = min(cols * c.page_size, 0x7fff0000)
     L = _lib or lib()

@@ -165,3 +165,43 @@ def test_binding_refuses_what_the_library_cannot_see():
         f8.f8_kv_append(torch.zeros(1, 2, 64), torch.zeros(1, 2, 64), torch.zeros(1, dtype=torch.int64), *kv.to(torch.int8))
     with pytest.raises(ValueError):
         f8.f8_attend_paged(torch.zeros(1, 4, 32).half(), kv[0].half(), kv[1].half(), torch.zeros(1, 3, dtype=torch.int32), torch.ones(1, dtype=torch.int32))
+
+
+def overlapping(rows, cols, dtype):
+    """Matrices whose rows share elements: one row for all of them, rows one and four elements apart."""
+    return [torch.zeros(1, cols, dtype=dtype).expand(rows, cols)] + [torch.zeros(cols + rows * s, dtype=dtype).unfold(0, cols, s)[:rows] for s in (1, 4)]
+
+
+def test_binding_refuses_matrices_whose_rows_overlap():
+    # the library takes rows that lie apart: with the width for their distance it would read behind the tensor
+    x, w, s8 = torch.zeros(4, 64), torch.zeros(8, 64, dtype=torch.int8), torch.int8
+    for bad in overlapping(4, 64, torch.float32):
+        for call in (lambda: f8.f8_quant_tokens(bad), lambda: f8.f8_quant_tokens(x, gate=bad), lambda: f8.f8_quant_tokens(x, values=True, out=bad),
+                     lambda: f8.f8_norm_tokens(bad), lambda: f8.f8_norm_tokens(x, res=bad), lambda: f8.f8_norm_tokens(x, gate=bad, gate_rows=1),
+                     lambda: f8.f8_norm_tokens(x, res_out=bad), lambda: f8.f8_norm_tokens(x, out=bad),
+                     lambda: f8.f8_linear_tokens(bad, w, torch.ones(8))):
+            with pytest.raises(ValueError):
+                call()
+    for bad in overlapping(4, 64, s8):
+        with pytest.raises(ValueError):
+            f8.f8_linear_scaled(bad, torch.ones(4), w, torch.ones(8))
+        with pytest.raises(ValueError):
+            f8.f8_linear_scaled(torch.zeros(4, 64, dtype=s8), torch.ones(4), bad, torch.ones(4))
+        with pytest.raises(ValueError):
+            f8.f8_quant_tokens(x, out=bad)
+    for bad in overlapping(4, 8, torch.float32):
+        with pytest.raises(ValueError):
+            f8.f8_linear_tokens(x, w, torch.ones(8), y=bad)
+    kv, q, lens, table = torch.zeros(2, 3, 16, 2, 64).half(), torch.zeros(4, 4, 64).half(), torch.ones(4, dtype=torch.int32), torch.zeros(4, 3, dtype=torch.int32)
+    for bad in overlapping(4, 8, torch.int32):
+        with pytest.raises(ValueError):
+            f8.f8_attend_paged(q, kv[0], kv[1], bad, lens)
+    for bad in (torch.zeros(1, 4, 64).half().expand(4, 4, 64), torch.zeros(4, 1, 64).half().expand(4, 4, 64), torch.zeros(4, 200).half().as_strided((4, 4, 64), (200, 32, 1)),
+                torch.zeros(4, 256).half().as_strided((4, 4, 64), (192, 64, 1))):
+        with pytest.raises(ValueError):
+            f8.f8_attend_paged(q, kv[0], kv[1], table, lens, out=bad)
+
+
+def test_binding_takes_single_rows_of_any_stride():
+    assert f8._matrix(torch.zeros(1, 64).expand(1, 64)) == 64 and f8._matrix(torch.zeros(64, 1).t()) == 64 and f8._matrix(torch.zeros(0, 64)) == 64
+    assert f8._matrix(torch.zeros(4, 80)[:, :64]) == 80 and f8._matrix(torch.zeros(4, 1)) == 1 and f8._matrix(torch.zeros(4, 2)[:, :1]) == 2
