@@ -18,8 +18,9 @@
 // m = max(s_t + max(log2 scale_t, SMALL)) (scores as powers of two), so that exp2(s_t - m) scale_t, the weight of a row of codes, is at
 // most 1 whatever the scales are.  The sum of the softmax takes exp2(s_t - m) itself, which a row with a small scale brings up to 2^-SMALL: rows
 // of zeros, whose scale is 2^-126 or 0, are the ones that come.  Weights are rounded
-// to 16 bits for the second product (as P is for 16-bit caches): relative 2^-12 (f16) or 2^-9 (bf16) of each weight, at random,
-// below the rounding of the 16-bit result.  Scores, maxima, sums and outputs are 32 bits.
+// to 16 bits for the second product (as P is for 16-bit caches): relative 2^-12 (f16) or 2^-9 (bf16) of each weight, at random.  In f16 all
+// weights and sums are 2^15 times what is written here, the largest that f16 holds: the relative error then holds down to 2^-29 of the largest
+// weight, and what lies below is off by 2^-40 of it at most, 2^-23 of it over 131072 tokens.  Scores, maxima, sums and outputs are 32 bits.
 //
 // Bound by HBM: every cached byte is read once, in whole rows, one tile ahead per wave (131072 tokens of 8 heads, 277 MB: 67 us with
 // the second launch, 4.2 TB/s; 64 requests of up to 8192 tokens, 491 MB: 113 us, 4.35 TB/s; a large copy reaches 5.5).  The vector units
@@ -41,8 +42,8 @@ typedef long long v2l __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = 4, TILE = 32, HEADS = 16;
 constexpr float LOG2E = 1.4426950408889634f;
-// The least that a value's scale counts for in the maximum, as a power of two: 2^31 tokens of 2^-SMALL each stay below the largest
-// 32-bit number.  Values whose scales all lie below it (1e-24) only lose bits below 2^-94, where their weights leave f16's normal range.
+// The least that a value's scale counts for in the maximum, as a power of two: 2^31 tokens of 2^(15 - SMALL) each stay below the largest
+// 32-bit number.  Values whose scales all lie below it (1e-24) only lose bits below 2^-109, where their weights leave f16's normal range.
 constexpr float SMALL = -80.0f;
 
 struct AttendParams {
@@ -106,6 +107,7 @@ __device__ __forceinline__ h2 codes_hi(uint32_t u) { return __builtin_bit_cast(h
 template <typename C>
 struct Operand {                            // 16-bit type of the products
   typedef f16 t;
+  static constexpr float UP = 15.0f;        // the largest weight as a power of two
   static __device__ __forceinline__ v4f mfma(v4i a, v4i b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
   }
@@ -113,6 +115,7 @@ struct Operand {                            // 16-bit type of the products
 template <>
 struct Operand<bf16> {
   typedef bf16 t;
+  static constexpr float UP = 0.0f;         // (has the range of 32 bits)
   static __device__ __forceinline__ v4f mfma(v4i a, v4i b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
   }
@@ -387,9 +390,10 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
       }
       typedef H t8 __attribute__((ext_vector_type(8)));
       t8 wh;
+      const float below = base - Op::UP;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float w = __builtin_amdgcn_exp2f(s[j] - base);
+        const float w = __builtin_amdgcn_exp2f(s[j] - below);
         l += w;
         wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : w);
       }

@@ -378,3 +378,41 @@ def test_rows_of_an_8_bit_cache_that_are_not_finite(bad):
         c.dev[1, c.table[0, (n - 1) // 16].item(), (n - 1) % 16] = 0
         q, out = run(c, 2, 2, 64, torch.bfloat16)
         assert out[0].isnan().all() and torch.isfinite(out[1]).all()
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("nats", [6, 10, 14, 17, 20, 24])
+def test_many_small_weights_beside_a_large_one(kind, dtype, nats):
+    """One token with nearly all the weight and a value in dimension 0 only: the other dimensions are the sum of the others' small
+    weights.  Errors: those of check(), but a weight's rounding stays relative down to 2^-29 of the largest weight (its type's
+    normal range, with the largest one brought to 2^15), and what lies below is off by 2^-40 of the largest.  So many requests that a
+    workgroup has one whole request, and a wave of it a quarter of the tokens, the large one among its first; all read the same pages."""
+    n, D, B, one = 2000, 64, 512, 5
+    g = torch.Generator().manual_seed(nats)
+    c = Cache(15, [n], 1, D, 16, kind)
+    t = torch.arange(n)
+    pg, pl = c.table[0, t // 16].long(), t % 16
+    k, v = torch.zeros(n, D), 1 + torch.rand(n, D, generator=g)
+    k[one, 0] = 1
+    v[one] = 0
+    v[one, 0] = 1.5
+    for i, x in enumerate((k, v)):
+        if kind == "s8":
+            s = torch.clamp(x.abs().amax(1) / 127, min=2.0 ** -126)
+            c.scales[i, pg, pl, 0] = s
+            x = torch.round(x / s[:, None])
+        c.kv[i, pg, pl, 0] = x.to(c.kv.dtype)
+    c.dev.copy_(c.kv)
+    if kind == "s8":
+        c.dev_scales.copy_(c.scales)
+    q = torch.zeros(B, 2, D, dtype=dtype)
+    q[:, :, 0] = 1
+    out = f8.f8_attend_paged(q.to(DEV), table=c.table.to(DEV).repeat(B, 1), lens=torch.full((B,), n, dtype=torch.int32, device=DEV),
+                             scale=float(nats), **c.args()).cpu()
+    k, v = (x[:, 0] for x in c.rows(0))
+    p = (k[:, 0] * nats).softmax(0)
+    want = p @ v
+    delta = (D + 8) * 2.0 ** -24 * (2 * nats + 1) + (D * 2.0 ** -25 * nats if kind == "s8" else 0)
+    half = HALF[torch.bfloat16 if kind == "bf16" else torch.float16]
+    err = (p @ v.abs()) * (half + 4 * delta) + n * 2.0 ** -40 * 2 + HALF[dtype] * want.abs() + (2.0 ** -25 if dtype == torch.float16 else 0)
+    assert ((out.double() - want).abs() <= err).all(), ((out.double() - want).abs() / want).max()
