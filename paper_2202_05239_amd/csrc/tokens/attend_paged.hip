@@ -253,14 +253,13 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
         }
       }
       if (S8) {
-        // a power of two brings the largest element of the head into [1, 2): f16 then holds what the 16-bit q had, elements
-        // 2^-14 below the largest excepted
+        // a power of two brings the largest element of the head to [2^14, 2^15): f16 then holds what the 16-bit q had, elements
+        // 2^-28 below the largest excepted
         top = max(top, (uint32_t)__shfl_xor((int)top, 16));
         top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        const int ex = (int)(top >> 23);
-        const bool plain = ex > 0 && ex < 254;
-        q_scale *= plain ? __int_as_float(ex << 23) : 1.0f;
-        const float inv = plain ? __int_as_float((254 - ex) << 23) : 1.0f;
+        const int ex = max((int)(top >> 23), 15);             // (the two factors are then normal numbers, for an infinity's exponent too)
+        q_scale *= __int_as_float((ex - 14) << 23);
+        const float inv = __int_as_float((268 - ex) << 23);
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll

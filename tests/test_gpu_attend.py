@@ -416,3 +416,48 @@ def test_many_small_weights_beside_a_large_one(kind, dtype, nats):
     half = HALF[torch.bfloat16 if kind == "bf16" else torch.float16]
     err = (p @ v.abs()) * (half + 4 * delta) + n * 2.0 ** -40 * 2 + HALF[dtype] * want.abs() + (2.0 ** -25 if dtype == torch.float16 else 0)
     assert ((out.double() - want).abs() <= err).all(), ((out.double() - want).abs() / want).max()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_small_elements_of_a_query_beside_a_large_one(dtype):
+    """8-bit keys that are zero where the query is largest: the scores are those of its small elements, which lose nothing down to
+    2^-28 of the largest.  Error of a score: its sum in 32 bits."""
+    n, D = 100, 64
+    g = torch.Generator().manual_seed(5)
+    for small in (2.0 ** -8, 2.0 ** -14, 2.0 ** -17, 2.0 ** -19):
+        c = Cache(16, [n], 1, D, 16, "s8")
+        t = torch.arange(n)
+        c.kv[0, c.table[0, t // 16].long(), t % 16, :, 7] = 0
+        c.dev.copy_(c.kv)
+        q = torch.randn(1, 2, D, generator=g) * small
+        q[0, :, 7] = 1.9
+        q = q.to(dtype)
+        s = 1 / small                                            # scores of some units
+        out = f8.f8_attend_paged(q.to(DEV), table=c.table.to(DEV), lens=torch.tensor([n], dtype=torch.int32, device=DEV), scale=s, **c.args()).cpu()
+        k, v = (x[:, 0] for x in c.rows(0))
+        for h in range(2):
+            qd = q[0, h].double()
+            score = k @ qd * s
+            p = score.softmax(0)
+            size = ((k.abs() @ qd.abs()) * s).max()
+            delta = (D + 8) * 2.0 ** -24 * (size + score.abs().max() + 1)
+            want, mass = p @ v, p @ v.abs()
+            err = mass * (2.0 ** -11 + 4 * delta) + n * 2.0 ** -40 * v.abs().max() + HALF[dtype] * want.abs() + 2.0 ** -25
+            assert ((out[0, h].double() - want).abs() <= err).all(), small
+
+
+@pytest.mark.parametrize("top", [2.0 ** -130, 2.0 ** -100, 1.0, 2.0 ** 100, 3e38])
+def test_queries_of_every_size(top):
+    # bf16 queries as small and as large as there are, and a scale that brings the scores back to some units
+    n, D = 70, 64
+    c = Cache(18, [n], 1, D, 16, "s8")
+    q = torch.randn(1, 2, D, generator=torch.Generator().manual_seed(6)).clamp(-3, 3) / 4
+    q[0, 0, 0], q[0, 1, 5] = 1, -1
+    q = (q.double() * top).bfloat16()
+    s = min(1 / top, 2.0 ** 125)                                  # (2^-130: as far as a scale can, scores of 2^-5 and below)
+    out = f8.f8_attend_paged(q.to(DEV), table=c.table.to(DEV), lens=torch.tensor([n], dtype=torch.int32, device=DEV), scale=s, **c.args()).cpu()
+    check(c, q, out, s)
+    q[0, 1, 5] = float("inf")
+    out = f8.f8_attend_paged(q.to(DEV), table=c.table.to(DEV), lens=torch.tensor([n], dtype=torch.int32, device=DEV), scale=s, **c.args()).cpu()
+    check(c, q[:, :1], out[:, :1], s)
+    assert out[0, 1].isnan().all()
