@@ -17,10 +17,14 @@
 // Codes are exact in 16-bit floating point.  A key's scale multiplies its score; a value's scale counts in the maximum,
 // m = max(s_t + max(log2 scale_t, SMALL)) (scores as powers of two), so that exp2(s_t - m) scale_t, the weight of a row of codes, is at
 // most 1 whatever the scales are.  The sum of the softmax takes exp2(s_t - m) itself, which a row with a small scale brings up to 2^-SMALL: rows
-// of zeros, whose scale is 2^-126 or 0, are the ones that come.  Weights are rounded
-// to 16 bits for the second product (as P is for 16-bit caches): relative 2^-12 (f16) or 2^-9 (bf16) of each weight, at random.  In f16 all
-// weights and sums are 2^15 times what is written here, the largest that f16 holds: the relative error then holds down to 2^-29 of the largest
-// weight, and what lies below is off by 2^-40 of it at most, 2^-23 of it over 131072 tokens.  Scores, maxima, sums and outputs are 32 bits.
+// of zeros, whose scale is 2^-126 or 0, are the ones that come.
+//
+// The second product takes weights of 16 bits.  Under 16-bit caches a weight goes in as two of them, what it rounds to and the rest: one
+// alone would be as coarse as the result (8 requests of up to 300 tokens, off the exact result: bf16 1.84e-3 with one, 1.66e-3 with two, which
+// is the rounding of the result alone; f16 2.18e-4 and 2.02e-4; 6.2 and 6.4 us, 16 requests of up to 8192 tokens 44.9 and 45.6).  Under 8-bit
+// caches it is rounded once, to f16, relative 2^-11: an eighth of the half unit that 8 bits leave a row's largest element.
+// In f16 all weights and sums are 2^15 times what is written here, the largest that f16 holds: the relative error then holds down to 2^-29 of
+// the largest weight, and what lies below is off by 2^-40 of it at most, 2^-23 of it over 131072 tokens.  Scores, maxima, sums and outputs are 32 bits.
 //
 // Bound by HBM: every cached byte is read once, in whole rows, one tile ahead per wave (131072 tokens of 8 heads, 277 MB: 67 us with
 // the second launch, 4.2 TB/s; 64 requests of up to 8192 tokens, 491 MB: 113 us, 4.35 TB/s; a large copy reaches 5.5).  The vector units
@@ -158,6 +162,7 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
   typedef Operand<C> Op;
   typedef typename Op::t H;
   constexpr bool S8 = sizeof(C) == 1;
+  constexpr bool REST = !S8;                 // weights in two parts
   constexpr int E = DP / 16, VB = E * (int)sizeof(C);     // elements and bytes of a value row per lane
   constexpr int KL = DP * (int)sizeof(C) / 64;            // 16-byte loads of a key row per lane
   constexpr int KS = DP / 32;                             // products per block of 16 scores
@@ -388,15 +393,17 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
         m = top;
       }
       typedef H t8 __attribute__((ext_vector_type(8)));
-      t8 wh;
+      t8 wh, wl;
       const float below = base - Op::UP;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float w = __builtin_amdgcn_exp2f(s[j] - below);
         l += w;
-        wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : w);
+        const float weight = S8 ? w * vs[j >> 2][j & 3] : w;
+        wh[j] = (H)weight;
+        if constexpr (REST) wl[j] = (H)(weight - (float)wh[j]);
       }
-      const v4i pt = __builtin_bit_cast(v4i, wh);
+      const v4i pt = __builtin_bit_cast(v4i, wh), rest = __builtin_bit_cast(v4i, wl);
 #pragma unroll
       for (int n = 0; n < E; ++n) {
         v4i a;
@@ -413,6 +420,7 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
           for (int j = 0; j < 4; ++j) a[j] = (int)__builtin_amdgcn_perm(x.v[2 * j + 1].d[n >> 1], x.v[2 * j].d[n >> 1], sel);
         }
         o[n] = Op::mfma(a, pt, o[n]);
+        if constexpr (REST) o[n] = Op::mfma(a, rest, o[n]);
       }
     };
 

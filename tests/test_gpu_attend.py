@@ -461,3 +461,23 @@ def test_queries_of_every_size(top):
     out = f8.f8_attend_paged(q.to(DEV), table=c.table.to(DEV), lens=torch.tensor([n], dtype=torch.int32, device=DEV), scale=s, **c.args()).cpu()
     check(c, q[:, :1], out[:, :1], s)
     assert out[0, 1].isnan().all()
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS[2:])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_weights_of_16_bit_caches(kind, dtype, D):
+    """Weights in two parts of the cache's type: off by the square of its half unit, 2^-16 at most (f16 also by 2^-40 of the largest).
+    Otherwise as in check(): scores in 32 bits, the result's own rounding."""
+    lens = [2, 9, 64, 300, 1500]
+    c = Cache(19 + D, lens, 2, D, 16, kind)
+    q, out = run(c, len(lens), 6, D, dtype, scale=0.03)
+    for b, n in enumerate(lens):
+        k, v = (t.repeat_interleave(3, 1) for t in c.rows(b))
+        qd = q[b].double()
+        s = torch.einsum("hd,nhd->hn", qd, k) * 0.03
+        p = s.softmax(-1)
+        want, mass = torch.einsum("hn,nhd->hd", p, v), torch.einsum("hn,nhd->hd", p, v.abs())
+        size = torch.einsum("hd,nhd->hn", qd.abs(), k.abs()).amax(-1) * 0.03
+        delta = (D + 8) * 2.0 ** -24 * (size + s.abs().amax(-1) + 1)
+        err = mass * (2.0 ** -16 + 4 * delta[:, None]) + n * 2.0 ** -40 * v.abs().max() + HALF[dtype] * want.abs() + (2.0 ** -25 if dtype == torch.float16 else 0)
+        assert ((out[b].double() - want).abs() <= err).all(), n
