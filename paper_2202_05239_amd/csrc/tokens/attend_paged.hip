@@ -19,12 +19,13 @@
 // most 1 whatever the scales are.  The sum of the softmax takes exp2(s_t - m) itself, which a row with a small scale brings up to 2^-SMALL: rows
 // of zeros, whose scale is 2^-126 or 0, are the ones that come.
 //
-// The second product takes weights of 16 bits.  Under 16-bit caches a weight goes in as two of them, what it rounds to and the rest: one
+// The second product takes weights of 16 bits.  Under 16-bit caches a weight goes in as two of them, its front and the rest: one
 // alone would be as coarse as the result (8 requests of up to 300 tokens, off the exact result: bf16 1.84e-3 with one, 1.66e-3 with two, which
-// is the rounding of the result alone; f16 2.18e-4 and 2.02e-4; 6.2 and 6.4 us, 16 requests of up to 8192 tokens 44.9 and 45.6).  Under 8-bit
+// is the rounding of the result alone; f16 2.18e-4 and 2.02e-4; 6.3 and 6.5 us, 16 requests of up to 8192 tokens 45.2 and 45.9).  Under 8-bit
 // caches it is rounded once, to f16, relative 2^-11: an eighth of the half unit that 8 bits leave a row's largest element.
 // In f16 all weights and sums are 2^15 times what is written here, the largest that f16 holds: the relative error then holds down to 2^-29 of
-// the largest weight, and what lies below is off by 2^-40 of it at most, 2^-23 of it over 131072 tokens.  Scores, maxima, sums and outputs are 32 bits.
+// the largest weight, and what lies below is off by 2^-40 of it at most, 2^-23 of it over 131072 tokens
+// (in two parts 2^-39 above that line: a rest is never 0).  Scores, maxima, sums and outputs are 32 bits.
 //
 // Bound by HBM: every cached byte is read once, in whole rows, one tile ahead per wave (131072 tokens of 8 heads, 277 MB: 67 us with
 // the second launch, 4.2 TB/s; 64 requests of up to 8192 tokens, 491 MB: 113 us, 4.35 TB/s; a large copy reaches 5.5).  The vector units
@@ -112,6 +113,13 @@ template <typename C>
 struct Operand {                            // 16-bit type of the products
   typedef f16 t;
   static constexpr float UP = 15.0f;        // the largest weight as a power of two
+  // Two weights, cut to 16 bits, and what is left of them: never negative, nor 0 where the weight is a normal number, so that an infinite
+  // value times both is infinite
+  static __device__ __forceinline__ uint32_t cut(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b)); }
+  static __device__ __forceinline__ t rest(float w, uint32_t pair, int k) {
+    const float left = w - (float)__builtin_bit_cast(h2, pair)[k];
+    return (t)fmaxf(left, fminf(w * 0x1p-10f, 0x1p-24f));
+  }
   static __device__ __forceinline__ v4f mfma(v4i a, v4i b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
   }
@@ -120,6 +128,11 @@ template <>
 struct Operand<bf16> {
   typedef bf16 t;
   static constexpr float UP = 0.0f;         // (has the range of 32 bits)
+  static __device__ __forceinline__ uint32_t cut(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
+  static __device__ __forceinline__ t rest(float w, uint32_t pair, int k) {
+    const float left = w - __uint_as_float(k ? pair & 0xffff0000u : pair << 16);
+    return (t)fmaxf(left, fminf(w, 0x1p-100f));
+  }
   static __device__ __forceinline__ v4f mfma(v4i a, v4i b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
   }
@@ -162,7 +175,6 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
   typedef Operand<C> Op;
   typedef typename Op::t H;
   constexpr bool S8 = sizeof(C) == 1;
-  constexpr bool REST = !S8;                 // weights in two parts
   constexpr int E = DP / 16, VB = E * (int)sizeof(C);     // elements and bytes of a value row per lane
   constexpr int KL = DP * (int)sizeof(C) / 64;            // 16-byte loads of a key row per lane
   constexpr int KS = DP / 32;                             // products per block of 16 scores
@@ -393,17 +405,29 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
         m = top;
       }
       typedef H t8 __attribute__((ext_vector_type(8)));
-      t8 wh, wl;
+      float w[8];
+      v4i pt, rest;
       const float below = base - Op::UP;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float w = __builtin_amdgcn_exp2f(s[j] - below);
-        l += w;
-        const float weight = S8 ? w * vs[j >> 2][j & 3] : w;
-        wh[j] = (H)weight;
-        if constexpr (REST) wl[j] = (H)(weight - (float)wh[j]);
+        w[j] = __builtin_amdgcn_exp2f(s[j] - below);
+        l += w[j];
       }
-      const v4i pt = __builtin_bit_cast(v4i, wh), rest = __builtin_bit_cast(v4i, wl);
+      if constexpr (S8) {
+        t8 wh;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) wh[j] = (H)(w[j] * vs[j >> 2][j & 3]);
+        pt = __builtin_bit_cast(v4i, wh);
+      } else {
+        t8 wl;
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const uint32_t pair = Op::cut(w[j], w[j + 1]);
+          pt[j / 2] = (int)pair;
+          wl[j] = Op::rest(w[j], pair, 0), wl[j + 1] = Op::rest(w[j + 1], pair, 1);
+        }
+        rest = __builtin_bit_cast(v4i, wl);
+      }
 #pragma unroll
       for (int n = 0; n < E; ++n) {
         v4i a;
@@ -420,7 +444,7 @@ __global__ __launch_bounds__(64 * WAVES, DP * sizeof(C) > 128 ? 1 : 2) void atte
           for (int j = 0; j < 4; ++j) a[j] = (int)__builtin_amdgcn_perm(x.v[2 * j + 1].d[n >> 1], x.v[2 * j].d[n >> 1], sel);
         }
         o[n] = Op::mfma(a, pt, o[n]);
-        if constexpr (REST) o[n] = Op::mfma(a, rest, o[n]);
+        if constexpr (!S8) o[n] = Op::mfma(a, rest, o[n]);
       }
     };
 

@@ -481,3 +481,21 @@ def test_weights_of_16_bit_caches(kind, dtype, D):
         delta = (D + 8) * 2.0 ** -24 * (size + s.abs().amax(-1) + 1)
         err = mass * (2.0 ** -16 + 4 * delta[:, None]) + n * 2.0 ** -40 * v.abs().max() + HALF[dtype] * want.abs() + (2.0 ** -25 if dtype == torch.float16 else 0)
         assert ((out[b].double() - want).abs() <= err).all(), n
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 40, 3000])
+def test_infinite_values_of_16_bit_caches(dtype, n):
+    # an infinity that has some weight gives an infinity of its sign, two that differ give NaN
+    c = Cache(20, [n, 33], 2, 64, 16, "f16" if dtype == torch.float16 else "bf16")
+    at = (1, c.table[0, (n - 1) // 16].item(), (n - 1) % 16)
+    c.dev[at][0, 5], c.dev[at][0, 6], c.dev[at][1, 63] = float("inf"), -float("inf"), float("inf")
+    if n > 1:
+        c.dev[1, c.table[0, 0].item(), 0, 1, 63] = -float("inf")
+    for scale in (0.0, 0.01):                                     # weights that are all the same, with nothing left of them, and others
+        q, out = run(c, 2, 4, 64, dtype, scale=scale)
+        want = torch.zeros(4, 64)
+        want[:2, 5], want[:2, 6], want[2:, 63] = float("inf"), -float("inf"), float("nan") if n > 1 else float("inf")
+        odd = ~torch.isfinite(want)
+        assert torch.equal(torch.nan_to_num(out[0].float()[odd], 1e9, 2e9, -2e9), torch.nan_to_num(want[odd], 1e9, 2e9, -2e9))
+        assert torch.isfinite(out[0][~odd]).all() and torch.isfinite(out[1]).all()
