@@ -542,7 +542,7 @@ def f8_norm_tokens(a, res=None, post=None, post_w=None, post_b=None, gate=None, 
         if res.dtype != dtype:
             raise TypeError("res has to be in the type of a")
     if gate is not None:
-        gate_rows = rows if gate_rows is None else int(gate_rows)
+        gate_rows = max(rows, 1) if gate_rows is None else int(gate_rows)
         ldg = _matrix(gate)
         if gate.dtype != dtype:
             raise TypeError("gate has to be in the type of a")

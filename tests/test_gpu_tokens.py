@@ -213,6 +213,15 @@ def test_norm_keeps_nan_in_its_row():
     assert (f8.f8_norm_tokens(z, pre="rms")[1] == 0).all() and (f8.f8_norm_tokens(z + 5, pre="layer")[1] == 0).all()
 
 
+def test_norm_of_no_rows():
+    a = torch.empty(0, 64, dtype=torch.float16, device=DEV)
+    for gate in (None, torch.ones(1, 64, dtype=torch.float16, device=DEV), torch.ones(0, 64, dtype=torch.float16, device=DEV)):
+        r, y = f8.f8_norm_tokens(a, gate=gate)
+        assert r.shape == (0, 64) and y.shape == (0, 64)
+        r, codes, scale = f8.f8_norm_tokens(a, res=a, gate=gate, codes=True)
+        assert codes.shape == (0, 64) and scale.shape == (0,)
+
+
 # ---- the products ---------------------------------------------------------------------------------
 
 def codes_of(g, rows, cols):
