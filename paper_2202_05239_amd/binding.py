@@ -486,6 +486,13 @@ def _vector(t, n, dtype=None):
     return t.data_ptr()
 
 
+def _no_gradient(*tensors):
+    """Refuses what autograd follows: the results would come back without their gradient."""
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise RuntimeError("the calls on tokens have no gradient: detach their inputs, or call them under torch.no_grad()")
+
+
 def _scratch(workspace, n, device):
     """(address, bytes, tensor) of at least n bytes; a tensor made here goes back to torch's allocator after the launch, which hands it
     on in the order of the stream."""
@@ -502,6 +509,7 @@ def f8_quant_tokens(x, gate=None, act=None, values=False, out=None, scale=None):
     codes stand for, in x's type: (values, scale)."""
     kind, ldx, shape, dtype = _real(x), _matrix(x), x.shape, x.dtype
     rows, cols = shape
+    _no_gradient(x, gate)
     if out is None:
         out, ldy = torch.empty(shape, dtype=dtype if values else torch.int8, device=x.device), cols
     else:
@@ -531,6 +539,7 @@ def f8_norm_tokens(a, res=None, post=None, post_w=None, post_b=None, gate=None, 
     (r, y), or with codes=True (r, codes, scale); r is None with keep_res=False.  gate [n][cols]: gate_rows rows share a row of it."""
     kind, lda, shape, dtype = _real(a), _matrix(a), a.shape, a.dtype
     rows, cols = shape
+    _no_gradient(a, res, gate, post_w, post_b, pre_w, pre_b)
     w_type, at_w = None, [None] * 4
     for i, t in enumerate((post_w, post_b, pre_w, pre_b)):
         if t is not None:
@@ -589,6 +598,7 @@ def f8_linear_scaled(x, sx, w, sw, bias=None, y=None, y_dtype=None):
     nothing else is asked for."""
     if x.dtype != torch.int8:
         raise TypeError("the tokens have to be int8")
+    _no_gradient(sx, sw, bias)
     d, y, M, N = _linear_desc(x, F8_S8, w, y, y_dtype or torch.bfloat16)
     rc = (_lib or lib()).f8_linear_scaled(x.data_ptr(), _vector(sx, M, torch.float32), w.data_ptr(), _vector(sw, N, torch.float32),
                                           _vector(bias, N, torch.float32), y.data_ptr(), d, _stream())
@@ -599,6 +609,7 @@ def f8_linear_scaled(x, sx, w, sw, bias=None, y=None, y_dtype=None):
 
 def f8_linear_tokens(x, w, sw, bias=None, y=None, y_dtype=None, workspace=None):
     """The same from real tokens, which are quantised on the way; y in x's type if nothing else is asked for."""
+    _no_gradient(x, sw, bias)
     d, y, M, N = _linear_desc(x, _real(x), w, y, y_dtype or x.dtype)
     L = _lib or lib()
     at_ws, n, _keep = _scratch(workspace, L.f8_linear_workspace_bytes(M, d.K), x.device)
@@ -627,6 +638,7 @@ def _kv_layout(k, v, k_scale, v_scale):
 def f8_kv_append(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None):
     """Keys and values of new tokens, [tokens][heads][dim], into the cache's slots (page * page_size + place; negative: skipped)."""
     c = _kv_layout(k_cache, v_cache, k_scale, v_scale)
+    _no_gradient(k, v)
     shape, ks, vs = k.shape, k.stride(), v.stride()
     if v.shape != shape or k.dtype != v.dtype or shape[1:] != (c.heads, c.dim) or ks[2] != 1 or vs[2] != 1:
         raise ValueError("k and v have to be [tokens][%d][%d] of one type, the last dimension contiguous" % (c.heads, c.dim))
@@ -642,6 +654,7 @@ def f8_attend_paged(q, k_cache, v_cache, table, lens, k_scale=None, v_scale=None
     """One new token per request, q [batch][q_heads][dim], over its lens[b] cached tokens, whose pages table [batch][cols] lists.
     scale: of the scores (1 / sqrt(dim)); max_len: no request is longer (as long as the table allows)."""
     c = _kv_layout(k_cache, v_cache, k_scale, v_scale)
+    _no_gradient(q, k_cache, v_cache)
     shape, qs = q.shape, q.stride()
     B, H, D = shape
     if D != c.dim or qs[2] != 1:

@@ -205,3 +205,22 @@ def test_binding_refuses_matrices_whose_rows_overlap():
 def test_binding_takes_single_rows_of_any_stride():
     assert f8._matrix(torch.zeros(1, 64).expand(1, 64)) == 64 and f8._matrix(torch.zeros(64, 1).t()) == 64 and f8._matrix(torch.zeros(0, 64)) == 64
     assert f8._matrix(torch.zeros(4, 80)[:, :64]) == 80 and f8._matrix(torch.zeros(4, 1)) == 1 and f8._matrix(torch.zeros(4, 2)[:, :1]) == 2
+
+
+def test_binding_refuses_what_autograd_follows():
+    # (a result without its gradient would go unnoticed; under no_grad the same calls go on, here as far as a GPU is needed)
+    x, w, one = torch.zeros(4, 64), torch.zeros(8, 64, dtype=torch.int8), torch.ones(8)
+    live = lambda t: t.clone().requires_grad_()  # noqa: E731
+    kv, q = torch.zeros(2, 3, 16, 2, 64).half(), torch.zeros(1, 4, 64).half()
+    new, slot, table, lens = torch.zeros(1, 2, 64).half(), torch.zeros(1, dtype=torch.int64), torch.zeros(1, 3, dtype=torch.int32), torch.ones(1, dtype=torch.int32)
+    calls = [lambda: f8.f8_quant_tokens(live(x)), lambda: f8.f8_quant_tokens(x, gate=live(x)),
+             lambda: f8.f8_norm_tokens(live(x)), lambda: f8.f8_norm_tokens(x, res=live(x)), lambda: f8.f8_norm_tokens(x, pre_w=live(torch.ones(64))),
+             lambda: f8.f8_linear_tokens(live(x), w, one), lambda: f8.f8_linear_tokens(x, w, live(one)), lambda: f8.f8_linear_tokens(x, w, one, bias=live(one)),
+             lambda: f8.f8_linear_scaled(w, live(one), w, one), lambda: f8.f8_kv_append(live(new), new, slot, kv[0], kv[1]),
+             lambda: f8.f8_attend_paged(live(q), kv[0], kv[1], table, lens)]
+    for call in calls:
+        with pytest.raises(RuntimeError, match="gradient"):
+            call()
+    with torch.no_grad():
+        f8._no_gradient(live(x), None)
+    f8._no_gradient(x, None)
