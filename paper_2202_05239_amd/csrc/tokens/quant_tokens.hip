@@ -23,12 +23,15 @@ struct QuantParams {
 };
 
 // silu(g) = g / (1 + e^-g); gelu(g) = g / (1 + e^(-2 u)), u = sqrt(2/pi) (g + 0.044715 g^3), the tanh form.  For large -g the
-// exponential is infinite and the quotient 0; g = -inf gives NaN, as the formulas do.  The exponential as 2^(u log2 e) is off by
-// |u| units in the last place, which counts up to u = -20, where silu itself is below 2^-24 of its neighbours; with it and a
-// reciprocal instead of exact calls the kernel is no longer bound by its instructions (8192 x 16384 bf16: 177 us before).
+// exponential is infinite and the quotient 0; g = -inf gives NaN, as the formulas do.  For 16-bit tensors, which round at 2^-11 or above,
+// the exponential is 2^(u log2 e), off by up to |u| units in the last place of 32 bits (2^-17 at u = -100), and the quotient a product
+// with a reciprocal: with exact calls the kernel is bound by its instructions (8192 x 16384 bf16 177 us against 140).  32-bit tensors
+// get the exact calls (8192 x 16384 305 us either way, 64 x 4096 4.6 and 5.4).
+template <typename T>
 __device__ __forceinline__ float act_of(int act, float g) {
   if (act == F8_ACT_NONE) return g;
   const float u = act == F8_ACT_SILU ? g : 1.5957691216057308f * g * __builtin_fmaf(0.044715f * g, g, 1.0f);
+  if constexpr (sizeof(T) == 4) return g / (1.0f + expf(-u));
   return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * u));
 }
 
@@ -52,7 +55,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void quant_tokens_kernel(Qua
       float g[8];
       load_piece<T, Map>(gate, i, t, p.cols, g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] *= act_of(p.act, g[j]);
+      for (int j = 0; j < 8; ++j) v[i][j] *= act_of<T>(p.act, g[j]);
     }
   }
 #pragma unroll

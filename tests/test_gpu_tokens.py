@@ -121,6 +121,21 @@ def test_gated_rows(act, dtype):
         assert ((codes.cpu().double() - v / s[:, None]).abs() <= 0.5 + 127 * 4 * rel).all()
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gates_in_32_bits(act):
+    """Rows of one column, whose scale is |act(g)| / 127.  silu: exponential to 2 units in the last place, sum, quotient, division by
+    127: 4 + 3 half units, 8 allowed.  gelu: its argument u is off by 5 half units relative, which are |u| times as many of the result."""
+    low = -84.0 if act == "silu" else -9.0
+    g = torch.cat([torch.linspace(low, 30, 4096), torch.linspace(-1, 1, 1001), torch.tensor([-20.5, -40.25, -60.125, -80.0625]).clamp_min(low)])[:, None]
+    codes, scale = f8.f8_quant_tokens(torch.ones_like(g).to(DEV), gate=g.to(DEV), act=act)
+    gd = g.double()[:, 0]
+    u = gd if act == "silu" else 2 * math.sqrt(2 / math.pi) * (gd + 0.044715 * gd ** 3)
+    want = gd / (1 + torch.exp(-u)) / 127
+    tol = (8 + (5 * u.abs() if act == "gelu" else 0)) * U32
+    assert ((scale.cpu().double() - want.abs()).abs() <= tol * want.abs() + TINY).all()
+    assert torch.equal(codes.cpu()[:, 0].sign().int(), want.sign().int())
+
+
 def test_extreme_gates():
     g = torch.tensor([[-1e4, -88.0, -100.0, 0.0, 1e4, 30.0, -30.0, 3e38]])
     for act in ("silu", "gelu"):
