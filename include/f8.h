@@ -407,7 +407,7 @@ f8_status f8_norm_tokens(const void *a, const void *res, const void *post_w, con
 /* Product of 8-bit tokens x [M][K] and 8-bit weights w [N][K]:
  *     y[m][n] = sx[m] * sw[n] * sum_k x[m][k] w[n][k] + bias[n]
  * with the sum exact in 32 bits; bias [N] float or NULL; y in y_type (real).  1 <= K <= F8_LINEAR_MAX_K, M and N up to
- * F8_LINEAR_MAX_ROWS.  x_type is F8_S8. */
+ * F8_LINEAR_MAX_ROWS (results of 2^36 elements and more: F8_ERR_UNSUPPORTED where a launch cannot hold their tiles).  x_type is F8_S8. */
 #define F8_LINEAR_MAX_K 131071
 #define F8_LINEAR_MAX_ROWS (1 << 26)
 typedef struct {

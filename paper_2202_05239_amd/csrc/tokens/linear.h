@@ -87,9 +87,11 @@ constexpr int64_t LINEAR_TILES_MOST = 1 << 22;   // workgroups of a launch (2^32
 // Tiles through LDS by its own loads, for operands whose rows start on 4 bytes.  `tile`: which (linear_tile.hip).
 f8_status launch_linear_tile(const LinearParams &p, int y_type, int tile, hipStream_t s);
 // What takes least, by estimate: `tile` over tokens 0 .. M1 - 1 and channels 0 .. N1 - 1, and if that is not all, `tile2` over the rest.
+// (The rest is less than a round of the first tile: its workgroups always fit a launch.)
 struct LinearPlan {
   int tile, M1, N1, tile2;
   float us;
+  int64_t wgs;                             // of the first launch
 };
 LinearPlan linear_plan(int M, int N, int K);
 

@@ -198,9 +198,8 @@ __global__ __launch_bounds__(64 * WN * WM * KG) void linear_tile_kernel(LinearPa
 template <typename T, int WN, int WM, int NB, int MB, int RING, int KG>
 f8_status launch(const LinearParams &p, hipStream_t s) {
   constexpr int BN = 32 * NB * WN, BM = 32 * MB * WM;
-  const int64_t tn = (p.N + BN - 1) / BN, tm = (p.M + BM - 1) / BM;
-  if (tn * tm > LINEAR_TILES_MOST) return F8_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((linear_tile_kernel<T, WN, WM, NB, MB, RING, KG>), dim3((unsigned)(tn * tm)), dim3(64 * WN * WM * KG), 0, s, p, (int)tm, (int)tn);
+  const int tn = (p.N + BN - 1) / BN, tm = (p.M + BM - 1) / BM;
+  hipLaunchKernelGGL((linear_tile_kernel<T, WN, WM, NB, MB, RING, KG>), dim3((unsigned)(tn * tm)), dim3(64 * WN * WM * KG), 0, s, p, tm, tn);
   return launch_status();
 }
 
@@ -273,14 +272,16 @@ LinearPlan linear_plan(int M, int N, int K) {
     if (n1 > 0 && n1 < N) {
       const int tile2 = best_tile(M, N - n1, K, &rest);
       const float us = tile_us(t, M, n1, K) + rest + 2.0f;
-      if (us < 0.95f * plan.us) plan = LinearPlan{i, M, n1, tile2, us};
+      if (us < 0.95f * plan.us) plan = LinearPlan{i, M, n1, tile2, us, 0};
     }
     if (m1 > 0 && m1 < M) {
       const int tile2 = best_tile(M - m1, N, K, &rest);
       const float us = tile_us(t, m1, N, K) + rest + 2.0f;
-      if (us < 0.95f * plan.us) plan = LinearPlan{i, m1, N, tile2, us};
+      if (us < 0.95f * plan.us) plan = LinearPlan{i, m1, N, tile2, us, 0};
     }
   }
+  const Tile &t = TILES[plan.tile];
+  plan.wgs = (int64_t)((plan.M1 + t.bm - 1) / t.bm) * ((plan.N1 + t.bn - 1) / t.bn);
   return plan;
 }
 

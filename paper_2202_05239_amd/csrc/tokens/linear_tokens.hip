@@ -88,17 +88,17 @@ __global__ __launch_bounds__(256, 2) void linear_any_kernel(LinearParams p, int 
 
 template <typename T, int TILE>
 f8_status launch_any_tile(const LinearParams &p, hipStream_t s) {
-  const int64_t tm = (p.M + TILE - 1) / TILE, tn = (p.N + TILE - 1) / TILE;
-  if (tm * tn > LINEAR_TILES_MOST) return F8_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((linear_any_kernel<T, TILE>), dim3((unsigned)(tm * tn)), dim3(256), 0, s, p, (int)tm);
+  const int tm = (p.M + TILE - 1) / TILE, tn = (p.N + TILE - 1) / TILE;
+  hipLaunchKernelGGL((linear_any_kernel<T, TILE>), dim3((unsigned)(tm * tn)), dim3(256), 0, s, p, tm);
   return launch_status();
 }
 
 // Tiles of 64 where those of 128 would leave CUs without one.
+int64_t any_tiles(const LinearParams &p, int tile) { return (int64_t)((p.M + tile - 1) / tile) * ((p.N + tile - 1) / tile); }
+int any_tile(const LinearParams &p) { return any_tiles(p, 128) < 256 ? 64 : 128; }
 template <typename T>
 f8_status launch_any(const LinearParams &p, hipStream_t s) {
-  const int64_t tiles = (int64_t)((p.M + 127) / 128) * ((p.N + 127) / 128);
-  return tiles < 256 ? launch_any_tile<T, 64>(p, s) : launch_any_tile<T, 128>(p, s);
+  return any_tile(p) == 64 ? launch_any_tile<T, 64>(p, s) : launch_any_tile<T, 128>(p, s);
 }
 
 f8_status check(const f8_linear_desc *d) {
@@ -143,12 +143,25 @@ bool few_quantises(int M, int N, int K) {
   return M <= LINEAR_FEW && stretches <= (N <= 8192 ? LINEAR_FEW_HELD : LINEAR_FEW_HELD / 2);
 }
 
-f8_status enqueue_linear(const LinearParams &p, int y_type, hipStream_t s) {
+// Which kernel takes a product.  What does not fit a launch is known before anything is enqueued.
+struct Route {
+  bool tiles, few, fits;
+  LinearPlan plan;
+};
+Route route_of(const LinearParams &p) {
   // tiles: rows on 4 bytes, and within reach of 31-bit offsets inside a tile
-  const bool tiles = aligned_to(p.x, 4) && aligned_to(p.w, 4) && p.ldx % 4 == 0 && p.ldw % 4 == 0 && p.ldx < (1 << 22) && p.ldw < (1 << 22);
-  const LinearPlan plan = linear_plan(p.M, p.N, p.K);
-  if (p.M <= LINEAR_FEW_MOST && few_us(p, !tiles) < (tiles ? plan.us : any_us(p))) return launch_linear_few(p, F8_S8, y_type, s);
-  if (tiles) {
+  Route r;
+  r.tiles = aligned_to(p.x, 4) && aligned_to(p.w, 4) && p.ldx % 4 == 0 && p.ldw % 4 == 0 && p.ldx < (1 << 22) && p.ldw < (1 << 22);
+  r.plan = linear_plan(p.M, p.N, p.K);
+  r.few = p.M <= LINEAR_FEW_MOST && few_us(p, !r.tiles) < (r.tiles ? r.plan.us : any_us(p));
+  r.fits = r.few || (r.tiles ? r.plan.wgs : any_tiles(p, any_tile(p))) <= LINEAR_TILES_MOST;
+  return r;
+}
+
+f8_status enqueue_linear(const LinearParams &p, const Route &r, int y_type, hipStream_t s) {
+  const LinearPlan &plan = r.plan;
+  if (r.few) return launch_linear_few(p, F8_S8, y_type, s);
+  if (r.tiles) {
     LinearParams part = p;
     part.M = plan.M1, part.N = plan.N1;
     const f8_status st = launch_linear_tile(part, y_type, plan.tile, s);
@@ -187,7 +200,8 @@ f8_status f8_linear_scaled(const int8_t *x, const float *sx, const int8_t *w, co
   if (!sx) return F8_ERR_NULL;
   if (!aligned_to(sx, 4)) return F8_ERR_ALIGN;
   const LinearParams p{x, w, sx, sw, bias, y, d->ldx, d->ldw, d->ldy, d->M, d->N, d->K};
-  return enqueue_linear(p, d->y_type, static_cast<hipStream_t>(stream));
+  const Route r = route_of(p);
+  return r.fits ? enqueue_linear(p, r, d->y_type, static_cast<hipStream_t>(stream)) : F8_ERR_UNSUPPORTED;
 }
 
 size_t f8_linear_workspace_bytes(int M, int K) {
@@ -214,10 +228,11 @@ f8_status f8_linear_tokens(const void *x, const int8_t *w, const float *sw, cons
   const int64_t pitch = code_pitch(d->K);
   int8_t *codes = static_cast<int8_t *>(workspace);
   float *sx = reinterpret_cast<float *>(codes + d->M * pitch);
-  st = enqueue_quant_tokens(x, d->ldx, d->x_type, codes, pitch, (int)pitch, sx, d->M, d->K, s);
-  if (st != F8_OK) return st;
   p.x = codes, p.sx = sx, p.ldx = pitch;
-  return enqueue_linear(p, d->y_type, s);
+  const Route r = route_of(p);
+  if (!r.fits) return F8_ERR_UNSUPPORTED;
+  st = enqueue_quant_tokens(x, d->ldx, d->x_type, codes, pitch, (int)pitch, sx, d->M, d->K, s);
+  return st == F8_OK ? enqueue_linear(p, r, d->y_type, s) : st;
 }
 
 }  // extern "C"

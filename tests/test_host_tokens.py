@@ -224,3 +224,15 @@ def test_binding_refuses_what_autograd_follows():
     with torch.no_grad():
         f8._no_gradient(live(x), None)
     f8._no_gradient(x, None)
+
+
+def test_products_that_no_launch_holds_are_refused_before_anything_runs():
+    # (without a GPU a launch is error 9: the quantiser in front must not have been tried)
+    L = f8.lib()
+    most = 1 << 26
+    ws = L.f8_linear_workspace_bytes(most, 32)
+    for y_type, w in ((f8.F8_F32, P), (f8.F8_BF16, P), (f8.F8_F16, ODD)):
+        d = l_desc(M=most, N=most, y_type=y_type, ldy=most)
+        assert L.f8_linear_scaled(P, P, w, P, None, P, d, None) == 8
+        d.x_type = f8.F8_BF16
+        assert L.f8_linear_tokens(P, w, P, None, P, d, P, ws, None) == 8
