@@ -92,8 +92,11 @@ void launch(const QuantParams &p, hipStream_t s) {
 }
 
 // Threads to a row: as many as leave each one or two pieces, up to 1024 (16384 gated columns, 8192 rows, us: 1024 threads of two pieces
-// 141, 512 of four 170, 256 of eight 201).  Widths just over 4096 leave half of 512 threads' second pieces empty: 256 threads of three, unless
-// rows are so few that each one's own time counts (1531 x 4100 f16 6.0 us against 7.5, 48 x 4100 3.6 against 3.3).
+// 141, 512 of four 170, 256 of eight 201).  Widths from 4097 to 6144 leave a quarter to a half of 512 threads' pieces empty: 256 threads of three, unless
+// rows are so few that each one's own time counts.  The line lies between 256 and 768 rows at all of these widths (bf16, three | two pieces, us): 4100
+// columns 256 rows 3.9 | 3.6, 512 4.1 | 4.0, 768 4.5 | 4.6, 2048 7.0 | 8.4, 16384 41 | 52; 6144 columns 3.5 | 3.5, 3.9 | 4.0, 4.3 | 4.7, 7.7 | 9.1,
+// 54 | 62; gated 5120 columns 5.8 | 5.0, 6.3 | 5.9, 6.7 | 7.0, 13.6 | 15.2, 85 | 102; 32 bits alike, behind only far out of the caches
+// (16384 x 6144 91.6 | 90.6, gated 176 | 165).
 template <typename T>
 f8_status launch_row(const QuantParams &p, hipStream_t s) {
   if (p.pad <= 512) launch<T, 64, 1>(p, s);
