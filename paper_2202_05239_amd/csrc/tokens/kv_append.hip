@@ -68,7 +68,8 @@ f8_status launch(const AppendParams &p, hipStream_t s) {
   dim3 grid = block_grid(((int64_t)p.rows + 256 / LANES - 1) / (256 / LANES));
   const dim3 block(256);
   grid.z = 2;
-  if (p.dim <= LANES * 8) hipLaunchKernelGGL((kv_append_kernel<T, C, 1>), grid, block, 0, s, p);
+  static_assert(RowMap<LANES, 2>::most == 256, "the most dimensions of a head");
+  if (p.dim <= RowMap<LANES, 1>::most) hipLaunchKernelGGL((kv_append_kernel<T, C, 1>), grid, block, 0, s, p);
   else hipLaunchKernelGGL((kv_append_kernel<T, C, 2>), grid, block, 0, s, p);
   return launch_status();
 }

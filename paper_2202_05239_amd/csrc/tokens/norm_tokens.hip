@@ -132,10 +132,13 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_tokens_kernel(Norm
   }
 }
 
+// (false where the threads' pieces do not cover a row)
 template <typename T, int TPR, int NV>
-void launch(const NormParams &p, hipStream_t s) {
+bool launch(const NormParams &p, hipStream_t s) {
+  if (p.cols > RowMap<TPR, NV>::most) return false;
   constexpr int THREADS = TPR == 64 ? 256 : TPR, RPB = THREADS / TPR;
   hipLaunchKernelGGL((norm_tokens_kernel<T, TPR, NV>), block_grid(((int64_t)p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
+  return true;
 }
 
 // Threads to a row: as many as leave each one or two pieces (registers, and so workgroups to a CU, are what counts: 4096 columns with
@@ -143,17 +146,11 @@ void launch(const NormParams &p, hipStream_t s) {
 // faster: 256 of two pieces 101 us, 512 of one 105.
 template <typename T>
 f8_status launch_row(const NormParams &p, hipStream_t s) {
-  if (p.cols <= 512) launch<T, 64, 1>(p, s);
-  else if (p.cols <= 1024) launch<T, 64, 2>(p, s);
-  else if (p.cols <= 2048) launch<T, 256, 1>(p, s);
-  else if (p.cols <= 4096 && p.post == F8_NORM_NONE) launch<T, 512, 1>(p, s);
-  else if (p.cols <= 4096) launch<T, 256, 2>(p, s);
-  else if (p.cols <= 8192) launch<T, 512, 2>(p, s);
-  else if (p.cols <= 16384) launch<T, 1024, 2>(p, s);
-  else launch<T, 1024, 8>(p, s);
+  static_assert(RowMap<1024, 8>::most == ROW_MOST, "the last shape takes every row");
+  launch<T, 64, 1>(p, s) || launch<T, 64, 2>(p, s) || launch<T, 256, 1>(p, s) || (p.post == F8_NORM_NONE && launch<T, 512, 1>(p, s)) ||
+      launch<T, 256, 2>(p, s) || launch<T, 512, 2>(p, s) || launch<T, 1024, 2>(p, s) || launch<T, 1024, 8>(p, s);
   return launch_status();
 }
-
 
 bool norm_form(int f) { return f == F8_NORM_NONE || f == F8_NORM_RMS || f == F8_NORM_LAYER; }
 

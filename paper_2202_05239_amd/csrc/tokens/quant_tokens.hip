@@ -85,10 +85,13 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void quant_tokens_kernel(Qua
   }
 }
 
+// (false where the threads' pieces do not cover a row)
 template <typename T, int TPR, int NV>
-void launch(const QuantParams &p, hipStream_t s) {
+bool launch(const QuantParams &p, hipStream_t s) {
+  if (p.pad > RowMap<TPR, NV>::most) return false;
   constexpr int THREADS = TPR == 64 ? 256 : TPR, RPB = THREADS / TPR;
   hipLaunchKernelGGL((quant_tokens_kernel<T, TPR, NV>), block_grid(((int64_t)p.rows + RPB - 1) / RPB), dim3(THREADS), 0, s, p);
+  return true;
 }
 
 // Threads to a row: as many as leave each one or two pieces, up to 1024 (16384 gated columns, 8192 rows, us: 1024 threads of two pieces
@@ -99,17 +102,11 @@ void launch(const QuantParams &p, hipStream_t s) {
 // (16384 x 6144 91.6 | 90.6, gated 176 | 165).
 template <typename T>
 f8_status launch_row(const QuantParams &p, hipStream_t s) {
-  if (p.pad <= 512) launch<T, 64, 1>(p, s);
-  else if (p.pad <= 1024) launch<T, 64, 2>(p, s);
-  else if (p.pad <= 2048) launch<T, 256, 1>(p, s);
-  else if (p.pad <= 4096) launch<T, 256, 2>(p, s);
-  else if (p.pad <= 6144 && p.rows >= 512) launch<T, 256, 3>(p, s);
-  else if (p.pad <= 8192) launch<T, 512, 2>(p, s);
-  else if (p.pad <= 16384) launch<T, 1024, 2>(p, s);
-  else launch<T, 1024, 8>(p, s);
+  static_assert(RowMap<1024, 8>::most == ROW_MOST, "the last shape takes every row");
+  launch<T, 64, 1>(p, s) || launch<T, 64, 2>(p, s) || launch<T, 256, 1>(p, s) || launch<T, 256, 2>(p, s) || (p.rows >= 512 && launch<T, 256, 3>(p, s)) ||
+      launch<T, 512, 2>(p, s) || launch<T, 1024, 2>(p, s) || launch<T, 1024, 8>(p, s);
   return launch_status();
 }
-
 
 f8_status enqueue(const QuantParams &p, int x_type, hipStream_t s) {
   return x_type == F8_F32 ? launch_row<float>(p, s) : x_type == F8_F16 ? launch_row<f16>(p, s) : launch_row<bf16>(p, s);
