@@ -27,10 +27,10 @@
 // the largest weight, and what lies below is off by 2^-40 of it at most, 2^-23 of it over 131072 tokens
 // (in two parts 2^-39 above that line: a rest is never 0).  Scores, maxima, sums and outputs are 32 bits.
 //
-// Bound by HBM: every cached byte is read once, in whole rows, one tile ahead per wave (131072 tokens of 8 heads, 277 MB: 67 us with
-// the second launch, 4.2 TB/s; 64 requests of up to 8192 tokens, 491 MB: 113 us, 4.35 TB/s; a large copy reaches 5.5).  The vector units
-// are a third busy (350 instructions a tile, most of them codes into f16).  Without the tile ahead the two took 97 and 239 us; with
-// the requests' lengths cut into equal stretches, a workgroup each, instead of units dealt out evenly, 68 and 167.
+// Bound by HBM: every cached byte is read once, in whole rows, one tile ahead per wave (131072 tokens of 8 heads, 277 MB: 58 us, 4.8 TB/s, and
+// 7 of the second launch; 64 requests of up to 8192 tokens, 491 MB: 103 us, 4.75 TB/s, and 8; a large copy reaches 5.5).  The vector units
+// are a third busy (350 instructions a tile, most of them codes into f16).  Without the tile ahead the two took 97 and 239 us with their
+// second launch; with the requests' lengths cut into equal stretches, a workgroup each, instead of units dealt out evenly, 68 and 167.
 #include <math.h>
 
 #include "tokens_device.h"

@@ -11,10 +11,10 @@
 // registers by then, so the buffer is free for the loads of the step after next, and the first fragments of the next step arrive
 // behind the second half of the slice.
 //
-// Bound by the power that matrix instructions on real operands take: 8192 x 8192 x 8192 takes 460-475 us (2.35 Pop/s; a loop of
-// nothing but matrix instructions on random bytes reaches 3.49), the matrix pipes are busy 72 % of the time at a clock that has come
-// down to 1.6 GHz.  What only removes stalls lowers the clock in step and leaves the time as it is, measured: reads that
-// collide two ways in LDS (half of all LDS cycles) or none; four waves with 128 x 128 outputs each and two thirds of the reads (467 us);
+// 8192 x 8192 x 8192 takes 449 - 478 us (2.3 - 2.45 Pop/s; a loop of nothing but matrix instructions on random bytes reaches 3.4 - 3.5).
+// The matrix pipes are 61 - 64 % busy at 1.5 - 1.85 GHz: the clock is what power leaves (the loop holds 1.78 GHz on random bytes, its pipes 90 %
+// busy, and 2.3 on zeros), the rest are stalls.  What was tried against those left the time as it is (468 us then): reads that
+// collide two ways in LDS (half of all LDS cycles) or none; four waves with 128 x 128 outputs each and two thirds of the reads (467);
 // the loads of a step spread over the slices instead of one burst (469); workgroups that stay and fetch the next tile's operands
 // before they store the last one's results (468).
 #include <math.h>

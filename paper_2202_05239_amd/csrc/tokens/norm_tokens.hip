@@ -7,7 +7,7 @@
 // y in the type of a, or as 8-bit tokens (tokens_device.h) for the product behind.  r is rounded where it is stored; y comes
 // from the 32-bit one.  Bound by HBM: a row is held in registers in 32 bits from its first load to its last store, the sums run
 // over the workgroup in a fixed order, and the variance of a layer norm is that of the centred row, not a difference of moments.
-// 16384 x 4096 bf16 with norms on both sides and a gate, 537 MB: 100 us, 5.35 TB/s, what a copy reaches; 64 x 4096 3.2 us, a row's chain
+// 16384 x 4096 bf16 with norms on both sides and a gate, 537 MB: 100 - 106 us, 5.1 - 5.4 TB/s (a copy 5.5); 64 x 4096 4.6 us, a row's chain
 // of loads and one or two reductions.
 #include "tokens_device.h"
 #include "tokens_host.h"

@@ -4,7 +4,7 @@
 //   result: the codes and scales, or the values code * scale that they stand for, in the type of x.
 //
 // Bound by HBM: every element is read once, its row stays in registers between the maximum and the codes, and is written once (8192 x
-// 16384 bf16 with a silu gate, 805 MB: 140 us, 5.7 TB/s).  Few rows are one chain of load, maximum and store: 33 x 1111 3.0 us.
+// 16384 bf16 with a silu gate, 805 MB: 140 us, 5.7 TB/s).  Few rows are one chain of load, maximum and store: 33 x 1111 3.8 us.
 #include <math.h>
 
 #include "tokens_device.h"
