@@ -48,6 +48,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p) {
     for (int d = LANES / 2; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
     const TokenScale s = token_scale(__uint_as_float(top));
     if (!there) return;
+    lift(v, s);
     if (l == 0) p.scale[kv][page * p.spage + place * p.stoken + head * p.shead] = s.scale;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {

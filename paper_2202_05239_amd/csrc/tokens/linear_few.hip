@@ -87,6 +87,7 @@ __global__ __launch_bounds__(THREADS) void linear_few_kernel(LinearParams p) {
       const int r = task / stretches, k = (task - r * stretches) * 512 + lane * 8;
       const TokenScale s = token_scale(__uint_as_float(tops[r]));
       if (k == 0) scales[r] = s.scale;
+      lift(v[h], s);
       int q[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) q[j] = code_of(v[h][j], s);

@@ -123,6 +123,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void norm_tokens_kernel(Norm
     for (int j = 0; j < 8; ++j) top = max(top, Map::col(i, j, t) < p.cols ? magnitude(v[i][j]) : 0u);
   const TokenScale s = token_scale(row_amax<TPR>(top, lds + 4 * W));
   if (t == 0) p.scale[row] = s.scale;
+  lift(v, s);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     int q[8];

@@ -64,6 +64,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void quant_tokens_kernel(Qua
     for (int j = 0; j < 8; ++j) top = max(top, magnitude(v[i][j]));
   const TokenScale s = token_scale(row_amax<TPR>(top, lds));
   if (t == 0 && p.scale) p.scale[row] = s.scale;
+  lift(v, s);
   if (p.codes) {
     int8_t *y = static_cast<int8_t *>(p.y) + row * p.ldy;
 #pragma unroll

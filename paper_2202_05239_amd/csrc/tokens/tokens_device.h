@@ -132,19 +132,35 @@ __device__ __forceinline__ float row_amax(uint32_t bits, float *lds) {
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
 struct TokenScale {
-  float scale, inv;
+  float scale, by, inv;                   // `by`: the scale that elements are divided by (see lift), inv: its reciprocal
   uint32_t real;                          // all bits set where the scale is finite, else 0
 };
+// Rows below about 2^-93 are divided as 2^64 times themselves: the remainder in over_scale would leave the normal range.
+constexpr float SMALL_SCALE = 0x1p-100f, LIFT = 0x1p64f;
 __device__ __forceinline__ TokenScale token_scale(float amax) {
   float s = amax / 127.0f;
   s = s < 1.17549435e-38f ? 1.17549435e-38f : s;   // (false for a NaN, which stays)
-  return TokenScale{s, 1.0f / s, s < __builtin_inff() ? 0xffffffffu : 0u};
+  const float by = s < SMALL_SCALE ? s * LIFT : s;
+  return TokenScale{s, by, 1.0f / by, s < __builtin_inff() ? 0xffffffffu : 0u};
 }
-// v / scale, correctly rounded without a division for each element: the product with the reciprocal, corrected by its exact
+__device__ __forceinline__ void lift(float (&v)[8], const TokenScale &s) {
+  if (s.scale < SMALL_SCALE) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= LIFT;
+  }
+}
+template <int NV>
+__device__ __forceinline__ void lift(float (&v)[NV][8], const TokenScale &s) {
+  if (s.scale < SMALL_SCALE) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) lift(v[i], s);
+  }
+}
+// A lifted v over its scale, correctly rounded without a division for each element: the product with the reciprocal, corrected by its exact
 // remainder.  (One operation off in the last place would turn codes at ties.)
 __device__ __forceinline__ float over_scale(float v, const TokenScale &s) {
   const float q = v * s.inv;
-  return __builtin_fmaf(__builtin_fmaf(-q, s.scale, v), s.inv, q);
+  return __builtin_fmaf(__builtin_fmaf(-q, s.by, v), s.inv, q);
 }
 // The code in the low byte: at 1.5 * 2^23 the unit of the sum is 1, so the addition rounds half to even and leaves the integer in
 // the low bits.  Codes of a row whose scale is not finite are 0.

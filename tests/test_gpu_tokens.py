@@ -90,6 +90,33 @@ def test_ties_and_extreme_scales():
     assert scale.item() == TINY and torch.equal(codes.cpu().float(), torch.round(small.double() / TINY).float())
 
 
+def test_ties_of_the_smallest_rows():
+    # quotients whose remainder lies below the normal range: ties and their neighbours, scales from 2^-126 to 2^-90
+    g = gen(21)
+    amax = (127 * torch.exp2(-126 + 36 * torch.rand(300, 1, generator=g)) * (1 + torch.rand(300, 1, generator=g))).float()
+    s = torch.clamp(amax / torch.tensor(127.0), min=TINY)
+    ties = (torch.arange(126) + 0.5) * s
+    rows = torch.cat([amax, ties, torch.nextafter(ties, torch.tensor(math.inf)), -torch.nextafter(ties, torch.tensor(0.0))], 1)
+    want, s = quant_ref(rows)
+    codes, scale = f8.f8_quant_tokens(rows.to(DEV))
+    assert torch.equal(codes.cpu().float(), want) and torch.equal(scale.cpu(), s[:, 0])
+    values, _ = f8.f8_quant_tokens(rows.to(DEV), values=True)
+    assert torch.equal(values.cpu(), want * s)
+    # the same rows through the product, the norm without a norm, and the cache
+    w, sw = torch.eye(379, dtype=torch.int8, device=DEV), torch.ones(379, device=DEV)
+    for n in (1, 16, 300):
+        y = f8.f8_linear_tokens(rows[:n].to(DEV), w, sw)
+        assert torch.equal(y.cpu(), (want * s)[:n])
+    _, codes, scale = f8.f8_norm_tokens(rows.to(DEV), pre=None, codes=True)
+    assert torch.equal(codes.cpu().float(), want) and torch.equal(scale.cpu(), s[:, 0])
+    heads = torch.cat([rows[:, :1], rows[:, 127:254], rows[:, 254:]], 1)[:, :240].reshape(300, 1, 240).contiguous()
+    want, s = quant_ref(heads[:, 0])
+    cache, scales = torch.zeros(2, 300, 1, 1, 240, dtype=torch.int8, device=DEV), torch.zeros(2, 300, 1, 1, device=DEV)
+    f8.f8_kv_append(heads.to(DEV), -heads.to(DEV), torch.arange(300, device=DEV), cache[0], cache[1], scales[0], scales[1])
+    for i, sign in ((0, 1), (1, -1)):
+        assert torch.equal(cache[i, :, 0, 0].cpu().float(), sign * want) and torch.equal(scales[i, :, 0, 0].cpu(), s[:, 0])
+
+
 def test_rows_that_are_not_finite_show_it():
     x = torch.randn(4, 300, generator=gen(1))
     x[0, 17], x[1, 299], x[2, 0] = float("nan"), float("inf"), -float("inf")
