@@ -450,7 +450,8 @@ f8_status f8_kv_append(const void *k, const void *v, const int64_t *slots, void 
  *     out = sum_t softmax_t(scale * q . k_t) v_t   over t < lens[b].
  * Token t of request b lies in page table[b * table_ld + t / page_size], place t % page_size.  lens are clamped to 0 .. max_len,
  * which the caller bounds ahead of the launch (max_len <= table_cols * page_size; 0 needs no table); a request without tokens gives zeros.  A table
- * entry outside 0 .. pages - 1 takes its tokens out of the sums.  k_cache, v_cache and their strides are multiples of 16 bytes.
+ * entry outside 0 .. pages - 1 takes its tokens out of the sums.  Values of an 8-bit cache lose bits where all scales that matter to a
+ * request lie below 2^-109.  k_cache, v_cache and their strides are multiples of 16 bytes.
  * Workspace: f8_attend_workspace_bytes(batch, q_heads, heads, dim, max_len) bytes, which may be 0 (then it may be NULL). */
 typedef struct {
   int32_t batch, q_heads, type;
