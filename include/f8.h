@@ -465,6 +465,80 @@ f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cach
                           const int32_t *table, const int32_t *lens, void *out, const f8_kv_layout *c, const f8_attend_desc *d,
                           void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- several continuations of one prompt: beams, and requests that begin alike ----
+ *
+ * Requests may share pages: table rows name the same page, and refs[page] counts the rows that hold it (and whatever else of the
+ * caller's does).  A page is free where its count is not positive.  The calls below keep tables and counts on the device and read them there;
+ * they are functions of their inputs (outputs do not overlap inputs unless said otherwise), so a captured step runs on two sets of them in turn. */
+
+/* f8_attend_paged for requests that begin alike: requests first[g] .. first[g + 1] - 1 (first [groups + 1], ascending; requests in no
+ * group are their own) have their first shared[g] tokens in common, which are read once for all of them.  The result is f8_attend_paged's
+ * of the same arguments but for rounding, wherever the pages that the members' rows list hold the same first shared[g] tokens, in one page or in copies: they are read through the
+ * first member that has all of them (a shorter one reads its own).  first and shared are read on the device; weights of
+ * 16-bit caches are rounded once to the cache's type.  Workspace: f8_attend_shared_workspace_bytes(batch, groups, q_heads, heads, dim, max_len) bytes. */
+size_t f8_attend_shared_workspace_bytes(int batch, int groups, int q_heads, int kv_heads, int dim, int max_len);
+f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cache, const float *k_scale, const float *v_scale,
+                           const int32_t *table, const int32_t *lens, const int32_t *first, const int32_t *shared, void *out,
+                           const f8_kv_layout *c, const f8_attend_desc *d, int groups, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Beam search's selection.  With logits [batch][beams][vocab] (`type` real, rows ld elements apart, beam i of prompt b is row b * beams + i), the beams'
+ * scores [batch][beams] and done [batch][beams] (0 or not; NULL: none is),
+ *     S[b][i][t] = scores[b][i] + logits[b][i][t] - log sum_u exp logits[b][i][u],
+ * of a beam that is done scores[b][i] for t = eos and -infinity for every other t.  The `keep` largest S of each prompt, in
+ * descending order and ties in that of (i, t), come as score [batch][keep] (32 bits; formed and compared in 64), parent [batch][keep] = b * beams + i
+ * and token [batch][keep].  A beam whose logits are all -infinity has S of -infinity; one with a NaN or +infinity among its
+ * logits or as its score has S of NaN throughout, which stands above every number.  Logits of a beam that is done are not read.
+ * 1 <= keep <= F8_BEAM_MAX_KEEP, keep <= beams * vocab, beams * keep * ceil(vocab / 16384) <= 8192 and beams <= 1024 (else F8_ERR_UNSUPPORTED).
+ * Workspace: f8_beam_workspace_bytes(batch, beams, vocab, keep) bytes. */
+#define F8_BEAM_MAX_KEEP 64
+typedef struct {
+  int32_t batch, beams, vocab, keep;
+  int32_t type, eos;
+  int64_t ld;                        /* elements */
+} f8_beam_desc;
+size_t f8_beam_workspace_bytes(int batch, int beams, int vocab, int keep);
+f8_status f8_beam_step(const void *logits, const float *scores, const uint8_t *done, float *score, int32_t *parent, int32_t *token,
+                       const f8_beam_desc *d, void *workspace, size_t workspace_bytes, void *stream);
+
+/* One step of the requests that share a cache: request b goes on from request parent[b] (outside 0 .. batch - 1: it ends) by `grow` tokens.
+ * table [batch][cols], lens and refs [pages] are those before the step, table_out, lens_out and refs_out those after it:
+ *   - a request holds the pages of its parent, ceil(lens / page_size) entries of the table's row (entries outside 0 .. pages - 1 are
+ *     carried along and hold nothing); pages that nobody holds any more are free from then on, for this step too;
+ *   - a page that is not full, that requests will write into (grow > 0), stays with the lowest of them if they are all that hold it; for the others it is
+ *     copied: into a new page, with a line of moves;
+ *   - new pages for these copies and for the tokens that find no room are the free ones of the lowest index, request by request, the copy's first.
+ * Row b of table_out holds the pages and then -1.  slots [batch][grow] say where f8_kv_append puts the new tokens (-1: nowhere), moves [batch][3] what
+ * f8_kv_copy has to copy before: (page, new page, tokens), behind the last one (-1, -1, 0).  info[0]: number of moves; info[1]: pages that were wanted
+ * and not there, in the pool or as columns of the table.  Entries of these are -1 (of a copy: its tokens are lost), lens_out counts their tokens up to cols *
+ * page_size all the same.  Workspace: f8_kv_fork_workspace_bytes(batch, pages) bytes. */
+typedef struct {
+  int32_t batch, cols, pages, page_size, grow;
+  int64_t table_ld, out_ld;          /* entries */
+} f8_kv_fork_desc;
+size_t f8_kv_fork_workspace_bytes(int batch, int pages);
+f8_status f8_kv_fork(const int32_t *parent, const int32_t *table, const int32_t *lens, const int32_t *refs, int32_t *table_out,
+                     int32_t *lens_out, int32_t *refs_out, int64_t *slots, int32_t *moves, int32_t *info, const f8_kv_fork_desc *d,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* Moves the pages in use to the front of the pool: with U pages in use, the ones at U and beyond go, in ascending order, to the free ones below U.
+ * table [rows][cols] (table_out may be it) and refs [pages] (refs_out may not) are rewritten, entries that name no page in use stay.
+ * moves [pages / 2][3] lists (page, new page, page_size) for f8_kv_copy, behind the last one (-1, -1, 0); info[0]: number of moves, info[1]: U.
+ * Workspace: f8_kv_compact_workspace_bytes(pages) bytes. */
+typedef struct {
+  int32_t rows, cols, pages, page_size;
+  int64_t table_ld, out_ld;          /* entries */
+} f8_kv_compact_desc;
+size_t f8_kv_compact_workspace_bytes(int pages);
+f8_status f8_kv_compact(const int32_t *table, const int32_t *refs, int32_t *table_out, int32_t *refs_out, int32_t *moves, int32_t *info,
+                        const f8_kv_compact_desc *d, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Copies pages of a cache (of one layer: a cache per layer takes a call each, with the same list): for each of the n lines (src, dst, tokens) of moves,
+ * the first `tokens` places of page src into page dst, keys and values, of 8-bit caches their scales too; other places stay as they are.
+ * Lines with a page outside the cache are skipped.  count (device, may be NULL): lines from *count on are not looked at.  No page may be dst
+ * twice, or dst and src. */
+f8_status f8_kv_copy(const int32_t *moves, const int32_t *count, void *k_cache, void *v_cache, float *k_scale, float *v_scale,
+                     const f8_kv_layout *c, int n, void *stream);
+
 /* ---- helpers (host side, set-up only) ---- */
 
 /* A PACT clipping level alpha (Eq. 3) expressed in output LSBs for fractional length

@@ -31,6 +31,8 @@ EXPORTS = [
     "f8_tensor_stats_f32", "f8_quant_error_f32", "f8_fold_work_doubles", "f8_fold_conv_bn",
     "f8_quant_tokens", "f8_norm_tokens", "f8_linear_scaled", "f8_linear_workspace_bytes", "f8_linear_tokens",
     "f8_kv_append", "f8_attend_workspace_bytes", "f8_attend_paged",
+    "f8_beam_workspace_bytes", "f8_beam_step", "f8_kv_fork_workspace_bytes", "f8_kv_fork", "f8_kv_compact_workspace_bytes", "f8_kv_compact", "f8_kv_copy",
+    "f8_attend_shared_workspace_bytes", "f8_attend_shared",
 ]
 F8_STATS_WORK_DOUBLES = 4096
 
@@ -110,6 +112,18 @@ class f8_attend_desc(ctypes.Structure):
                 ("table_ld", _i64), ("q_token", _i64), ("q_head", _i64), ("o_token", _i64), ("o_head", _i64)]
 
 
+class f8_beam_desc(ctypes.Structure):
+    _fields_ = [("batch", _i32), ("beams", _i32), ("vocab", _i32), ("keep", _i32), ("type", _i32), ("eos", _i32), ("ld", _i64)]
+
+
+class f8_kv_fork_desc(ctypes.Structure):
+    _fields_ = [("batch", _i32), ("cols", _i32), ("pages", _i32), ("page_size", _i32), ("grow", _i32), ("table_ld", _i64), ("out_ld", _i64)]
+
+
+class f8_kv_compact_desc(ctypes.Structure):
+    _fields_ = [("rows", _i32), ("cols", _i32), ("pages", _i32), ("page_size", _i32), ("table_ld", _i64), ("out_ld", _i64)]
+
+
 _lib = None
 
 
@@ -179,6 +193,19 @@ def lib():
     L.f8_attend_workspace_bytes.argtypes = [i32] * 5
     L.f8_attend_workspace_bytes.restype = sz
     L.f8_attend_paged.argtypes = [vp] * 8 + [P(f8_kv_layout), P(f8_attend_desc), vp, sz, vp]
+    L.f8_beam_workspace_bytes.argtypes = [i32] * 4
+    L.f8_beam_workspace_bytes.restype = sz
+    L.f8_beam_step.argtypes = [vp] * 6 + [P(f8_beam_desc), vp, sz, vp]
+    L.f8_kv_fork_workspace_bytes.argtypes = [i32, i32]
+    L.f8_kv_fork_workspace_bytes.restype = sz
+    L.f8_kv_fork.argtypes = [vp] * 10 + [P(f8_kv_fork_desc), vp, sz, vp]
+    L.f8_kv_compact_workspace_bytes.argtypes = [i32]
+    L.f8_kv_compact_workspace_bytes.restype = sz
+    L.f8_kv_compact.argtypes = [vp] * 6 + [P(f8_kv_compact_desc), vp, sz, vp]
+    L.f8_kv_copy.argtypes = [vp] * 6 + [P(f8_kv_layout), i32, vp]
+    L.f8_attend_shared_workspace_bytes.argtypes = [i32] * 6
+    L.f8_attend_shared_workspace_bytes.restype = sz
+    L.f8_attend_shared.argtypes = [vp] * 10 + [P(f8_kv_layout), P(f8_attend_desc), i32, vp, sz, vp]
     L.f8_mfma_i8_yardstick.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double), vp]
     L.f8_mfma_i8_yardstick_operands.argtypes = [vp, i32, ctypes.c_uint32, ctypes.POINTER(ctypes.c_double), vp]
     L.f8_tuning_set.argtypes = [ctypes.c_char_p, i32]
@@ -650,9 +677,7 @@ def f8_kv_append(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None):
         raise F8Error(rc, "f8_kv_append")
 
 
-def f8_attend_paged(q, k_cache, v_cache, table, lens, k_scale=None, v_scale=None, scale=None, max_len=None, out=None, workspace=None):
-    """One new token per request, q [batch][q_heads][dim], over its lens[b] cached tokens, whose pages table [batch][cols] lists.
-    scale: of the scores (1 / sqrt(dim)); max_len: no request is longer (as long as the table allows)."""
+def _attend_desc(q, k_cache, v_cache, k_scale, v_scale, table, scale, max_len, out):
     c = _kv_layout(k_cache, v_cache, k_scale, v_scale)
     _no_gradient(q, k_cache, v_cache)
     shape, qs = q.shape, q.stride()
@@ -673,14 +698,122 @@ def f8_attend_paged(q, k_cache, v_cache, table, lens, k_scale=None, v_scale=None
             raise ValueError("out overlaps itself: shape %s, strides %s" % (tuple(shape), os))
     if max_len is None:
         max_len = min(cols * c.page_size, 0x7fff0000)
+    return c, f8_attend_desc(B, H, _real(q), max_len, cols, D ** -0.5 if scale is None else scale, _matrix(table), qs[0], qs[1], os[0], os[1]), B, out
+
+
+def f8_attend_paged(q, k_cache, v_cache, table, lens, k_scale=None, v_scale=None, scale=None, max_len=None, out=None, workspace=None):
+    """One new token per request, q [batch][q_heads][dim], over its lens[b] cached tokens, whose pages table [batch][cols] lists.
+    scale: of the scores (1 / sqrt(dim)); max_len: no request is longer (as long as the table allows)."""
+    c, d, B, out = _attend_desc(q, k_cache, v_cache, k_scale, v_scale, table, scale, max_len, out)
     L = _lib or lib()
-    at_ws, n, _keep = _scratch(workspace, L.f8_attend_workspace_bytes(B, H, c.heads, D, max_len), q.device)
-    d = f8_attend_desc(B, H, _real(q), max_len, cols, D ** -0.5 if scale is None else scale, _matrix(table), qs[0], qs[1], os[0], os[1])
+    at_ws, n, _keep = _scratch(workspace, L.f8_attend_workspace_bytes(B, d.q_heads, c.heads, c.dim, d.max_len), q.device)
     rc = L.f8_attend_paged(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), table.data_ptr(),
                            _vector(lens, B, torch.int32), out.data_ptr(), c, d, at_ws, n, _stream())
     if rc:
         raise F8Error(rc, "f8_attend_paged")
     return out
+
+
+def f8_attend_shared(q, k_cache, v_cache, table, lens, first, shared, k_scale=None, v_scale=None, scale=None, max_len=None, out=None,
+                     workspace=None):
+    """f8_attend_paged for groups of requests that begin alike: requests first[g] .. first[g + 1] - 1 have their first shared[g] tokens in
+    common, which are read once for all of them.  first [groups + 1] and shared [groups] are int32."""
+    c, d, B, out = _attend_desc(q, k_cache, v_cache, k_scale, v_scale, table, scale, max_len, out)
+    groups = shared.numel()
+    L = _lib or lib()
+    at_ws, n, _keep = _scratch(workspace, L.f8_attend_shared_workspace_bytes(B, groups, d.q_heads, c.heads, c.dim, d.max_len), q.device)
+    rc = L.f8_attend_shared(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), table.data_ptr(),
+                            _vector(lens, B, torch.int32), _vector(first, groups + 1, torch.int32), _vector(shared, groups, torch.int32), out.data_ptr(),
+                            c, d, groups, at_ws, n, _stream())
+    if rc:
+        raise F8Error(rc, "f8_attend_shared")
+    return out
+
+
+def f8_beam_step(logits, scores, keep=None, done=None, eos=0, out=None, workspace=None):
+    """The `keep` (as many as beams) best continuations of each prompt from logits [batch][beams][vocab] and the beams' float32 scores
+    [batch][beams]: (score, parent, token) [batch][keep], parent as the row b * beams + i that f8_kv_fork takes.  done (bool or uint8, like
+    scores): beams that go on with eos at the same score."""
+    kind, shape, st = _real(logits), logits.shape, logits.stride()
+    _no_gradient(logits, scores)
+    if len(shape) != 3 or (st[2] != 1 and shape[2] > 1):
+        raise ValueError("logits have to be [batch][beams][vocab], the last dimension contiguous")
+    B, K, V = shape
+    ld = st[1] if K > 1 else st[0] if B > 1 else V
+    if (B > 1 and st[0] != K * ld and K > 1) or (ld < V and B * K > 1):
+        raise ValueError("rows of logits have to lie at one distance, not overlapping: shape %s, strides %s" % (tuple(shape), st))
+    if done is not None and done.dtype not in (torch.bool, torch.uint8):
+        raise TypeError("done has to be bool or uint8")
+    keep = K if keep is None else int(keep)
+    if out is None:
+        out = tuple(torch.empty((B, keep), dtype=t, device=logits.device) for t in (torch.float32, torch.int32, torch.int32))
+    d = f8_beam_desc(B, K, V, keep, kind, eos, max(ld, V))
+    L = _lib or lib()
+    at_ws, n, _keep = _scratch(workspace, L.f8_beam_workspace_bytes(B, K, V, keep), logits.device)
+    rc = L.f8_beam_step(logits.data_ptr(), _vector(scores, B * K, torch.float32), _vector(done, B * K), _vector(out[0], B * keep, torch.float32),
+                        _vector(out[1], B * keep, torch.int32), _vector(out[2], B * keep, torch.int32), d, at_ws, n, _stream())
+    if rc:
+        raise F8Error(rc, "f8_beam_step")
+    return out
+
+
+def _int_matrix(t, what, shape=None):
+    if t.dtype != torch.int32:
+        raise TypeError("%s has to be int32" % what)
+    return _matrix(t, shape)
+
+
+def f8_kv_fork(parent, table, lens, refs, page_size, grow=1, out=None, workspace=None):
+    """Requests go on from their parents (-1: they end) by `grow` tokens each: (table, lens, refs, slots, moves, info) after that, from
+    table [batch][cols], lens [batch] and the holders refs [pages] of every page, all int32.  slots [batch][grow] (int64) is where
+    f8_kv_append puts the new tokens, moves [batch][3] what f8_kv_copy copies first; info: (moves, pages that were missing).  out: that
+    tuple's tensors, none of which may be an input."""
+    ld, (B, cols), dev = _int_matrix(table, "the table"), table.shape, table.device
+    pages, i32 = refs.numel(), torch.int32
+    if out is None:
+        new = lambda *s: torch.empty(s, dtype=i32, device=dev)  # noqa: E731
+        out = (new(B, cols), new(B), new(pages), torch.empty((B, grow), dtype=torch.int64, device=dev), new(B, 3), new(2))
+    d = f8_kv_fork_desc(B, cols, pages, page_size, grow, ld, _int_matrix(out[0], "the table", table.shape))
+    L = _lib or lib()
+    at_ws, n, _keep = _scratch(workspace, L.f8_kv_fork_workspace_bytes(B, pages), dev)
+    rc = L.f8_kv_fork(_vector(parent, B, i32), table.data_ptr(), _vector(lens, B, i32), _vector(refs, pages, i32), out[0].data_ptr(), _vector(out[1], B, i32),
+                      _vector(out[2], pages, i32), _vector(out[3], B * grow, torch.int64), _vector(out[4], 3 * B, i32), _vector(out[5], 2, i32), d, at_ws, n,
+                      _stream())
+    if rc:
+        raise F8Error(rc, "f8_kv_fork")
+    return out
+
+
+def f8_kv_compact(table, refs, page_size, out=None, workspace=None):
+    """Moves the pages in use to the front of the pool: (table, refs, moves, info) after that; moves [pages // 2][3] for f8_kv_copy, info:
+    (moves, pages in use).  out: that tuple's tensors; its table may be the input's."""
+    ld, (rows, cols), dev = _int_matrix(table, "the table"), table.shape, table.device
+    pages, i32 = refs.numel(), torch.int32
+    if out is None:
+        new = lambda *s: torch.empty(s, dtype=i32, device=dev)  # noqa: E731
+        out = (new(rows, cols), new(pages), new(pages // 2, 3), new(2))
+    d = f8_kv_compact_desc(rows, cols, pages, page_size, ld, _int_matrix(out[0], "the table", table.shape))
+    L = _lib or lib()
+    at_ws, n, _keep = _scratch(workspace, L.f8_kv_compact_workspace_bytes(pages), dev)
+    rc = L.f8_kv_compact(table.data_ptr(), _vector(refs, pages, i32), out[0].data_ptr(), _vector(out[1], pages, i32), _vector(out[2], pages // 2 * 3, i32),
+                         _vector(out[3], 2, i32), d, at_ws, n, _stream())
+    if rc:
+        raise F8Error(rc, "f8_kv_compact")
+    return out
+
+
+def f8_kv_copy(moves, k_cache, v_cache, k_scale=None, v_scale=None, info=None):
+    """Copies pages of a cache: for each line (src, dst, tokens) of moves, int32 [n][3], the first `tokens` places of page src into dst.  info:
+    the tensor that came with the moves, whose first element is the number of lines that count."""
+    c = _kv_layout(k_cache, v_cache, k_scale, v_scale)
+    if len(moves.shape) != 2 or moves.shape[1] != 3 or moves.dtype != torch.int32 or not moves.is_contiguous():
+        raise ValueError("moves has to be a contiguous int32 matrix [n][3]")
+    if info is not None and (info.dtype != torch.int32 or info.numel() < 1):
+        raise TypeError("info has to be int32")
+    rc = (_lib or lib()).f8_kv_copy(moves.data_ptr(), _ptr(info), k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scale), _ptr(v_scale), c, moves.shape[0],
+                                    _stream())
+    if rc:
+        raise F8Error(rc, "f8_kv_copy")
 
 
 def out_hw(H, W, R, S, stride, pad):
