@@ -19,6 +19,9 @@ FLAGS = [
     # keep the compiler from forming packed-fp32 instructions (none of this code needs them)
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
+# of single sources: attend_shared.hip rescales its accumulators with vector instructions now and then, and moves all of them between the two
+# halves of the register file around every matrix instruction if they live in the accumulation half (400 moves to a tile)
+MORE_FLAGS = {"attend_shared.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def sources():
@@ -44,7 +47,7 @@ def build(verbose: bool = False) -> str:
     objs = [os.path.join(OBJ_DIR, os.path.basename(s)[:-4] + ".o") for s in srcs]
     jobs = min(len(srcs), max(1, min(8, os.cpu_count() or 1)))
     with ThreadPoolExecutor(jobs) as pool:
-        list(pool.map(lambda so: _run([hipcc] + FLAGS + ["-c", so[0], "-o", so[1]], verbose), zip(srcs, objs)))
+        list(pool.map(lambda so: _run([hipcc] + FLAGS + MORE_FLAGS.get(os.path.basename(so[0]), []) + ["-c", so[0], "-o", so[1]], verbose), zip(srcs, objs)))
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs, verbose)
     return LIB
 

@@ -21,9 +21,6 @@ namespace {
 constexpr int WAVES = 4, TILE = 32, COLS = 16, UNIT = WAVES * TILE, THREADS = 64 * WAVES;
 constexpr int GROUPS_LDS = 1024;             // groups whose bounds a workgroup keeps in LDS
 constexpr int WGS = 256;
-// The maximum that weights are taken against follows the scores only where they pass it by more than this, as a power of two: the
-// lanes of a column then seldom have to agree on a new one.
-constexpr float SLACK = 4.0f;
 
 struct SharedParams {
   const void *q, *k, *v;
@@ -38,10 +35,13 @@ struct SharedParams {
   float scale;                               // of the scores, times log2 e
 };
 
-// How the work is dealt out.  An item is a group (its prefix) or a request (its own tokens).  A pair is an item, a cache head and a block
-// of up to `rows` query heads that read it; its units are rounds of a workgroup's waves over its tokens.  All units lie in a row, groups first, and
-// every workgroup takes an equal run of them.  A pair that lies in one run leaves its piece at its own place; one that is cut leaves a piece in each
-// run, at slot 1 of the run that it begins in and at slot 0 of the others.
+// How the work is dealt out, first the prefixes and then the requests' own tokens.
+// A pair of the first kind is a group, a cache head and a block of up to `rows` query heads that read it; its units are rounds of a workgroup's
+// four waves over the prefix.  All units lie in a row and every workgroup takes an equal run of them.  A pair of the second kind is a request, a cache
+// head and up to 16 of its query heads; its units are tiles, and every wave takes an equal run on its own: these pairs are many and
+// short, and a pair's way to its first rows is 4 us (a workgroup to such a pair: 64 requests of 700 tokens, 8 heads, 107 us).
+// A pair that lies in one run leaves its piece at its own place; one that is cut leaves a piece in each run, at slot 1 of the run that it begins in and at
+// slot 0 of the others.
 struct Prefix {
   int b0, n, tokens;                         // requests b0 .. b0 + n - 1
 };
@@ -69,22 +69,21 @@ struct Work {
     return n <= len(b) ? n : 0;
   }
   static __device__ __forceinline__ int units(int tokens) { return (tokens + UNIT - 1) / UNIT; }
+  static __device__ __forceinline__ int tiles(int tokens) { return (tokens + TILE - 1) / TILE; }
   __device__ __forceinline__ int blocks(int requests) const { return (requests + p.per_block - 1) / p.per_block * p.chunks; }
-  __device__ __forceinline__ int64_t units_of(int item) const {
-    if (item < p.groups) {
-      const Prefix x = prefix(item);
-      return x.tokens > 0 ? (int64_t)units(x.tokens) * p.heads * blocks(x.n) : 0;
-    }
-    const int b = item - p.groups;
-    return (int64_t)units(len(b) - prefix_of(b)) * p.heads * p.chunks;
+  __device__ __forceinline__ int own_chunks() const { return (p.group + COLS - 1) / COLS; }
+  __device__ __forceinline__ int64_t units_of(int g) const {
+    const Prefix x = prefix(g);
+    return x.tokens > 0 ? (int64_t)units(x.tokens) * p.heads * blocks(x.n) : 0;
   }
+  __device__ __forceinline__ int64_t tiles_of(int b) const { return (int64_t)tiles(len(b) - prefix_of(b)) * p.heads * own_chunks(); }
 };
-// Pieces: of pairs in one run [2][batch][query heads] (the prefix's part, the own part), then [workgroups][2][rows].
+// Pieces: of pairs in one run [2][batch][query heads] (the prefix's part, the own part), then [workgroups][2][rows] and [waves][2][COLS].
 __device__ __forceinline__ int64_t whole_at(const SharedParams &p, bool own, int b, int hq) {
   return ((int64_t)(own ? p.batch : 0) + b) * p.heads * p.group + hq;
 }
-__device__ __forceinline__ int64_t cut_at(const SharedParams &p, int64_t run, int slot, int row) {
-  return (int64_t)2 * p.batch * p.heads * p.group + (2 * run + slot) * p.rows + row;
+__device__ __forceinline__ int64_t cut_at(const SharedParams &p, bool own, int64_t run, int slot, int row) {
+  return (int64_t)2 * p.batch * p.heads * p.group + (own ? (int64_t)2 * p.wgs * p.rows + (2 * run + slot) * COLS : (2 * run + slot) * p.rows) + row;
 }
 
 __device__ __forceinline__ const int32_t *bounds(const SharedParams &p, int32_t *lds, int threads) {
@@ -94,54 +93,38 @@ __device__ __forceinline__ const int32_t *bounds(const SharedParams &p, int32_t 
   return lds;
 }
 
+// What a wave keeps in LDS of a tile: where its 32 rows begin, in elements, and (8-bit caches) the scales of its keys and values and the logarithms
+// of both, SMALL at least.
 struct TileRows {
   int64_t at[TILE];
-  float scale[3 * TILE];
+  float scale[4 * TILE];
 };
 
-// Powers of two: the weight of the largest score, which leaves room for SLACK above it.
+// The maximum that weights are taken against follows the scores only where they pass it by more than SLACK, as a power of two, and the largest
+// weight of a tile is at most 2^TOP: an accumulator is seldom touched by anything but products.  bf16 has the range of 32 bits.
+// f16 weights keep their relative error down to 2^-21 of the largest one, what lies below is off by 2^-32 of it at most.
 template <typename C>
-constexpr float up() { return Operand<C>::UP > SLACK ? Operand<C>::UP - SLACK : 0.0f; }
+struct Weights {
+  static constexpr float SLACK = 8.0f, TOP = 15.0f;
+  // what a weight has at least, so that it counts against an infinite value: f16's smallest number, 2^-31 of the largest weight
+  static constexpr float LEAST = sizeof(C) == 1 ? 0.0f : 0x1p-24f;
+};
+template <>
+struct Weights<bf16> {
+  static constexpr float SLACK = 40.0f, TOP = 0.0f, LEAST = 0.0f;
+};
 
-// What a weight has at least, so that it counts against an infinite value whatever its type holds: f16's smallest number, 2^-35 of the
-// largest weight.
-template <typename C>
-constexpr float floor_of() { return __is_same(C, f16) ? 0x1p-24f : 0.0f; }
+__device__ const v4i zeros[1] = {v4i{0, 0, 0, 0}};          // keys' dimensions beyond the head's
 
-template <typename C, typename Q, int DP, int NB>
-__global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams p) {
-  typedef Operand<C> Op;
-  typedef typename Op::t H;
-  typedef H t8 __attribute__((ext_vector_type(8)));
-  constexpr bool S8 = sizeof(C) == 1;
-  constexpr int E = DP / 16, VB = E * (int)sizeof(C);     // elements and bytes of a value row per lane
-  constexpr int KL = DP * (int)sizeof(C) / 64;            // 16-byte loads of a key row per lane
-  constexpr int KS = DP / 32;                             // products per block of 16 scores
-  __shared__ TileRows rows[WAVES][2];
-  __shared__ float part[WAVES][COLS][DP + 1], ml[WAVES][NB * COLS][2];
-  __shared__ int64_t scan[WAVES][2], before;
-  __shared__ int from, found[WAVES];
-  __shared__ int32_t first_lds[GROUPS_LDS + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
-  const Work work{p, bounds(p, first_lds, THREADS)};
-  // (runs that follow one another lie on one XCD: the blocks of a head meet in its L2)
-  const uint32_t run = xcd_remap(blockIdx.x, gridDim.x);
-  const int items = p.groups + p.batch;
-
-  // the item that holds the run's first unit
-  int64_t left, start, done = 0;
-  {
-    int64_t sum[2] = {0, 0};
-    for (int i = threadIdx.x; i < items; i += THREADS) sum[0] += work.units_of(i);
-    wg_sum<WAVES>(sum, scan);
-    const Runs runs(uniform64(sum[0]), p.wgs);
-    start = runs.start(run);
-    left = runs.start((int64_t)run + 1) - start;
-    if (left == 0) return;
-  }
-  for (int i0 = 0;; i0 += THREADS) {
+// The item (of n, of(i) units each) that unit `start` lies in, for each of R starts, all below the sum; from[r] and before[r] (in LDS) get it and the units
+// in front of it.
+template <int R, typename Of>
+__device__ __forceinline__ void find_items(int n, const int64_t (&starts)[R], Of of, int64_t (*scan)[2], int *from, int64_t *before) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t done = 0;
+  for (int i0 = 0; i0 < n; i0 += THREADS) {
     const int i = i0 + (int)threadIdx.x;
-    const int64_t mine = i < items ? work.units_of(i) : 0;
+    const int64_t mine = i < n ? of(i) : 0;
     int64_t upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -157,150 +140,148 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
       all += scan[w][0];
     }
     at += upto - mine;
-    if (mine > 0 && at <= start && start < at + mine) from = i, before = at;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (mine > 0 && at <= starts[r] && starts[r] < at + mine) from[r] = i, before[r] = at;
     __syncthreads();
     done += all;
-    if (start < done) break;
+    if (starts[R - 1] < done) break;
   }
-  int item = __builtin_amdgcn_readfirstlane(from);
-  left = uniform64(left);
-  int64_t in = uniform64(start - before);       // units of the item in front of this run
+}
 
-  for (bool more = true; more;) {
-    // the pair: requests b0 .. b0 + n - 1, `heads` query heads of cache head kvh from hq0 on, tokens t_begin .. t_end - 1 of row `leader` of the table
-    const bool own = item >= p.groups;
-    int b0, n, t_begin, t_end, leader, pairs;
-    if (own) {
-      b0 = item - p.groups, n = 1, t_begin = work.prefix_of(b0), t_end = work.len(b0), leader = b0, pairs = p.heads * p.chunks;
-    } else {
-      const Prefix x = work.prefix(item);
-      b0 = x.b0, n = x.n, t_begin = 0, t_end = x.tokens, leader = b0, pairs = p.heads * work.blocks(n);
-    }
-    b0 = __builtin_amdgcn_readfirstlane(b0), n = __builtin_amdgcn_readfirstlane(n), leader = b0;
-    t_begin = __builtin_amdgcn_readfirstlane(t_begin), t_end = __builtin_amdgcn_readfirstlane(t_end);
-    pairs = __builtin_amdgcn_readfirstlane(pairs);
-    if (!own && work.len(leader) < t_end) {
-      // (an empty place in front) the first member that has all of the prefix; without any nobody reads what comes out
-      int have = 0x7fffffff;
-      for (int i = b0 + (int)threadIdx.x; i < b0 + n && have == 0x7fffffff; i += THREADS)
-        if (work.len(i) >= t_end) have = i;
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) have = min(have, __shfl_xor(have, d));
-      if (lane == 0) found[wave] = have;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) have = min(have, found[w]);
-      __syncthreads();
-      leader = __builtin_amdgcn_readfirstlane(have);
-      if (leader == 0x7fffffff) leader = b0, t_end = 0;
-    }
-    const int units = work.units(own ? t_end - t_begin : work.prefix(item).tokens);
-    const int pair = __builtin_amdgcn_readfirstlane((int)(in / units));
-    int unit = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)pair * units));
-    const int blocks = pairs / p.heads, kvh = pair / blocks, block = pair - kvh * blocks;
-    const int chunk = block % p.chunks, req0 = block / p.chunks * p.per_block;
-    const int h0 = chunk * p.rows, heads = p.chunks > 1 ? min(p.rows, p.group - h0) : p.group;
-    const int real_rows = min(n - req0, p.per_block) * heads, nb_used = (real_rows + COLS - 1) / COLS;
-    const int last = (int)min((int64_t)units, unit + left), begin = t_begin + unit * UNIT, end = min(t_end, t_begin + last * UNIT);
-    const int32_t *table = p.table + leader * p.table_ld;
-    auto place = [&](int row, int &b, int &hq) {             // of a row of the block
-      const int r = p.chunks > 1 ? 0 : (int)p.by_group.div((uint32_t)row);
-      b = b0 + req0 + r, hq = kvh * p.group + h0 + row - r * heads;
-    };
+template <typename C, typename Q, int DP, int NB>
+__global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams p) {
+  typedef Operand<C> Op;
+  typedef Weights<C> Wt;
+  typedef typename Op::t H;
+  typedef H t8 __attribute__((ext_vector_type(8)));
+  constexpr bool S8 = sizeof(C) == 1;
+  constexpr int E = DP / 16, VB = E * (int)sizeof(C);     // elements and bytes of a value row per lane
+  constexpr int KL = DP * (int)sizeof(C) / 64;            // 16-byte loads of a key row per lane
+  constexpr int KS = DP / 32;                             // products per block of 16 scores
+  constexpr int BLOCKS = NB > WAVES ? NB : WAVES;
+  __shared__ TileRows rows[WAVES][2];
+  __shared__ float part[WAVES][COLS][DP + 1], ml[WAVES][NB * COLS][2];
+  __shared__ int64_t scan[WAVES][2], before[1 + WAVES];
+  __shared__ int from[1 + WAVES], found[WAVES];
+  __shared__ v4i q_lds[BLOCKS][KS][64];
+  __shared__ float q_scale_lds[BLOCKS][COLS];
+  __shared__ int32_t first_lds[GROUPS_LDS + 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
+  const Work work{p, bounds(p, first_lds, THREADS)};
 
-    // Q^T as the right operand: the lane's column, the dimensions that its loads of K bring
-    v4i q[NB][KS];
-    float q_scale[NB];
-    const bool negative = p.scale < 0;
+  // Units and tiles of all, and this workgroup's and its waves' runs of them
+  int64_t sum[2] = {0, 0};
+  for (int i = threadIdx.x; i < p.groups; i += THREADS) sum[0] += work.units_of(i);
+  for (int i = threadIdx.x; i < p.batch; i += THREADS) sum[1] += work.tiles_of(i);
+  wg_sum<WAVES>(sum, scan);
+  const Runs runs(uniform64(sum[0]), p.wgs), own_runs(uniform64(sum[1]), p.wgs * WAVES);
+  // (a wave's runs follow those of the same wave of the workgroups in front: with few tiles every workgroup has some)
+  const int64_t run = blockIdx.x, own_run = (int64_t)wave * p.wgs + blockIdx.x;
+  int64_t left = uniform64(runs.start(run + 1) - runs.start(run)), own_left = uniform64(own_runs.start(own_run + 1) - own_runs.start(own_run));
+  if (left > 0) {
+    const int64_t starts[1] = {runs.start(run)};
+    find_items<1>(p.groups, starts, [&](int i) { return work.units_of(i); }, scan, from, before);
+  }
+  {
+    int64_t starts[WAVES];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      q_scale[nb] = fabsf(p.scale);
-      if (nb >= nb_used) continue;
-      const int row = nb * COLS + c16;
-      int b, hq;
-      place(min(row, real_rows - 1), b, hq);
-      const Q *src = static_cast<const Q *>(p.q) + b * p.qt + hq * p.qh;
-      v4i raw[KS];
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int d = S8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
-        __builtin_memcpy(&raw[s], src + (d < p.dim ? d : 0), 16);
-      }
-      float f[KS][8];
-      uint32_t top = 0;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int d = S8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
-        unpack8<Q>(&raw[s], f[s]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          f[s][j] = row < real_rows && d < p.dim ? (negative ? -f[s][j] : f[s][j]) : 0.0f;
-          top = max(top, magnitude(f[s][j]));
-        }
-      }
-      if constexpr (S8) {
-        // a power of two brings the largest element of the row to [2^14, 2^15): f16 then holds what the 16-bit q had, elements
-        // 2^-28 below the largest excepted
-        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        const int ex = max((int)(top >> 23), 15);             // (the two factors are then normal numbers, for an infinity's exponent too)
-        q_scale[nb] *= __int_as_float((ex - 14) << 23);
-        const float inv = __int_as_float((268 - ex) << 23);
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[s][j] *= inv;
-      }
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        t8 o;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = (H)f[s][j];
-        q[nb][s] = __builtin_bit_cast(v4i, o);
-      }
-    }
+    for (int w = 0; w < WAVES; ++w) starts[w] = own_runs.start((int64_t)w * p.wgs + blockIdx.x);
+    find_items<WAVES>(p.batch, starts, [&](int i) { return work.tiles_of(i); }, scan, from + 1, before + 1);
+  }
 
-    v4f o[NB][E];
-    float m[NB], l[NB];
+  v4f o[NB][E];
+  float m[NB], l[NB], q_scale[NB];
+  auto clear = [&]() {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       m[nb] = -INFINITY, l[nb] = 0.0f;
 #pragma unroll
       for (int e = 0; e < E; ++e) o[nb][e] = v4f{0, 0, 0, 0};
     }
+  };
+  // 16 query heads as columns into block nb of LDS; `src`: of the lane's column, nullptr for none
+  auto put_queries = [&](int nb, const Q *src) {
+    const Q *from = src ? src : static_cast<const Q *>(p.q);
+    v4i raw[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = S8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
+      __builtin_memcpy(&raw[s], from + (d < p.dim ? d : 0), 16);
+    }
+    float f[KS][8], scale = fabsf(p.scale);
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = S8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
+      unpack8<Q>(&raw[s], f[s]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        f[s][j] = src && d < p.dim ? (p.scale < 0 ? -f[s][j] : f[s][j]) : 0.0f;
+        top = max(top, magnitude(f[s][j]));
+      }
+    }
+    if constexpr (S8) {
+      // a power of two brings the largest element of the row to [2^14, 2^15): f16 then holds what the 16-bit q had, elements
+      // 2^-28 below the largest excepted
+      top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+      const int ex = max((int)(top >> 23), 15);               // (the two factors are then normal numbers, for an infinity's exponent too)
+      scale *= __int_as_float((ex - 14) << 23);
+      const float inv = __int_as_float((268 - ex) << 23);
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[s][j] *= inv;
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      t8 o;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = (H)f[s][j];
+      q_lds[nb][s][lane] = __builtin_bit_cast(v4i, o);
+    }
+    // (never 0, which -infinity in a place that a mask leaves out must not meet)
+    if (g == 0) q_scale_lds[nb][c16] = fmaxf(scale, 1.17549435e-38f);
+  };
 
+  // The tiles at t0, t0 + step .. below `end` of a row of the table, for N blocks of columns from block q0 of LDS on (all of these the same for a
+  // wave).  No branch between a tile's products, and none over lanes: the compiler (ROCm 7.2) has put copies of what lives across the loop
+  // into the block behind such a branch before that block had all its lanes back.
+  auto walk = [&](auto blocks_used, const int32_t *table, int kvh, int t0, int step, int end, int q0) {
+    constexpr int N = decltype(blocks_used)::value;
+    if (t0 >= end) return;
     const C *const kbase = static_cast<const C *>(p.k) + kvh * p.head, *const vbase = static_cast<const C *>(p.v) + kvh * p.head;
     const int dv = c16 * E < p.dim ? c16 * E : 0;
+    const int64_t none = reinterpret_cast<const char *>(zeros) - reinterpret_cast<const char *>(kbase);
     // The rows of a tile in registers.  The next one's keys are loaded when this one's scores are there, its values when this one's have been summed
-    // up: every load has half a tile's time on its way and no register waits twice.
+    // up: every load has half a tile's time on its way and no register waits twice.  All loads are issued whether there is a next tile or not (a token that
+    // does not exist reads row 0 of the cache): behind a branch around a load nobody knows how many are on their way, and the wait is for all.
     Raw<16> k[2][KL];
     Raw<VB> v[8];
     float tile_scale;                         // lanes 0..31: of the key of token `lane`, 32..63: of the value of token `lane - 32`
     uint32_t there;                           // its tokens that exist
-    auto look_up = [&](int t0) {              // page of token lane % 32 of the tile at t0
-      const int tok = t0 + (lane & 31);
-      return tok < end ? table[p.page_size.div((uint32_t)tok)] : -1;
+    auto look_up = [&](int t0) {              // page of token lane % 32 of the tile at t0, where there is one
+      return table[p.page_size.div((uint32_t)min(t0 + (lane & 31), end - 1))];
     };
     auto locate = [&](int t0, int page, int64_t (&at_lds)[TILE]) {
       const uint32_t tok = (uint32_t)(t0 + (lane & 31)), place = tok - p.page_size.div(tok) * p.page_size.d;
-      const bool real = (uint32_t)page < (uint32_t)p.pages;
-      const int64_t at = real ? page * p.page + place * p.token : 0;
-      if (lane < 32) at_lds[lane] = at;
+      const bool real = (int)tok < end && (uint32_t)page < (uint32_t)p.pages;
+      // (selected, not branched to, and written by both halves of the wave: see below)
+      const int64_t pg = real ? page : 0, pl = real ? (int)place : 0;
+      at_lds[lane & 31] = pg * p.page + pl * p.token;
       lanes_meet();
-      if constexpr (S8) {
-        const float *src = lane < 32 ? p.k_scale : p.v_scale;
-        tile_scale = real ? src[page * p.spage + place * p.stoken + kvh * p.shead] : 1.0f;
-      }
+      if constexpr (S8) tile_scale = (lane < 32 ? p.k_scale : p.v_scale)[pg * p.spage + pl * p.stoken + kvh * p.shead];
       return (uint32_t)__ballot(real);
     };
     auto load_keys = [&](const int64_t (&at_lds)[TILE]) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const C *row = kbase + at_lds[16 * h + c16];
+        const int64_t row = at_lds[16 * h + c16] * (int64_t)sizeof(C);
 #pragma unroll
         for (int i = 0; i < KL; ++i) {
           const int d = (i * 4 + g) * (16 / (int)sizeof(C));
-          k[h][i] = load_raw<16>(row + (d < p.dim ? d : 0));
+          k[h][i] = load_raw<16>(reinterpret_cast<const char *>(kbase) + (d < p.dim ? row + d * (int)sizeof(C) : none));
         }
       }
     };
@@ -311,29 +292,25 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
         for (int j = 0; j < 4; ++j) v[4 * h + j] = load_raw<VB>(vbase + at_lds[16 * h + 4 * g + j] + dv);
     };
 
-    // All tiles of this wave, for N blocks of columns: no branch between a tile's products
-    auto walk = [&](auto blocks_used) {
-      constexpr int N = decltype(blocks_used)::value;
-      int t0 = begin + wave * TILE, buf = 0;
-      if (t0 >= end) return;
+      int buf = 0;
       there = locate(t0, look_up(t0), rows[wave][0].at);
       load_keys(rows[wave][0].at);
+      int page = look_up(t0 + step);          // (in the order of the loop below)
       load_values(rows[wave][0].at);
-      int page = look_up(t0 + UNIT);
       for (;;) {
-        const bool next = t0 + UNIT < end;
         const uint32_t now = there;
         v4f ks[2], vs[2], vl[2];
         if constexpr (S8) {
           float *const scale_lds = rows[wave][buf].scale;
-          scale_lds[lane] = tile_scale;
-          if (lane >= 32) scale_lds[32 + lane] = fmaxf(__log2f(tile_scale), SMALL);
+          const float scale = now >> (lane & 31) & 1 ? tile_scale : 1.0f;
+          scale_lds[lane] = scale;
+          scale_lds[64 + lane] = fmaxf(__log2f(scale), SMALL);
           lanes_meet();
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             ks[h] = *reinterpret_cast<const v4f *>(scale_lds + 16 * h + 4 * g);
             vs[h] = *reinterpret_cast<const v4f *>(scale_lds + 32 + 16 * h + 4 * g);
-            vl[h] = *reinterpret_cast<const v4f *>(scale_lds + 64 + 16 * h + 4 * g);
+            vl[h] = *reinterpret_cast<const v4f *>(scale_lds + 96 + 16 * h + 4 * g);
           }
         }
         v4f acc[N][2];
@@ -343,10 +320,7 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < KL; ++i) {
-            const bool real = (i * 4 + g) * (16 / (int)sizeof(C)) < p.dim;
-            uint32_t d[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) d[j] = real ? k[h][i].d[j] : 0u;
+            const uint32_t(&d)[4] = k[h][i].d;
             if constexpr (S8) {
               h8 lo, hi;
 #pragma unroll
@@ -357,26 +331,17 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
                 to[4 * (j & 1)] = a[0], to[4 * (j & 1) + 1] = a[1], to[4 * (j & 1) + 2] = e[0], to[4 * (j & 1) + 3] = e[1];
               }
 #pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, lo), q[nb][2 * i], acc[nb][h]);
+              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, lo), q_lds[q0 + nb][2 * i][lane], acc[nb][h]);
 #pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, hi), q[nb][2 * i + 1], acc[nb][h]);
+              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, hi), q_lds[q0 + nb][2 * i + 1][lane], acc[nb][h]);
             } else {
 #pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(v4i{(int)d[0], (int)d[1], (int)d[2], (int)d[3]}, q[nb][i], acc[nb][h]);
+              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(v4i{(int)d[0], (int)d[1], (int)d[2], (int)d[3]}, q_lds[q0 + nb][i][lane], acc[nb][h]);
             }
           }
-        if (next) {
-          const int ahead = look_up(t0 + 2 * UNIT);
-          there = locate(t0 + UNIT, page, rows[wave][buf ^ 1].at);
-          load_keys(rows[wave][buf ^ 1].at);
-          page = ahead;
-        }
-#pragma unroll
-        for (int nb = 0; nb < N; ++nb)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[nb][h][j] *= S8 ? q_scale[nb] * ks[h][j] : q_scale[nb];
+        there = locate(t0 + step, page, rows[wave][buf ^ 1].at);
+        load_keys(rows[wave][buf ^ 1].at);
+        page = look_up(t0 + 2 * step);
         if (now != 0xffffffffu) {
 #pragma unroll
           for (int h = 0; h < 2; ++h)
@@ -398,8 +363,10 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top[nb] = fmaxf(top[nb], S8 ? acc[nb][h][j] + vl[h][j] : acc[nb][h][j]);
-          rises = rises || top[nb] > m[nb] + SLACK;
+            for (int j = 0; j < 4; ++j)
+              top[nb] = fmaxf(top[nb], S8 ? __builtin_fmaf(acc[nb][h][j], q_scale[nb] * ks[h][j], vl[h][j]) : acc[nb][h][j]);
+          if (!S8) top[nb] *= q_scale[nb];
+          rises = rises || top[nb] > m[nb] + Wt::SLACK;
         }
         if (__any(rises)) {                   // (seldom in a long context)
 #pragma unroll
@@ -419,13 +386,13 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
         v4i pt[N];
 #pragma unroll
         for (int nb = 0; nb < N; ++nb) {
-          const float below = (m[nb] == -INFINITY ? 0.0f : m[nb]) - up<C>();
+          const float below = (m[nb] == -INFINITY ? 0.0f : m[nb]) - (Wt::TOP - Wt::SLACK);
           t8 wh;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float w = __builtin_amdgcn_exp2f(acc[nb][j >> 2][j & 3] - below);
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[nb][j >> 2][j & 3], S8 ? q_scale[nb] * ks[j >> 2][j & 3] : q_scale[nb], -below));
             l[nb] += w;
-            wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : w + floor_of<C>());
+            wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : w + Wt::LEAST);
           }
           pt[nb] = __builtin_bit_cast(v4i, wh);
         }
@@ -452,18 +419,64 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_nop 15" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        if (!next) break;
         load_values(rows[wave][buf ^ 1].at);
-        buf ^= 1, t0 += UNIT;
+        buf ^= 1, t0 += step;
+        if (t0 >= end) break;
       }
+  };
+
+  // ---- prefixes ----
+  int item = left > 0 ? __builtin_amdgcn_readfirstlane(from[0]) : 0;
+  int64_t in = left > 0 ? uniform64(runs.start(run) - before[0]) : 0;        // units of the item in front of this run
+  while (left > 0) {
+    // requests b0 + req0 .., `heads` query heads of cache head kvh each, over tokens of the row `leader` of the table
+    const Prefix x = work.prefix(item);
+    const int b0 = __builtin_amdgcn_readfirstlane(x.b0), n = __builtin_amdgcn_readfirstlane(x.n), tokens = __builtin_amdgcn_readfirstlane(x.tokens);
+    const int units = work.units(tokens), blocks = work.blocks(n);
+    int leader = b0, t_end = tokens;
+    if (work.len(leader) < tokens) {
+      // (an empty place in front) the first member that has all of the prefix; without any nobody reads what comes out
+      int have = 0x7fffffff;
+      for (int i = b0 + (int)threadIdx.x; i < b0 + n && have == 0x7fffffff; i += THREADS)
+        if (work.len(i) >= tokens) have = i;
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) have = min(have, __shfl_xor(have, d));
+      if (lane == 0) found[wave] = have;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) have = min(have, found[w]);
+      __syncthreads();
+      leader = __builtin_amdgcn_readfirstlane(have);
+      if (leader == 0x7fffffff) leader = b0, t_end = 0;
+    }
+    const int pair = __builtin_amdgcn_readfirstlane((int)(in / units)), unit = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)pair * units));
+    const int kvh = pair / blocks, block = pair - kvh * blocks, chunk = block % p.chunks, req0 = block / p.chunks * p.per_block;
+    const int h0 = chunk * p.rows, heads = p.chunks > 1 ? min(p.rows, p.group - h0) : p.group;
+    const int real_rows = __builtin_amdgcn_readfirstlane(min(n - req0, p.per_block) * heads), nb_used = (real_rows + COLS - 1) / COLS;
+    const int last = (int)min((int64_t)units, unit + left), end = min(t_end, last * UNIT);
+    auto place = [&](int row, int &b, int &hq) {             // of a row of the block
+      const int r = p.chunks > 1 ? 0 : (int)p.by_group.div((uint32_t)row);
+      b = b0 + req0 + r, hq = kvh * p.group + h0 + row - r * heads;
     };
+    for (int nb = wave; nb < nb_used; nb += WAVES) {
+      const int row = nb * COLS + c16;
+      int b, hq;
+      place(min(row, real_rows - 1), b, hq);
+      put_queries(nb, row < real_rows ? static_cast<const Q *>(p.q) + b * p.qt + hq * p.qh : nullptr);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) q_scale[nb] = q_scale_lds[nb][c16];
+    clear();
+    const int32_t *table = p.table + leader * p.table_ld;
+    const int t0 = unit * UNIT + wave * TILE;
     if constexpr (NB >= 4) {
-      if (nb_used > 2) walk(std::integral_constant<int, 4>());
-      else if (nb_used > 1) walk(std::integral_constant<int, 2>());
-      else walk(std::integral_constant<int, 1>());
+      if (nb_used > 2) walk(std::integral_constant<int, 4>(), table, kvh, t0, UNIT, end, 0);
+      else if (nb_used > 1) walk(std::integral_constant<int, 2>(), table, kvh, t0, UNIT, end, 0);
+      else walk(std::integral_constant<int, 1>(), table, kvh, t0, UNIT, end, 0);
     } else {
-      if (nb_used > 1) walk(std::integral_constant<int, 2>());
-      else walk(std::integral_constant<int, 1>());
+      if (nb_used > 1) walk(std::integral_constant<int, 2>(), table, kvh, t0, UNIT, end, 0);
+      else walk(std::integral_constant<int, 1>(), table, kvh, t0, UNIT, end, 0);
     }
 
     // the waves join in LDS, 16 columns at a time, and leave the piece
@@ -502,20 +515,58 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
         }
         int b, hq;
         place(row, b, hq);
-        const int64_t at = whole ? whole_at(p, own, b, hq) : cut_at(p, run, unit == 0, row);
+        const int64_t at = whole ? whole_at(p, false, b, hq) : cut_at(p, false, run, unit == 0, row);
         p.part_o[at * p.dim + d] = of;
         if (d == 0) p.part_ml[2 * at] = mh, p.part_ml[2 * at + 1] = sum;
       }
       __syncthreads();
     }
-    left -= last - unit;
-    more = left > 0;
-    in += last - unit;
-    if (more && in == (int64_t)units * pairs) {               // the next item that has units
+    left -= last - unit, in += last - unit;
+    if (left > 0 && in == (int64_t)units * blocks * p.heads) {                // the next group that has units
       in = 0;
       do ++item;
       while (work.units_of(item) == 0);
       item = __builtin_amdgcn_readfirstlane(item);
+    }
+  }
+
+  // ---- own tokens, every wave for itself ----
+  int b = own_left > 0 ? __builtin_amdgcn_readfirstlane(from[1 + wave]) : 0;
+  in = own_left > 0 ? uniform64(own_runs.start(own_run) - before[1 + wave]) : 0;
+  const int own_chunks = work.own_chunks();
+  while (own_left > 0) {
+    const int t_begin = __builtin_amdgcn_readfirstlane(work.prefix_of(b)), len = __builtin_amdgcn_readfirstlane(work.len(b));
+    const int tiles = work.tiles(len - t_begin);
+    const int pair = __builtin_amdgcn_readfirstlane((int)(in / tiles)), tile = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)pair * tiles));
+    const int kvh = pair / own_chunks, h0 = (pair - kvh * own_chunks) * COLS, heads = min(COLS, p.group - h0), hq = kvh * p.group + h0 + c16;
+    const int last = (int)min((int64_t)tiles, tile + own_left);
+    lanes_meet();
+    put_queries(wave, c16 < heads ? static_cast<const Q *>(p.q) + b * p.qt + hq * p.qh : nullptr);
+    lanes_meet();
+    q_scale[0] = q_scale_lds[wave][c16];
+    clear();
+    walk(std::integral_constant<int, 1>(), p.table + b * p.table_ld, kvh, t_begin + tile * TILE, TILE, min(len, t_begin + last * TILE), wave);
+    l[0] += __shfl_xor(l[0], 16);
+    l[0] += __shfl_xor(l[0], 32);
+    if (c16 < heads) {
+      const int64_t at = tile == 0 && last == tiles ? whole_at(p, true, b, hq) : cut_at(p, true, own_run, tile == 0, c16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int d = (4 * g + j) * E;          // (dim is a multiple of 16 and so of E)
+        if (d < p.dim) {
+#pragma unroll
+          for (int e = 0; e < E; e += 4)
+            *reinterpret_cast<v4f *>(p.part_o + at * p.dim + d + e) = v4f{o[0][e][j], o[0][e + 1][j], o[0][e + 2][j], o[0][e + 3][j]};
+        }
+      }
+      if (g == 0) p.part_ml[2 * at] = m[0], p.part_ml[2 * at + 1] = l[0];
+    }
+    own_left -= last - tile, in += last - tile;
+    if (own_left > 0 && in == (int64_t)tiles * own_chunks * p.heads) {         // the next request that has tiles
+      in = 0;
+      do ++b;
+      while (work.tiles_of(b) == 0);
+      b = __builtin_amdgcn_readfirstlane(b);
     }
   }
 }
@@ -538,39 +589,43 @@ __global__ __launch_bounds__(64 * JOINERS) void join_shared_kernel(SharedParams 
   const int e = blockIdx.y * JOIN_PART + vec * 4, h = e / p.dim, d = e - h * p.dim;
   const bool real = h < heads;
   const int hq = kvh * p.group + h0 + (real ? h : 0), col = real ? d : 0;
-  // units in front of the group and of the request, and all of them
-  const int g = work.group_of(b), own = p.groups + b, prefix = work.prefix_of(b);
+  // units in front of the group, tiles in front of the request, and all of them
+  const int g = work.group_of(b), prefix = work.prefix_of(b);
   const Prefix x = g < 0 ? Prefix{0, 0, 0} : work.prefix(g);
   int64_t sum[2] = {0, 0}, front[2] = {0, 0};
-  for (int i = threadIdx.x; i < p.groups + p.batch; i += 64 * JOINERS) {
+  for (int i = threadIdx.x; i < p.groups; i += 64 * JOINERS) {
     const int64_t u = work.units_of(i);
     sum[0] += u;
-    if (i < own) front[0] += u;
-    if (i < g) front[1] += u;
+    if (i < g) front[0] += u;
+  }
+  for (int i = threadIdx.x; i < p.batch; i += 64 * JOINERS) {
+    const int64_t u = work.tiles_of(i);
+    sum[1] += u;
+    if (i < b) front[1] += u;
   }
   wg_sum<JOINERS>(sum, scan);
   wg_sum<JOINERS>(front, scan);
-  const Runs runs(uniform64(sum[0]), p.wgs);
-  // pieces of the prefix's pair and of the own one: places i0 .. i0 + n - 1
+  // pieces of the prefix's pair and of the own one
   struct Pieces {
-    int64_t first, rest;                      // rows of piece 0 and 1; the others follow 2 * rows apart
+    int64_t first, rest, step;                // rows of piece 0 and 1, and from there to the next
     int n;
   };
-  auto pieces = [&](int64_t at, int units, bool is_own, int row) {
-    if (units == 0) return Pieces{0, 0, 0};
+  auto pieces = [&](const Runs &runs, int64_t at, int units, bool own, int row) {
+    if (units == 0) return Pieces{0, 0, 0, 0};
     const int64_t i0 = runs.of(at), i1 = runs.of(at + units - 1);
-    if (i0 == i1) return Pieces{whole_at(p, is_own, b, hq), 0, 1};
-    return Pieces{cut_at(p, i0, 1, row), cut_at(p, i0 + 1, 0, row), (int)(i1 - i0) + 1};
+    if (i0 == i1) return Pieces{whole_at(p, own, b, hq), 0, 0, 1};
+    return Pieces{cut_at(p, own, i0, 1, row), cut_at(p, own, i0 + 1, 0, row), 2 * (own ? COLS : p.rows), (int)(i1 - i0) + 1};
   };
-  const int pu = prefix > 0 ? work.units(prefix) : 0, ou = work.units(work.len(b) - prefix);
+  const int pu = prefix > 0 ? work.units(prefix) : 0, ot = work.tiles(work.len(b) - prefix), in_group = h0 + (real ? h : 0);
   const int blocks = work.blocks(x.n), block = (b - x.b0) / p.per_block * p.chunks + chunk;
-  const Pieces a = pieces(uniform64(front[1] + ((int64_t)kvh * blocks + block) * pu), pu, false, (b - x.b0) % p.per_block * heads + (real ? h : 0));
-  const Pieces c = pieces(uniform64(front[0] + (int64_t)hc * ou), ou, true, real ? h : 0);
+  const Pieces a = pieces(Runs(uniform64(sum[0]), p.wgs), uniform64(front[0] + ((int64_t)kvh * blocks + block) * pu), pu, false,
+                          (b - x.b0) % p.per_block * heads + (real ? h : 0));
+  const Pieces c = pieces(Runs(uniform64(sum[1]), p.wgs * WAVES), front[1] + ((int64_t)kvh * work.own_chunks() + in_group / COLS) * ot, ot, true, in_group % COLS);
   const int n = a.n + c.n;
   auto row_of = [&](int i) {
     const Pieces &k = i < a.n ? a : c;
     const int j = i < a.n ? i : i - a.n;
-    return j == 0 ? k.first : k.rest + (int64_t)(j - 1) * 2 * p.rows;
+    return j == 0 ? k.first : k.rest + (j - 1) * k.step;
   };
   Q *out = static_cast<Q *>(p.out) + b * p.ot + hq * p.oh + col;
   const float2 *ml = reinterpret_cast<const float2 *>(p.part_ml);
@@ -632,7 +687,7 @@ f8_status launch(const SharedParams &p, hipStream_t s) {
 
 // Where a request's tokens fit one launch of f8_attend_paged, that is the faster way.
 bool alone(int groups, int max_len) { return groups == 0 || max_len <= 4 * UNIT; }
-size_t pieces_of(int64_t batch, int q_heads, int dim) { return (size_t)2 * batch * q_heads + (size_t)2 * WGS * blocks_of(dim) * COLS; }
+size_t pieces_of(int64_t batch, int q_heads, int dim) { return (size_t)2 * batch * q_heads + (size_t)2 * WGS * (blocks_of(dim) + WAVES) * COLS; }
 
 }  // namespace
 }  // namespace f8
