@@ -20,7 +20,10 @@ namespace {
 
 constexpr int WAVES = 4, TILE = 32, COLS = 16, UNIT = WAVES * TILE, THREADS = 64 * WAVES;
 constexpr int GROUPS_LDS = 1024;             // groups whose bounds a workgroup keeps in LDS
-constexpr int WGS = 256;
+constexpr int CUS = 256;
+// Workgroups, two to a CU where the registers allow it, and blocks of columns of a workgroup.
+constexpr int wgs_of(int dim) { return dim <= 128 ? 2 * CUS : CUS; }
+constexpr int blocks_of(int dim, int bytes) { return dim <= 64 && bytes == 2 ? 4 : 2; }
 
 struct SharedParams {
   const void *q, *k, *v;
@@ -150,7 +153,7 @@ __device__ __forceinline__ void find_items(int n, const int64_t (&starts)[R], Of
 }
 
 template <typename C, typename Q, int DP, int NB>
-__global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams p) {
+__global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kernel(SharedParams p) {
   typedef Operand<C> Op;
   typedef Weights<C> Wt;
   typedef typename Op::t H;
@@ -160,8 +163,16 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
   constexpr int KL = DP * (int)sizeof(C) / 64;            // 16-byte loads of a key row per lane
   constexpr int KS = DP / 32;                             // products per block of 16 scores
   constexpr int BLOCKS = NB > WAVES ? NB : WAVES;
+  constexpr int PIECES = DP * (int)sizeof(C) / 16;        // 16-byte pieces of a key row, and loads of a tile's keys
+  constexpr int KI = TILE * PIECES / 64;
+  // A wave's keys, and its part of a piece when its run is over.
+  union Stage {
+    v4i keys[TILE * PIECES];
+    float part[COLS][DP + 1];
+  };
+  __shared__ Stage stage[WAVES];
   __shared__ TileRows rows[WAVES][2];
-  __shared__ float part[WAVES][COLS][DP + 1], ml[WAVES][NB * COLS][2];
+  __shared__ float ml[WAVES][NB * COLS][2];
   __shared__ int64_t scan[WAVES][2], before[1 + WAVES];
   __shared__ int from[1 + WAVES], found[WAVES];
   __shared__ v4i q_lds[BLOCKS][KS][64];
@@ -253,13 +264,18 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
     if (t0 >= end) return;
     const C *const kbase = static_cast<const C *>(p.k) + kvh * p.head, *const vbase = static_cast<const C *>(p.v) + kvh * p.head;
     const int dv = c16 * E < p.dim ? c16 * E : 0;
-    const int64_t none = reinterpret_cast<const char *>(zeros) - reinterpret_cast<const char *>(kbase);
-    // The rows of a tile in registers.  The next one's keys are loaded when this one's scores are there, its values when this one's have been summed
-    // up: every load has half a tile's time on its way and no register waits twice.  All loads are issued whether there is a next tile or not (a token that
+    // Keys come as they lie in memory, rows of neighbouring lanes, and become the product's left operand in LDS: its lanes hold 16 bytes of 16 rows each, which
+    // the load unit would take a row at a time (a quarter of the rate).  A row's pieces are permuted by its number: no 16 rows' pieces share banks.
+    auto turned = [](int row) { return PIECES >= 16 ? row & 15 : PIECES == 8 ? row & 7 : row >> 1 & 3; };
+    const int key_row = lane / PIECES, key_piece = lane % PIECES;             // of load 0; load n is n * 64 / PIECES rows further
+    const bool key_real = key_piece * (16 / (int)sizeof(C)) < p.dim;
+    const int64_t key_on = key_real ? -1 : 0, key_from = key_real ? key_piece * 16 : reinterpret_cast<const char *>(zeros) - reinterpret_cast<const char *>(kbase);
+    v4i *const keys = stage[wave].keys;
+    // The next tile's keys are on their way from when this one's are in LDS, its values from when this one's have been summed up.  All loads are issued whether there is a next tile or not (a token that
     // does not exist reads row 0 of the cache): behind a branch around a load nobody knows how many are on their way, and the wait is for all.
-    Raw<16> k[2][KL];
+    v4i k[KI];
     Raw<VB> v[8];
-    float tile_scale;                         // lanes 0..31: of the key of token `lane`, 32..63: of the value of token `lane - 32`
+    float tile_scale = 1.0f;                  // lanes 0..31: of the key of token `lane`, 32..63: of the value of token `lane - 32`
     uint32_t there;                           // its tokens that exist
     auto look_up = [&](int t0) {              // page of token lane % 32 of the tile at t0, where there is one
       return table[p.page_size.div((uint32_t)min(t0 + (lane & 31), end - 1))];
@@ -276,15 +292,21 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
     };
     auto load_keys = [&](const int64_t (&at_lds)[TILE]) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int64_t row = at_lds[16 * h + c16] * (int64_t)sizeof(C);
-#pragma unroll
-        for (int i = 0; i < KL; ++i) {
-          const int d = (i * 4 + g) * (16 / (int)sizeof(C));
-          k[h][i] = load_raw<16>(reinterpret_cast<const char *>(kbase) + (d < p.dim ? row + d * (int)sizeof(C) : none));
-        }
+      for (int n = 0; n < KI; ++n) {
+        const int64_t row = at_lds[n * (64 / PIECES) + key_row] * (int64_t)sizeof(C);
+        k[n] = *reinterpret_cast<const v4i *>(reinterpret_cast<const char *>(kbase) + ((row & key_on) + key_from));
       }
     };
+    auto stage_keys = [&]() {
+      lanes_meet();
+#pragma unroll
+      for (int n = 0; n < KI; ++n) {
+        const int row = n * (64 / PIECES) + key_row;
+        keys[row * PIECES + (key_piece ^ turned(row))] = k[n];
+      }
+      lanes_meet();
+    };
+    auto key = [&](int h, int i) { return keys[(16 * h + c16) * PIECES + ((i * 4 + g) ^ turned(c16))]; };
     auto load_values = [&](const int64_t (&at_lds)[TILE]) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -299,10 +321,15 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
       load_values(rows[wave][0].at);
       for (;;) {
         const uint32_t now = there;
+        stage_keys();
+        const float now_scale = tile_scale;
+        there = locate(t0 + step, page, rows[wave][buf ^ 1].at);
+        load_keys(rows[wave][buf ^ 1].at);
+        page = look_up(t0 + 2 * step);
         v4f ks[2], vs[2], vl[2];
         if constexpr (S8) {
           float *const scale_lds = rows[wave][buf].scale;
-          const float scale = now >> (lane & 31) & 1 ? tile_scale : 1.0f;
+          const float scale = now >> (lane & 31) & 1 ? now_scale : 1.0f;
           scale_lds[lane] = scale;
           scale_lds[64 + lane] = fmaxf(__log2f(scale), SMALL);
           lanes_meet();
@@ -320,12 +347,12 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < KL; ++i) {
-            const uint32_t(&d)[4] = k[h][i].d;
+            const v4i d = key(h, i);
             if constexpr (S8) {
               h8 lo, hi;
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                const uint32_t u = d[j] ^ 0x80808080u;
+                const uint32_t u = (uint32_t)d[j] ^ 0x80808080u;
                 const h2 a = codes_lo(u), e = codes_hi(u);
                 h8 &to = j < 2 ? lo : hi;
                 to[4 * (j & 1)] = a[0], to[4 * (j & 1) + 1] = a[1], to[4 * (j & 1) + 2] = e[0], to[4 * (j & 1) + 3] = e[1];
@@ -336,12 +363,9 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
               for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, hi), q_lds[q0 + nb][2 * i + 1][lane], acc[nb][h]);
             } else {
 #pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(v4i{(int)d[0], (int)d[1], (int)d[2], (int)d[3]}, q_lds[q0 + nb][i][lane], acc[nb][h]);
+              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(d, q_lds[q0 + nb][i][lane], acc[nb][h]);
             }
           }
-        there = locate(t0 + step, page, rows[wave][buf ^ 1].at);
-        load_keys(rows[wave][buf ^ 1].at);
-        page = look_up(t0 + 2 * step);
         if (now != 0xffffffffu) {
 #pragma unroll
           for (int h = 0; h < 2; ++h)
@@ -499,7 +523,7 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
 #pragma unroll
       for (int e = 0; e < E; ++e)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) part[wave][c16][(4 * g + j) * E + e] = o[nb][e][j] * shrink;
+        for (int j = 0; j < 4; ++j) stage[wave].part[c16][(4 * g + j) * E + e] = o[nb][e][j] * shrink;
       __syncthreads();
       for (int i = threadIdx.x; i < COLS * DP; i += THREADS) {
         const int c = i / DP, d = i % DP, row = nb * COLS + c;
@@ -511,7 +535,7 @@ __global__ __launch_bounds__(THREADS, 1) void attend_shared_kernel(SharedParams 
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
           sum += ml[w][row][1] * __builtin_amdgcn_exp2f(ml[w][row][0] - base);
-          of += part[w][c][d];
+          of += stage[w].part[c][d];
         }
         int b, hq;
         place(row, b, hq);
@@ -669,15 +693,12 @@ __global__ __launch_bounds__(64 * JOINERS) void join_shared_kernel(SharedParams 
   for (int k = 0; k < 4; ++k) out[k] = (Q)(total == 0.0f ? 0.0f : o[k] / total);
 }
 
-// Blocks of columns of a workgroup, by the registers that a column's output takes.
-constexpr int blocks_of(int dim) { return dim <= 128 ? 4 : 2; }
-
 template <typename C, typename Q>
 f8_status launch(const SharedParams &p, hipStream_t s) {
   const dim3 grid(p.wgs), block(THREADS);
-  if (p.dim <= 64) hipLaunchKernelGGL((attend_shared_kernel<C, Q, 64, blocks_of(64)>), grid, block, 0, s, p);
-  else if (p.dim <= 128) hipLaunchKernelGGL((attend_shared_kernel<C, Q, 128, blocks_of(128)>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((attend_shared_kernel<C, Q, 256, blocks_of(256)>), grid, block, 0, s, p);
+  if (p.dim <= 64) hipLaunchKernelGGL((attend_shared_kernel<C, Q, 64, blocks_of(64, sizeof(C))>), grid, block, 0, s, p);
+  else if (p.dim <= 128) hipLaunchKernelGGL((attend_shared_kernel<C, Q, 128, blocks_of(128, sizeof(C))>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((attend_shared_kernel<C, Q, 256, blocks_of(256, sizeof(C))>), grid, block, 0, s, p);
   const f8_status st = launch_status();
   if (st != F8_OK) return st;
   const int elements = (p.chunks > 1 ? p.rows : p.group) * p.dim;
@@ -687,7 +708,7 @@ f8_status launch(const SharedParams &p, hipStream_t s) {
 
 // Where a request's tokens fit one launch of f8_attend_paged, that is the faster way.
 bool alone(int groups, int max_len) { return groups == 0 || max_len <= 4 * UNIT; }
-size_t pieces_of(int64_t batch, int q_heads, int dim) { return (size_t)2 * batch * q_heads + (size_t)2 * WGS * (blocks_of(dim) + WAVES) * COLS; }
+size_t pieces_of(int64_t batch, int q_heads, int dim) { return (size_t)2 * batch * q_heads + (size_t)2 * wgs_of(dim) * (blocks_of(dim, 2) + WAVES) * COLS; }
 
 }  // namespace
 }  // namespace f8
@@ -715,7 +736,7 @@ f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cac
     return f8_attend_paged(q, k_cache, v_cache, k_scale, v_scale, table, lens, out, c, d, workspace, workspace_bytes, stream);
   st = check_attend_pointers(q, k_cache, v_cache, k_scale, v_scale, table, lens, out, *c, *d);
   if (st != F8_OK) return st;
-  const int group = d->q_heads / c->heads, most = blocks_of(c->dim) * COLS, chunks = (group + most - 1) / most;
+  const int group = d->q_heads / c->heads, most = blocks_of(c->dim, (int)bytes_of(c->type)) * COLS, chunks = (group + most - 1) / most;
   if ((int64_t)d->batch * c->heads * chunks > 1 << 22) return F8_ERR_UNSUPPORTED;          // (workgroups of a launch)
   if (!workspace) return F8_ERR_NULL;
   if (!aligned_to(workspace, 16)) return F8_ERR_ALIGN;
@@ -724,7 +745,7 @@ f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cac
   const SharedParams p{q, k_cache, v_cache, k_scale, v_scale, table, lens, first, shared, out, ws, ws + pieces_of(d->batch, d->q_heads, c->dim) * c->dim,
                        d->q_token, d->q_head, d->o_token, d->o_head, c->page_stride, c->token_stride, c->head_stride,
                        c->scale_page, c->scale_token, c->scale_head, d->table_ld, d->batch, groups, c->heads, group, chunks,
-                       chunks > 1 ? 1 : most / group, c->dim, c->pages, d->max_len, WGS, most, FastDiv((uint32_t)c->page_size), FastDiv((uint32_t)group),
+                       chunks > 1 ? 1 : most / group, c->dim, c->pages, d->max_len, wgs_of(c->dim), most, FastDiv((uint32_t)c->page_size), FastDiv((uint32_t)group),
                        d->scale * LOG2E};
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (c->type == F8_S8) return d->type == F8_F16 ? launch<int8_t, f16>(p, hs) : launch<int8_t, bf16>(p, hs);
