@@ -4,10 +4,10 @@
 // their maximum m, sum exp(x - m) and `keep` largest, and a second launch (a workgroup to a prompt) adds up the sums, forms S of what
 // is left in 64 bits and takes the `keep` largest of that.  Bound by HBM: the logits are read once.
 //
-// The largest of a set.  Elements are keys (value, then lowest index: no two alike).  Threads form at least `keep` groups; every group's
-// largest key is one of the elements, so the least of these maxima is a lower bound of the keep-th largest key, which few elements pass (16 of 16384
-// random ones: about 45).  Those go to a list in LDS, and each one's place is the number of keys above it.  Where more pass than
-// the list holds, the bound is the keep-th largest of the threads' own maxima: what passes then are elements of `keep` threads.
+// The largest of a set.  Threads form at least `keep` groups; every group's largest element is one of the set's, so the least of these maxima is a
+// lower bound of the keep-th largest, which few elements reach (16 of 16384 random ones: about 45).  Those go to a list in LDS, as keys of which no
+// two are alike (value, then lowest index), and each one's place is the number of keys above it.  Where more reach it than
+// the list holds (many alike), the bound is the keep-th largest of the threads' own largest keys: what passes then are elements of `keep` threads.
 #include "tokens_device.h"
 #include "tokens_host.h"
 
@@ -18,7 +18,9 @@ constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int CHUNK = 16384;                                // logits of a workgroup at most
 constexpr int CANDIDATES = 8192;                            // of a prompt in the second launch at most
 constexpr int BEAMS = 1024;
-__host__ __device__ inline int each_of(uint32_t candidates) { return (int)((candidates + THREADS - 1) / THREADS); }   // of a thread there
+// Keys that the list has room for: those of `keep` threads, or as many as reach a bound that fits loosely
+__host__ __device__ inline int list_of(int keep, int each) { return keep * each < 512 ? 512 : keep * each; }
+inline int each_of(uint32_t candidates) { return (int)((candidates + THREADS - 1) / THREADS); }   // of a thread there
 
 struct Stat {
   double sum;                               // of exp(x - top)
@@ -36,7 +38,7 @@ struct BeamParams {
   int64_t ld;
   int beams, vocab, keep, splits, eos, groups;              // groups of threads: a power of two, at least `keep`
   int64_t blocks;
-  FastDiv by_splits;
+  FastDiv by_splits, by_row;                // by_row: candidates of a row in the second launch
 };
 
 // Numbers as unsigned integers of the same order, all above 0; -0 is 0 and NaN lies above all.
@@ -55,13 +57,14 @@ __device__ __forceinline__ double of_order(uint64_t o) {
   return __longlong_as_double((long long)(o >> 63 ? (o == ~0ull ? o : o & ~(1ull << 63)) : ~o));
 }
 
+constexpr float LOG2E = 1.4426950408889634f;
+
 // Keys: a logit and its token; S, its beam, its logit and token (a score may be so large that 64 bits give two logits of a beam the same
 // S: the larger one's is larger).  Key{} is no element.
 struct Key64 {
   uint64_t k;
   __device__ __forceinline__ bool operator<(const Key64 &o) const { return k < o.k; }
   __device__ __forceinline__ bool real() const { return k != 0; }
-  __device__ __forceinline__ Key64 from(int d) const { return Key64{(uint64_t)__shfl_xor((unsigned long long)k, d)}; }
 };
 struct KeyS {
   uint64_t s, beam, logit;                  // beam: ~i, logit: its order, ~token
@@ -69,92 +72,74 @@ struct KeyS {
     return s < o.s || (s == o.s && (beam < o.beam || (beam == o.beam && logit < o.logit)));
   }
   __device__ __forceinline__ bool real() const { return s != 0; }
-  __device__ __forceinline__ KeyS from(int d) const {
-    return KeyS{(uint64_t)__shfl_xor((unsigned long long)s, d), (uint64_t)__shfl_xor((unsigned long long)beam, d),
-                (uint64_t)__shfl_xor((unsigned long long)logit, d)};
-  }
 };
 
-template <typename K>
-struct Pick {
-  K top[THREADS], bound;
-  int n;
-};
+// One instruction for two maxima (fmaxf costs two for one, where it does not know that its operands are no signalling NaN).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
-// The `keep` largest of all threads' elements: mine is the largest of this thread's, each(bound, f) calls f for those of them that are not below
-// `bound` (and may for others).  out(place, key) is called for each, places from 0 in descending order; returns how many there are.
-// list: `most` keys, keep times a thread's elements.  Every thread of the workgroup comes here.
-template <typename K, typename Each, typename Out>
-__device__ __forceinline__ int pick(Pick<K> &l, K *list, int most, int keep, int groups, K mine, Each each, Out out) {
-  const int t = threadIdx.x, lane = t & 63;
-  // thread t belongs to group t mod `groups`: neighbours, which hold neighbouring elements, to different ones
-  K bound = mine;
-  for (int d = 32; d >= groups; d >>= 1) {
-    const K o = bound.from(d);
-    if (bound < o) bound = o;
-  }
-  l.top[t] = bound;
-  if (t == 0) l.n = 0;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w)
-    if (bound < l.top[w * 64 + lane]) bound = l.top[w * 64 + lane];
-  for (int d = min(groups, 64) >> 1; d > 0; d >>= 1) {
-    const K o = bound.from(d);
-    if (o < bound) bound = o;
-  }
-  auto collect = [&](K key) {
-    if (key.real() && !(key < bound)) {
-      const int i = atomicAdd(&l.n, 1);
-      if (i < most) list[i] = key;
-    }
-  };
-  each(bound, collect);
-  __syncthreads();
-  int n = l.n;
-  if (n > most) {
-    __syncthreads();
-    l.top[t] = mine;
-    if (t == 0) l.n = 0, l.bound = K{};
-    __syncthreads();
-    int above = 0;
-    for (int i = 0; i < THREADS; ++i) above += mine < l.top[i];
-    if (above == keep - 1 && mine.real()) l.bound = mine;
-    __syncthreads();
-    bound = l.bound;
-    each(bound, collect);
-    __syncthreads();
-    n = min(l.n, most);
-  }
-  for (int i = t; i < n; i += THREADS) {
+// The `keep` largest of a list of n keys, none alike: out(place, key) is called for each, places from 0 in descending order.
+template <typename K, typename Out>
+__device__ __forceinline__ void rank(const K *list, int n, int keep, Out out) {
+  for (int i = threadIdx.x; i < n; i += THREADS) {
     const K key = list[i];
     int above = 0;
     for (int j = 0; j < n; ++j) above += key < list[j];
     if (above < keep) out(above, key);
   }
-  return min(n, keep);
 }
 
-// exp(t) for t <= 0 to the last place of the hardware's exponential: the product with log2 e in two parts.
-__device__ __forceinline__ float exp_of(float t) {
-  return __builtin_amdgcn_exp2f(__builtin_fmaf(t, 1.44269502162933349609375f, t * 1.92596299e-8f));
+// The keep-th largest of the threads' keys (Key{} where fewer are real), for all threads.  `top`: a key to a thread, and one more.
+template <typename K>
+__device__ __forceinline__ K kth(K mine, int keep, K *top) {
+  const int t = threadIdx.x;
+  __syncthreads();
+  top[t] = mine;
+  if (t == 0) top[THREADS] = K{};
+  __syncthreads();
+  int above = 0;
+  for (int i = 0; i < THREADS; ++i) above += mine < top[i];
+  if (above == keep - 1 && mine.real()) top[THREADS] = mine;
+  __syncthreads();
+  return top[THREADS];
+}
+
+// The least of the groups' largest values, for all threads.  Thread t belongs to group t mod `groups`: neighbours, which hold neighbouring
+// elements, to different ones.  wave_top: [THREADS].
+__device__ __forceinline__ float least_of_groups(float v, int groups, float *wave_top) {
+  const int lane = threadIdx.x & 63;
+  for (int d = 32; d >= groups; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  wave_top[threadIdx.x] = v;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) v = fmaxf(v, wave_top[w * 64 + lane]);
+  for (int d = min(groups, 64) >> 1; d > 0; d >>= 1) v = fminf(v, __shfl_xor(v, d));
+  return v;
 }
 
 template <typename T, int NV>
-__global__ __launch_bounds__(THREADS) void beam_rows_kernel(BeamParams p) {
+__global__ __launch_bounds__(THREADS, NV < 8 ? 6 : 4) void beam_rows_kernel(BeamParams p) {
   typedef RowMap<THREADS, NV> Map;
   extern __shared__ __align__(16) uint8_t dynamic[];
-  __shared__ Pick<Key64> l;
+  Key64 *const list = reinterpret_cast<Key64 *>(dynamic);             // list_of(keep, NV * 8)
+  __shared__ Key64 top_keys[THREADS + 1];
+  __shared__ float wave_top[THREADS];
   __shared__ float tops[WAVES];
   __shared__ double sums[WAVES];
+  __shared__ uint16_t pieces[THREADS * NV];
+  __shared__ int count, reach;
   const int64_t block = row_block();
   if (block >= p.blocks) return;
   const int row = (int)p.by_splits.div((uint32_t)block), split = (int)block - row * p.splits;
   if (p.done && p.done[row]) return;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, most = list_of(p.keep, NV * 8);
   const int base = split * Map::most, cols = min(Map::most, p.vocab - base);
   const T *x = static_cast<const T *>(p.logits) + row * p.ld + base;
   float v[NV][8], piece[NV], top = -INFINITY;
+  if (t == 0) count = 0, reach = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) load_piece<T, Map>(x, i, t, cols, v[i]);
 #pragma unroll
@@ -164,56 +149,82 @@ __global__ __launch_bounds__(THREADS) void beam_rows_kernel(BeamParams p) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = j < here ? v[i][j] : -INFINITY;
     }
-    piece[i] = fmaxf(fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3])), fmaxf(fmaxf(v[i][4], v[i][5]), fmaxf(v[i][6], v[i][7])));
-    top = fmaxf(top, piece[i]);
+    piece[i] = max3(max3(v[i][0], v[i][1], v[i][2]), max3(v[i][3], v[i][4], v[i][5]), v[i][6]);
+    piece[i] = max3(piece[i], v[i][7], v[i][7]);
+    top = max3(top, piece[i], piece[i]);
   }
-  // the thread's largest: the first of its value
-  int at = 0x7fffffff;
-#pragma unroll
-  for (int i = NV - 1; i >= 0; --i) {
-    if (piece[i] == top) {
-#pragma unroll
-      for (int j = 7; j >= 0; --j)
-        if (v[i][j] == top && Map::col(i, j, t) < cols) at = Map::col(i, j, t);
-    }
-  }
-  const Key64 mine{at < cols ? (uint64_t)order_of(top) << 32 | (uint32_t)~(base + at) : 0};
   float m = top;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
   if (lane == 0) tops[wave] = m;
-  const int n = pick<Key64>(
-      l, reinterpret_cast<Key64 *>(dynamic), p.keep * NV * 8, p.keep, p.groups, mine,
-      [&](Key64 bound, auto f) {
-        const float least = bound.real() ? of_order((uint32_t)(bound.k >> 32)) : -INFINITY;
+  // (values alone: where many are alike, they all pass and the list runs over)
+  const float least = least_of_groups(top, p.groups, wave_top);
+  // pieces that reach the bound are put down, their elements looked at behind that by a thread each (read once more: 64 branches to 64 places
+  // of registers would cost more than the few cached lines)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          if (piece[i] >= least) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (v[i][j] >= least && Map::col(i, j, t) < cols)
-                f(Key64{(uint64_t)order_of(v[i][j]) << 32 | (uint32_t)~(base + Map::col(i, j, t))});
-          }
+  for (int i = 0; i < NV; ++i)
+    if (piece[i] >= least) pieces[atomicAdd(&reach, 1)] = (uint16_t)(i * THREADS + t);
+  __syncthreads();
+  const int elements = reach * 8;
+  for (int q = t; q < elements; q += THREADS) {
+    const int col = pieces[q >> 3] * 8 + (q & 7);
+    if (col < cols) {
+      const float e = (float)x[col];
+      if (e >= least) {
+        const int at = atomicAdd(&count, 1);
+        if (at < most) list[at].k = (uint64_t)order_of(e) << 32 | (uint32_t)~(base + col);
+      }
+    }
+  }
+  __syncthreads();
+  int n = count;
+  if (n > most) {
+    // the bound is the keep-th largest of the threads' own largest keys: what passes then are elements of `keep` threads (read once more, one
+    // by one: this way is seldom taken and must not cost the other one registers)
+    auto each = [&](auto f) {
+#pragma unroll 1
+      for (int i = 0; i < NV; ++i)
+#pragma unroll 1
+        for (int j = 0; j < 8; ++j) {
+          const int col = Map::col(i, j, t);
+          if (col < cols) f(Key64{(uint64_t)order_of((float)x[col]) << 32 | (uint32_t)~(base + col)});
         }
-      },
-      [&](int place, Key64 key) { p.best[(block * p.keep) + place] = key.k; });
+    };
+    Key64 mine{};
+    each([&](Key64 key) {
+      if (mine < key) mine = key;
+    });
+    const Key64 bound = kth<Key64>(mine, p.keep, top_keys);
+    if (t == 0) count = 0;
+    __syncthreads();
+    each([&](Key64 key) {
+      if (!(key < bound)) {
+        const int to = atomicAdd(&count, 1);
+        if (to < most) list[to] = key;
+      }
+    });
+    __syncthreads();
+    n = min(count, most);
+  }
+  rank<Key64>(list, n, p.keep, [&](int place, Key64 key) { p.best[block * p.keep + place] = key.k; });
   if (t >= n && t < p.keep) p.best[block * p.keep + t] = 0;
+  m = tops[0];
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) m = fmaxf(m, tops[w]);
+  for (int w = 1; w < WAVES; ++w) m = fmaxf(m, tops[w]);
   // (NaN and +infinity come out as a sum that is NaN: fmaxf passes over a NaN, the differences do not)
-  float part[2] = {0, 0};
+  float part[4] = {0, 0, 0, 0};
   if (m != -INFINITY) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) part[j & 1] += exp_of(v[i][j] - m);
+      for (int j = 0; j < 8; ++j) part[j & 3] += __builtin_amdgcn_exp2f((v[i][j] - m) * LOG2E);
   } else {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) part[0] += v[i][j] != v[i][j] ? v[i][j] : 0.0f;
   }
-  double sum = (double)part[0] + (double)part[1];
+  double sum = ((double)part[0] + (double)part[1]) + ((double)part[2] + (double)part[3]);
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   if (lane == 0) sums[wave] = sum;
@@ -224,67 +235,118 @@ __global__ __launch_bounds__(THREADS) void beam_rows_kernel(BeamParams p) {
   }
 }
 
+// PER: candidates of a thread, held in registers
+template <int PER>
 __global__ __launch_bounds__(THREADS) void beam_join_kernel(BeamParams p) {
   extern __shared__ __align__(16) uint8_t dynamic[];
-  __shared__ Pick<KeyS> l;
+  KeyS *const list = reinterpret_cast<KeyS *>(dynamic);               // list_of(keep, PER)
+  __shared__ KeyS top_keys[THREADS + 1];
+  __shared__ uint64_t wave_top[THREADS], least;
   __shared__ double lse[BEAMS];             // NaN or -infinity: S of the beam is that throughout; 0: it is done
-  const int b = blockIdx.x, t = threadIdx.x;
+  __shared__ float score_of[BEAMS];
+  __shared__ uint8_t done_of[BEAMS];
+  __shared__ int count;
+  const int b = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int64_t row0 = (int64_t)b * p.beams;
-  for (int i = t; i < p.beams; i += THREADS) {
+  const uint32_t per_row = (uint32_t)p.splits * p.keep, all = per_row * p.beams;
+  // the candidates' logits on their way, while the sums are added up (those of beams that are done were not written: not looked at)
+  uint64_t logit[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const uint32_t c = min((uint32_t)(k * THREADS + t), all - 1);
+    logit[k] = p.best[row0 * per_row + c];
+  }
+  if (t == 0) count = 0;
+  // a wave to a beam, a lane to a workgroup's part of the row
+  for (int i = wave; i < p.beams; i += WAVES) {
     const float score = p.scores[row0 + i];
-    double of = 0;
-    if (!(score < INFINITY)) {
-      of = (double)__builtin_nanf("");
-    } else if (score == -INFINITY) {
-      of = score;
-    } else if (!(p.done && p.done[row0 + i])) {
-      const Stat *s = p.stat + (row0 + i) * p.splits;
-      float top = -INFINITY;
-      for (int j = 0; j < p.splits; ++j) top = fmaxf(top, s[j].top);
-      double sum = 0;
-      for (int j = 0; j < p.splits; ++j) sum += s[j].top == -INFINITY ? s[j].sum : s[j].sum * exp((double)s[j].top - (double)top);
-      of = sum == 0 ? -(double)INFINITY : (double)top + log(sum);
+    const bool done = p.done && p.done[row0 + i];
+    const Stat *s = p.stat + (row0 + i) * p.splits;
+    float top = -INFINITY;
+    double sum = 0;
+    if (!done) {
+      for (int j = lane; j < p.splits; j += 64) {
+        const Stat x = s[j];
+        const float now = fmaxf(top, x.top);
+        // (a part without a number above -infinity adds its sum as it is: 0, or NaN)
+        if (top != -INFINITY && now > top) sum *= exp((double)top - (double)now);
+        sum += x.top == -INFINITY || x.top == now ? x.sum : x.sum * exp((double)x.top - (double)now);
+        top = now;
+      }
+      float all_top = top;
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) all_top = fmaxf(all_top, __shfl_xor(all_top, d));
+      if (top != -INFINITY && top < all_top) sum *= exp((double)top - (double)all_top);
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+      top = all_top;
     }
-    lse[i] = of;
+    if (lane == 0) {
+      score_of[i] = score, done_of[i] = done;
+      lse[i] = !(score < INFINITY) ? (double)__builtin_nanf("") : score == -INFINITY ? (double)score : done ? 0 : sum == 0 ? -(double)INFINITY : (double)top + log(sum);
+    }
   }
   __syncthreads();
-  const uint32_t per_row = (uint32_t)p.splits * p.keep, all = per_row * p.beams;
-  auto key_of = [&](uint32_t c) -> KeyS {
-    const uint32_t i = c / per_row, in = c - i * per_row;
-    const float score = p.scores[row0 + i];
+  KeyS key[PER];
+  uint64_t largest = 0;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const uint32_t c = k * THREADS + t, i = min(p.by_row.div(c), (uint32_t)p.beams - 1), in = c - i * per_row;
+    const float score = score_of[i];
     const double of = lse[i];
-    uint64_t logit;                          // (all the same where S is the same throughout: tokens in their order)
+    const bool some = in < (uint32_t)min(p.keep, p.vocab);              // of a row whose tokens are not looked at
+    uint64_t x = logit[k];                                              // (where S is the same throughout: tokens in their order)
     double s;
     if (of != of || of == -(double)INFINITY) {
-      if (in >= (uint32_t)min(p.keep, p.vocab)) return KeyS{};
-      logit = (uint32_t)~in, s = of;
-    } else if (p.done && p.done[row0 + i]) {
-      if (in >= (uint32_t)min(p.keep, p.vocab)) return KeyS{};
-      logit = (uint32_t)~(in == 0 ? p.eos : in - (in <= (uint32_t)p.eos)), s = in == 0 ? (double)score : -(double)INFINITY;
+      x = some ? (uint32_t)~in : 0, s = of;
+    } else if (done_of[i]) {
+      x = some ? (uint32_t)~(in == 0 ? p.eos : in - (in <= (uint32_t)p.eos)) : 0, s = in == 0 ? (double)score : -(double)INFINITY;
     } else {
-      logit = p.best[(row0 + i) * per_row + in];
-      if (logit == 0) return KeyS{};
-      s = (double)score + ((double)of_order((uint32_t)(logit >> 32)) - of);
+      s = (double)score + ((double)of_order((uint32_t)(x >> 32)) - of);
     }
-    return KeyS{order_of(s), ~(uint64_t)i, logit};
+    if (c >= all) x = 0;
+    key[k] = x == 0 ? KeyS{} : KeyS{order_of(s), ~(uint64_t)i, x};
+    if (largest < key[k].s) largest = key[k].s;
+  }
+  // the keep-th largest of the threads' largest (in S alone)
+  wave_top[t] = largest;
+  if (t == 0) least = ~0ull;
+  __syncthreads();
+  int above = 0;
+#pragma unroll 8
+  for (int i = 0; i < THREADS; ++i) above += largest < wave_top[i];
+  if (above < p.keep) atomicMin((unsigned long long *)&least, (unsigned long long)largest);
+  __syncthreads();
+  const int most = list_of(p.keep, PER);
+  auto collect = [&](KeyS bound) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (key[k].real() && !(key[k] < bound)) {
+        const int at = atomicAdd(&count, 1);
+        if (at < most) list[at] = key[k];
+      }
   };
-  KeyS mine{};
-  for (uint32_t c = t; c < all; c += THREADS) {
-    const KeyS k = key_of(c);
-    if (mine < k) mine = k;
+  collect(KeyS{least, 0, 0});
+  __syncthreads();
+  int n = count;
+  if (n > most) {
+    KeyS most_of{};
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (most_of < key[k]) most_of = key[k];
+    const KeyS bound = kth<KeyS>(most_of, p.keep, top_keys);
+    if (t == 0) count = 0;
+    __syncthreads();
+    collect(bound);
+    __syncthreads();
+    n = min(count, most);
   }
   const int64_t out = (int64_t)b * p.keep;
-  pick<KeyS>(
-      l, reinterpret_cast<KeyS *>(dynamic), p.keep * each_of(all), p.keep, p.groups, mine,
-      [&](KeyS bound, auto f) {
-        if (bound.real() && mine < bound) return;
-        for (uint32_t c = t; c < all; c += THREADS) f(key_of(c));
-      },
-      [&](int place, KeyS key) {
-        p.score[out + place] = (float)of_order(key.s);
-        p.parent[out + place] = (int32_t)(row0 + (int64_t)~key.beam);
-        p.token[out + place] = (int32_t)~(uint32_t)key.logit;
-      });
+  rank<KeyS>(list, n, p.keep, [&](int place, KeyS k) {
+    p.score[out + place] = (float)of_order(k.s);
+    p.parent[out + place] = (int32_t)(row0 + (int64_t)~k.beam);
+    p.token[out + place] = (int32_t)~(uint32_t)k.logit;
+  });
 }
 
 // Pieces of 8 logits to a thread of the first launch.  The second one's work grows with the number of workgroups to a row, so a row is cut as
@@ -306,13 +368,19 @@ int splits_of(int64_t rows, int vocab, int beams, int keep) {
 template <typename T>
 void launch_rows(const BeamParams &p, int nv, hipStream_t s) {
   const dim3 grid = block_grid(p.blocks), block(THREADS);
-  const size_t lds = (size_t)p.keep * nv * 8 * sizeof(Key64);
+  const size_t lds = (size_t)list_of(p.keep, nv * 8) * sizeof(Key64);
   switch (nv) {
     case 1: hipLaunchKernelGGL((beam_rows_kernel<T, 1>), grid, block, lds, s, p); break;
     case 2: hipLaunchKernelGGL((beam_rows_kernel<T, 2>), grid, block, lds, s, p); break;
     case 4: hipLaunchKernelGGL((beam_rows_kernel<T, 4>), grid, block, lds, s, p); break;
     default: hipLaunchKernelGGL((beam_rows_kernel<T, 8>), grid, block, lds, s, p);
   }
+}
+
+template <int PER>
+void launch_join(const BeamParams &p, int batch, hipStream_t s) {
+  static_assert(CANDIDATES <= 32 * THREADS, "candidates of a thread");
+  hipLaunchKernelGGL((beam_join_kernel<PER>), dim3(batch), dim3(THREADS), (size_t)list_of(p.keep, PER) * sizeof(KeyS), s, p);
 }
 
 }  // namespace
@@ -351,14 +419,17 @@ f8_status f8_beam_step(const void *logits, const float *scores, const uint8_t *d
   const int64_t parts = rows * splits;
   Stat *stat = static_cast<Stat *>(workspace);
   const BeamParams p{logits, scores, done, score, parent, token, reinterpret_cast<uint64_t *>(stat + parts), stat, d->ld, d->beams, d->vocab, d->keep, splits,
-                     d->eos, groups, parts, FastDiv((uint32_t)splits)};
+                     d->eos, groups, parts, FastDiv((uint32_t)splits), FastDiv((uint32_t)(splits * d->keep))};
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (d->type == F8_F32) launch_rows<float>(p, nv, s);
   else if (d->type == F8_F16) launch_rows<f16>(p, nv, s);
   else launch_rows<bf16>(p, nv, s);
   const f8_status st = launch_status();
   if (st != F8_OK) return st;
-  hipLaunchKernelGGL(beam_join_kernel, dim3(d->batch), dim3(THREADS), (size_t)d->keep * each_of((uint32_t)(d->beams * splits * d->keep)) * sizeof(KeyS), s, p);
+  const int each = each_of((uint32_t)(d->beams * splits * d->keep));
+  if (each <= 4) launch_join<4>(p, d->batch, s);
+  else if (each <= 16) launch_join<16>(p, d->batch, s);
+  else launch_join<32>(p, d->batch, s);
   return launch_status();
 }
 
