@@ -745,13 +745,17 @@ def f8_beam_step(logits, scores, keep=None, done=None, eos=0, out=None, workspac
     if done is not None and done.dtype not in (torch.bool, torch.uint8):
         raise TypeError("done has to be bool or uint8")
     keep = K if keep is None else int(keep)
+    at_scores = _vector(scores, B * K, torch.float32)
     if out is None:
-        out = tuple(torch.empty((B, keep), dtype=t, device=logits.device) for t in (torch.float32, torch.int32, torch.int32))
+        score, parent = scores.new_empty((B, keep)), torch.empty((B, keep), dtype=torch.int32, device=logits.device)
+        out = (score, parent, torch.empty_like(parent))
+    elif len(out) != 3 or any(t.shape != (B, keep) or t.dtype != k or not t.is_contiguous() for t, k in zip(out, (torch.float32, torch.int32, torch.int32))):
+        raise ValueError("out has to be (float32, int32, int32) tensors [%d][%d], contiguous" % (B, keep))
     d = f8_beam_desc(B, K, V, keep, kind, eos, max(ld, V))
     L = _lib or lib()
     at_ws, n, _keep = _scratch(workspace, L.f8_beam_workspace_bytes(B, K, V, keep), logits.device)
-    rc = L.f8_beam_step(logits.data_ptr(), _vector(scores, B * K, torch.float32), _vector(done, B * K), _vector(out[0], B * keep, torch.float32),
-                        _vector(out[1], B * keep, torch.int32), _vector(out[2], B * keep, torch.int32), d, at_ws, n, _stream())
+    rc = L.f8_beam_step(logits.data_ptr(), at_scores, _vector(done, B * K), out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), d, at_ws, n,
+                        _stream())
     if rc:
         raise F8Error(rc, "f8_beam_step")
     return out
@@ -770,15 +774,18 @@ def f8_kv_fork(parent, table, lens, refs, page_size, grow=1, out=None, workspace
     tuple's tensors, none of which may be an input."""
     ld, (B, cols), dev = _int_matrix(table, "the table"), table.shape, table.device
     pages, i32 = refs.numel(), torch.int32
-    if out is None:
-        new = lambda *s: torch.empty(s, dtype=i32, device=dev)  # noqa: E731
-        out = (new(B, cols), new(B), new(pages), torch.empty((B, grow), dtype=torch.int64, device=dev), new(B, 3), new(2))
-    d = f8_kv_fork_desc(B, cols, pages, page_size, grow, ld, _int_matrix(out[0], "the table", table.shape))
+    ins = (_vector(parent, B, i32), table.data_ptr(), _vector(lens, B, i32), _vector(refs, pages, i32))
+    if out is None:                                      # (of tensors that were looked at: new_empty and empty_like take half of empty's 2 us)
+        out_ld, out = cols, (table.new_empty((B, cols)), torch.empty_like(lens), torch.empty_like(refs),
+                             torch.empty((B, grow), dtype=torch.int64, device=dev), refs.new_empty((B, 3)), refs.new_empty(2))
+    else:
+        out_ld = _int_matrix(out[0], "the table", table.shape)
+        for t, size, kind in zip(out[1:], (B, pages, B * grow, 3 * B, 2), (i32, i32, torch.int64, i32, i32)):
+            _vector(t, size, kind)
+    d = f8_kv_fork_desc(B, cols, pages, page_size, grow, ld, out_ld)
     L = _lib or lib()
     at_ws, n, _keep = _scratch(workspace, L.f8_kv_fork_workspace_bytes(B, pages), dev)
-    rc = L.f8_kv_fork(_vector(parent, B, i32), table.data_ptr(), _vector(lens, B, i32), _vector(refs, pages, i32), out[0].data_ptr(), _vector(out[1], B, i32),
-                      _vector(out[2], pages, i32), _vector(out[3], B * grow, torch.int64), _vector(out[4], 3 * B, i32), _vector(out[5], 2, i32), d, at_ws, n,
-                      _stream())
+    rc = L.f8_kv_fork(*ins, *[t.data_ptr() for t in out], d, at_ws, n, _stream())
     if rc:
         raise F8Error(rc, "f8_kv_fork")
     return out
@@ -789,14 +796,17 @@ def f8_kv_compact(table, refs, page_size, out=None, workspace=None):
     (moves, pages in use).  out: that tuple's tensors; its table may be the input's."""
     ld, (rows, cols), dev = _int_matrix(table, "the table"), table.shape, table.device
     pages, i32 = refs.numel(), torch.int32
+    at_refs = _vector(refs, pages, i32)
     if out is None:
-        new = lambda *s: torch.empty(s, dtype=i32, device=dev)  # noqa: E731
-        out = (new(rows, cols), new(pages), new(pages // 2, 3), new(2))
-    d = f8_kv_compact_desc(rows, cols, pages, page_size, ld, _int_matrix(out[0], "the table", table.shape))
+        out_ld, out = cols, (table.new_empty((rows, cols)), torch.empty_like(refs), refs.new_empty((pages // 2, 3)), refs.new_empty(2))
+    else:
+        out_ld = _int_matrix(out[0], "the table", table.shape)
+        for t, size in zip(out[1:], (pages, pages // 2 * 3, 2)):
+            _vector(t, size, i32)
+    d = f8_kv_compact_desc(rows, cols, pages, page_size, ld, out_ld)
     L = _lib or lib()
     at_ws, n, _keep = _scratch(workspace, L.f8_kv_compact_workspace_bytes(pages), dev)
-    rc = L.f8_kv_compact(table.data_ptr(), _vector(refs, pages, i32), out[0].data_ptr(), _vector(out[1], pages, i32), _vector(out[2], pages // 2 * 3, i32),
-                         _vector(out[3], 2, i32), d, at_ws, n, _stream())
+    rc = L.f8_kv_compact(table.data_ptr(), at_refs, *[t.data_ptr() for t in out], d, at_ws, n, _stream())
     if rc:
         raise F8Error(rc, "f8_kv_compact")
     return out
