@@ -19,11 +19,17 @@ namespace f8 {
 namespace {
 
 constexpr int WAVES = 4, TILE = 32, COLS = 16, UNIT = WAVES * TILE, THREADS = 64 * WAVES;
-constexpr int GROUPS_LDS = 1024;             // groups whose bounds a workgroup keeps in LDS
+constexpr int ITEMS_LDS = 512;               // groups, and requests, that a workgroup keeps in LDS
 constexpr int CUS = 256;
 // Workgroups, two to a CU where the registers allow it, and blocks of columns of a workgroup.
 constexpr int wgs_of(int dim) { return dim <= 128 ? 2 * CUS : CUS; }
 constexpr int blocks_of(int dim, int bytes) { return dim <= 64 && bytes == 2 ? 4 : 2; }
+
+// What the first launch leaves of a request for the second one: units in front of its group, tiles in front of it, its tokens and those of them that
+// its group reads, the group.  One more behind the last: the units and tiles of all.
+struct __align__(16) Record {
+  int units, tiles, len, prefix, b0, n, unused[2];
+};
 
 struct SharedParams {
   const void *q, *k, *v;
@@ -31,6 +37,8 @@ struct SharedParams {
   const int32_t *table, *lens, *first, *shared;
   void *out;
   float *part_o, *part_ml;                   // [pieces][dim] and [pieces][2]
+  Record *records;                           // [batch + 1]
+  int32_t *group_units;                      // [groups]: units in front of it
   int64_t qt, qh, ot, oh, page, token, head, spage, stoken, shead, table_ld;
   int batch, groups, heads, group, chunks, per_block, dim, pages, max_len, wgs;
   int rows;                                  // of a block: query heads of per_block requests, or some of one request's
@@ -48,38 +56,55 @@ struct SharedParams {
 struct Prefix {
   int b0, n, tokens;                         // requests b0 .. b0 + n - 1
 };
+__device__ __forceinline__ int units(int tokens) { return (int)((uint32_t)(tokens + UNIT - 1) / UNIT); }
+__device__ __forceinline__ int tiles(int tokens) { return (int)((uint32_t)(tokens + TILE - 1) / TILE); }
+__device__ __forceinline__ int blocks_of(const SharedParams &p, int requests) { return (requests + p.per_block - 1) / p.per_block * p.chunks; }
+__device__ __forceinline__ int own_chunks(const SharedParams &p) { return (p.group + COLS - 1) / COLS; }
+struct Items {                               // (in LDS)
+  int32_t first[ITEMS_LDS + 1], shared[ITEMS_LDS], lens[ITEMS_LDS], units[ITEMS_LDS];
+};
 struct Work {
   const SharedParams &p;
-  const int32_t *first;                      // (in LDS where it fits)
-  __device__ __forceinline__ int len(int b) const { return min(max(p.lens[b], 0), p.max_len); }
+  Items &lds;
+  __device__ __forceinline__ Work(const SharedParams &p, Items &lds) : p(p), lds(lds) {
+    if (p.groups <= ITEMS_LDS)
+      for (int i = threadIdx.x; i <= p.groups; i += THREADS) {
+        lds.first[i] = p.first[i];
+        if (i < p.groups) lds.shared[i] = p.shared[i];
+      }
+    if (p.batch <= ITEMS_LDS)
+      for (int i = threadIdx.x; i < p.batch; i += THREADS) lds.lens[i] = p.lens[i];
+    __syncthreads();
+  }
+  // (as an atomic, so that the compiler keeps the two kinds of memory apart: one load of either is a flat one, which all others wait for)
+  static __device__ __forceinline__ int far(const int32_t *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+  __device__ __forceinline__ int first(int g) const { return p.groups <= ITEMS_LDS ? lds.first[g] : far(p.first + g); }
+  __device__ __forceinline__ int len(int b) const { return min(max(p.batch <= ITEMS_LDS ? lds.lens[b] : far(p.lens + b), 0), p.max_len); }
   __device__ __forceinline__ Prefix prefix(int g) const {
-    const int b0 = min(max(first[g], 0), p.batch), n = min(max(first[g + 1], 0), p.batch) - b0;
-    return Prefix{b0, n, n > 1 ? min(max(p.shared[g], 0), p.max_len) : 0};
+    const int b0 = min(max(first(g), 0), p.batch), n = min(max(first(g + 1), 0), p.batch) - b0;
+    return Prefix{b0, n, n > 1 ? min(max(p.groups <= ITEMS_LDS ? lds.shared[g] : far(p.shared + g), 0), p.max_len) : 0};
   }
   // The group that request b belongs to, or -1
   __device__ __forceinline__ int group_of(int b) const {
     int lo = 0, hi = p.groups;               // the last group that begins at b or before it: in lo .. hi - 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (first[mid] <= b) lo = mid;
+      if (first(mid) <= b) lo = mid;
       else hi = mid;
     }
-    return first[lo] <= b && b < first[lo + 1] ? lo : -1;
+    return first(lo) <= b && b < first(lo + 1) ? lo : -1;
   }
   // Tokens of request b that its group reads for it: all of the prefix, or nothing where it ends inside it
   __device__ __forceinline__ int prefix_of(int b) const {
     const int g = group_of(b), n = g < 0 ? 0 : prefix(g).tokens;
     return n <= len(b) ? n : 0;
   }
-  static __device__ __forceinline__ int units(int tokens) { return (tokens + UNIT - 1) / UNIT; }
-  static __device__ __forceinline__ int tiles(int tokens) { return (tokens + TILE - 1) / TILE; }
-  __device__ __forceinline__ int blocks(int requests) const { return (requests + p.per_block - 1) / p.per_block * p.chunks; }
-  __device__ __forceinline__ int own_chunks() const { return (p.group + COLS - 1) / COLS; }
+  __device__ __forceinline__ int blocks(int requests) const { return blocks_of(p, requests); }
   __device__ __forceinline__ int64_t units_of(int g) const {
     const Prefix x = prefix(g);
     return x.tokens > 0 ? (int64_t)units(x.tokens) * p.heads * blocks(x.n) : 0;
   }
-  __device__ __forceinline__ int64_t tiles_of(int b) const { return (int64_t)tiles(len(b) - prefix_of(b)) * p.heads * own_chunks(); }
+  __device__ __forceinline__ int64_t tiles_of(int b) const { return (int64_t)tiles(len(b) - prefix_of(b)) * p.heads * own_chunks(p); }
 };
 // Pieces: of pairs in one run [2][batch][query heads] (the prefix's part, the own part), then [workgroups][2][rows] and [waves][2][COLS].
 __device__ __forceinline__ int64_t whole_at(const SharedParams &p, bool own, int b, int hq) {
@@ -89,12 +114,17 @@ __device__ __forceinline__ int64_t cut_at(const SharedParams &p, bool own, int64
   return (int64_t)2 * p.batch * p.heads * p.group + (own ? (int64_t)2 * p.wgs * p.rows + (2 * run + slot) * COLS : (2 * run + slot) * p.rows) + row;
 }
 
-__device__ __forceinline__ const int32_t *bounds(const SharedParams &p, int32_t *lds, int threads) {
-  if (p.groups > GROUPS_LDS) return p.first;
-  for (int i = threadIdx.x; i <= p.groups; i += threads) lds[i] = p.first[i];
-  __syncthreads();
-  return lds;
-}
+// `total` units in N equal runs, N a power of two, the first `more` of them one longer.
+template <int N>
+struct Equal {
+  int per, more;
+  __device__ __forceinline__ explicit Equal(int total) : per(total / N), more(total % N) {}
+  __device__ __forceinline__ int start(int i) const { return i * per + min(i, more); }
+  __device__ __forceinline__ int of(int unit) const {
+    const int longer = more * (per + 1);
+    return (int)(unit < longer ? (uint32_t)unit / (uint32_t)(per + 1) : (uint32_t)more + (uint32_t)(unit - longer) / (uint32_t)per);
+  }
+};
 
 // What a wave keeps in LDS of a tile: where its 32 rows begin, in elements, and (8-bit caches) the scales of its keys and values and the logarithms
 // of both, SMALL at least.
@@ -119,37 +149,28 @@ struct Weights<bf16> {
 
 __device__ const v4i zeros[1] = {v4i{0, 0, 0, 0}};          // keys' dimensions beyond the head's
 
-// The item (of n, of(i) units each) that unit `start` lies in, for each of R starts, all below the sum; from[r] and before[r] (in LDS) get it and the units
-// in front of it.
-template <int R, typename Of>
-__device__ __forceinline__ void find_items(int n, const int64_t (&starts)[R], Of of, int64_t (*scan)[2], int *from, int64_t *before) {
+// Two values of each thread: their sums over the threads in front, with `done` of those before them; `done` then has this round's too.
+__device__ __forceinline__ void scan_step(const int64_t (&mine)[2], int64_t (&at)[2], int64_t (&done)[2], int64_t (*lds)[2]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t done = 0;
-  for (int i0 = 0; i0 < n; i0 += THREADS) {
-    const int i = i0 + (int)threadIdx.x;
-    const int64_t mine = i < n ? of(i) : 0;
-    int64_t upto = mine;
+  int64_t upto[2] = {mine[0], mine[1]};
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t o = __shfl_up((long long)upto, d);
-      if (lane >= d) upto += o;
-    }
-    if (lane == 63) scan[wave][0] = upto;
-    __syncthreads();
-    int64_t at = done, all = 0;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t a = __shfl_up((long long)upto[0], d), b = __shfl_up((long long)upto[1], d);
+    upto[0] += lane >= d ? a : 0, upto[1] += lane >= d ? b : 0;
+  }
+  if (lane == 63) lds[wave][0] = upto[0], lds[wave][1] = upto[1];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    at[k] = done[k] + upto[k] - mine[k];
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-      if (w < wave) at += scan[w][0];
-      all += scan[w][0];
+      const int64_t o = lds[w][k];
+      at[k] += w < wave ? o : 0, done[k] += o;
     }
-    at += upto - mine;
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-      if (mine > 0 && at <= starts[r] && starts[r] < at + mine) from[r] = i, before[r] = at;
-    __syncthreads();
-    done += all;
-    if (starts[R - 1] < done) break;
+    done[k] = uniform64(done[k]);
   }
+  __syncthreads();
 }
 
 template <typename C, typename Q, int DP, int NB>
@@ -168,37 +189,71 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
   // A wave's keys, and its part of a piece when its run is over.
   union Stage {
     v4i keys[TILE * PIECES];
-    float part[COLS][DP + 1];
+    float part[COLS][DP + 4];
   };
   __shared__ Stage stage[WAVES];
   __shared__ TileRows rows[WAVES][2];
   __shared__ float ml[WAVES][NB * COLS][2];
-  __shared__ int64_t scan[WAVES][2], before[1 + WAVES];
-  __shared__ int from[1 + WAVES], found[WAVES];
+  __shared__ int64_t scan[WAVES][2];
+  __shared__ int from[1 + WAVES], before[1 + WAVES], found[WAVES];
   __shared__ v4i q_lds[BLOCKS][KS][64];
   __shared__ float q_scale_lds[BLOCKS][COLS];
-  __shared__ int32_t first_lds[GROUPS_LDS + 1];
+  __shared__ Items items;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
-  const Work work{p, bounds(p, first_lds, THREADS)};
+  const Work work(p, items);
 
-  // Units and tiles of all, and this workgroup's and its waves' runs of them
-  int64_t sum[2] = {0, 0};
-  for (int i = threadIdx.x; i < p.groups; i += THREADS) sum[0] += work.units_of(i);
-  for (int i = threadIdx.x; i < p.batch; i += THREADS) sum[1] += work.tiles_of(i);
-  wg_sum<WAVES>(sum, scan);
-  const Runs runs(uniform64(sum[0]), p.wgs), own_runs(uniform64(sum[1]), p.wgs * WAVES);
-  // (a wave's runs follow those of the same wave of the workgroups in front: with few tiles every workgroup has some)
-  const int64_t run = blockIdx.x, own_run = (int64_t)wave * p.wgs + blockIdx.x;
-  int64_t left = uniform64(runs.start(run + 1) - runs.start(run)), own_left = uniform64(own_runs.start(own_run + 1) - own_runs.start(own_run));
-  if (left > 0) {
-    const int64_t starts[1] = {runs.start(run)};
-    find_items<1>(p.groups, starts, [&](int i) { return work.units_of(i); }, scan, from, before);
+  // Units and tiles of all, and in front of each; this workgroup's and its waves' runs of them, and the items that these begin in
+  constexpr int WGS = wgs_of(DP);
+  const int most = max(p.groups, p.batch);
+  int64_t mine[2], at[2], done[2] = {0, 0};
+  auto scan_from = [&](int i0) {
+    const int i = i0 + (int)threadIdx.x;
+    mine[0] = i < p.groups ? work.units_of(i) : 0, mine[1] = i < p.batch ? work.tiles_of(i) : 0;
+    scan_step(mine, at, done, scan);
+  };
+  for (int i0 = 0; i0 < most; i0 += THREADS) {
+    scan_from(i0);
+    if (blockIdx.x == 0) {
+      const int i = i0 + (int)threadIdx.x;
+      if (i < p.groups) {
+        if (p.groups <= ITEMS_LDS) items.units[i] = (int)at[0];
+        else __hip_atomic_store(p.group_units + i, (int)at[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      if (i < p.batch) p.records[i].tiles = (int)at[1];
+    }
   }
-  {
-    int64_t starts[WAVES];
+  // (more than fits 31 bits: groups that overlap, which nothing is computed for)
+  const int all_units = done[0] <= 0x7fffffff ? (int)done[0] : 0, all_tiles = (int)done[1];
+  const Equal<WGS> runs(all_units);
+  const Equal<WGS * WAVES> own_runs(all_tiles);
+  // (a wave's runs follow those of the same wave of the workgroups in front: with few tiles every workgroup has some)
+  const int run = blockIdx.x, own_run = wave * WGS + (int)blockIdx.x;
+  int left = runs.start(run + 1) - runs.start(run), own_left = own_runs.start(own_run + 1) - own_runs.start(own_run);
+  auto find = [&](int i0) {
+    const int i = i0 + (int)threadIdx.x, start = runs.start(run);
+    if (at[0] <= start && start < at[0] + mine[0]) from[0] = i, before[0] = (int)at[0];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) starts[w] = own_runs.start((int64_t)w * p.wgs + blockIdx.x);
-    find_items<WAVES>(p.batch, starts, [&](int i) { return work.tiles_of(i); }, scan, from + 1, before + 1);
+    for (int w = 0; w < WAVES; ++w) {
+      const int start = own_runs.start(w * WGS + (int)blockIdx.x);
+      if (at[1] <= start && start < at[1] + mine[1]) from[1 + w] = i, before[1 + w] = (int)at[1];
+    }
+  };
+  if (most <= THREADS) {
+    find(0);
+  } else {
+    done[0] = done[1] = 0;
+    for (int i0 = 0; i0 < most; i0 += THREADS) scan_from(i0), find(i0);
+  }
+  __syncthreads();
+  if (blockIdx.x == 0) {
+    for (int b = threadIdx.x; b < p.batch; b += THREADS) {
+      const int g = work.group_of(b), len = work.len(b);
+      const Prefix x = g < 0 ? Prefix{b, 1, 0} : work.prefix(g);
+      Record &r = p.records[b];
+      r.units = g < 0 ? 0 : p.groups <= ITEMS_LDS ? items.units[g] : work.far(p.group_units + g);
+      r.len = len, r.prefix = x.tokens <= len ? x.tokens : 0, r.b0 = x.b0, r.n = x.n;
+    }
+    if (threadIdx.x == 0) p.records[p.batch].units = all_units, p.records[p.batch].tiles = all_tiles;
   }
 
   v4f o[NB][E];
@@ -211,15 +266,16 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
       for (int e = 0; e < E; ++e) o[nb][e] = v4f{0, 0, 0, 0};
     }
   };
-  // 16 query heads as columns into block nb of LDS; `src`: of the lane's column, nullptr for none
-  auto put_queries = [&](int nb, const Q *src) {
-    const Q *from = src ? src : static_cast<const Q *>(p.q);
-    v4i raw[KS];
+  // 16 query heads as columns, on their way and then into block nb of LDS (`real`: the lane's column is one)
+  v4i raw[KS];
+  auto load_queries = [&](const Q *src) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const int d = S8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
-      __builtin_memcpy(&raw[s], from + (d < p.dim ? d : 0), 16);
+      __builtin_memcpy(&raw[s], src + (d < p.dim ? d : 0), 16);
     }
+  };
+  auto put_queries = [&](int nb, bool real) __attribute__((always_inline)) {
     float f[KS][8], scale = fabsf(p.scale);
     uint32_t top = 0;
 #pragma unroll
@@ -228,7 +284,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
       unpack8<Q>(&raw[s], f[s]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        f[s][j] = src && d < p.dim ? (p.scale < 0 ? -f[s][j] : f[s][j]) : 0.0f;
+        f[s][j] = real && d < p.dim ? (p.scale < 0 ? -f[s][j] : f[s][j]) : 0.0f;
         top = max(top, magnitude(f[s][j]));
       }
     }
@@ -259,9 +315,13 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
   // The tiles at t0, t0 + step .. below `end` of a row of the table, for N blocks of columns from block q0 of LDS on (all of these the same for a
   // wave).  No branch between a tile's products, and none over lanes: the compiler (ROCm 7.2) has put copies of what lives across the loop
   // into the block behind such a branch before that block had all its lanes back.
-  auto walk = [&](auto blocks_used, const int32_t *table, int kvh, int t0, int step, int end, int q0) {
+  // `ready` is called when the first rows are on their way: it waits for the queries.
+  auto walk = [&](auto blocks_used, const int32_t *table, int kvh, int t0, int step, int end, int q0, auto ready) {
     constexpr int N = decltype(blocks_used)::value;
-    if (t0 >= end) return;
+    if (t0 >= end) {
+      ready();
+      return;
+    }
     const C *const kbase = static_cast<const C *>(p.k) + kvh * p.head, *const vbase = static_cast<const C *>(p.v) + kvh * p.head;
     const int dv = c16 * E < p.dim ? c16 * E : 0;
     // Keys come as they lie in memory, rows of neighbouring lanes, and become the product's left operand in LDS: its lanes hold 16 bytes of 16 rows each, which
@@ -319,6 +379,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
       load_keys(rows[wave][0].at);
       int page = look_up(t0 + step);          // (in the order of the loop below)
       load_values(rows[wave][0].at);
+      ready();
       for (;;) {
         const uint32_t now = there;
         stage_keys();
@@ -451,12 +512,12 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
 
   // ---- prefixes ----
   int item = left > 0 ? __builtin_amdgcn_readfirstlane(from[0]) : 0;
-  int64_t in = left > 0 ? uniform64(runs.start(run) - before[0]) : 0;        // units of the item in front of this run
+  int in = left > 0 ? __builtin_amdgcn_readfirstlane(runs.start(run) - before[0]) : 0;        // units of the item in front of this run
   while (left > 0) {
     // requests b0 + req0 .., `heads` query heads of cache head kvh each, over tokens of the row `leader` of the table
     const Prefix x = work.prefix(item);
     const int b0 = __builtin_amdgcn_readfirstlane(x.b0), n = __builtin_amdgcn_readfirstlane(x.n), tokens = __builtin_amdgcn_readfirstlane(x.tokens);
-    const int units = work.units(tokens), blocks = work.blocks(n);
+    const int item_units = units(tokens), blocks = work.blocks(n);
     int leader = b0, t_end = tokens;
     if (work.len(leader) < tokens) {
       // (an empty place in front) the first member that has all of the prefix; without any nobody reads what comes out
@@ -473,38 +534,41 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
       leader = __builtin_amdgcn_readfirstlane(have);
       if (leader == 0x7fffffff) leader = b0, t_end = 0;
     }
-    const int pair = __builtin_amdgcn_readfirstlane((int)(in / units)), unit = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)pair * units));
+    const int pair = __builtin_amdgcn_readfirstlane((int)((uint32_t)in / (uint32_t)item_units)), unit = in - pair * item_units;
     const int kvh = pair / blocks, block = pair - kvh * blocks, chunk = block % p.chunks, req0 = block / p.chunks * p.per_block;
     const int h0 = chunk * p.rows, heads = p.chunks > 1 ? min(p.rows, p.group - h0) : p.group;
     const int real_rows = __builtin_amdgcn_readfirstlane(min(n - req0, p.per_block) * heads), nb_used = (real_rows + COLS - 1) / COLS;
-    const int last = (int)min((int64_t)units, unit + left), end = min(t_end, last * UNIT);
+    const int last = min(item_units, unit + left), end = min(t_end, last * UNIT);
     auto place = [&](int row, int &b, int &hq) {             // of a row of the block
       const int r = p.chunks > 1 ? 0 : (int)p.by_group.div((uint32_t)row);
       b = b0 + req0 + r, hq = kvh * p.group + h0 + row - r * heads;
     };
-    for (int nb = wave; nb < nb_used; nb += WAVES) {
-      const int row = nb * COLS + c16;
+    const int row0 = wave * COLS + c16;
+    {
       int b, hq;
-      place(min(row, real_rows - 1), b, hq);
-      put_queries(nb, row < real_rows ? static_cast<const Q *>(p.q) + b * p.qt + hq * p.qh : nullptr);
+      place(min(row0, real_rows - 1), b, hq);
+      load_queries(static_cast<const Q *>(p.q) + b * p.qt + hq * p.qh);
     }
-    __syncthreads();
+    auto ready = [&]() {
+      if (wave < nb_used) put_queries(wave, row0 < real_rows);
+      __syncthreads();
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) q_scale[nb] = q_scale_lds[nb][c16];
-    clear();
+      for (int nb = 0; nb < NB; ++nb) q_scale[nb] = q_scale_lds[nb][c16];
+      clear();
+    };
     const int32_t *table = p.table + leader * p.table_ld;
     const int t0 = unit * UNIT + wave * TILE;
     if constexpr (NB >= 4) {
-      if (nb_used > 2) walk(std::integral_constant<int, 4>(), table, kvh, t0, UNIT, end, 0);
-      else if (nb_used > 1) walk(std::integral_constant<int, 2>(), table, kvh, t0, UNIT, end, 0);
-      else walk(std::integral_constant<int, 1>(), table, kvh, t0, UNIT, end, 0);
+      if (nb_used > 2) walk(std::integral_constant<int, 4>(), table, kvh, t0, UNIT, end, 0, ready);
+      else if (nb_used > 1) walk(std::integral_constant<int, 2>(), table, kvh, t0, UNIT, end, 0, ready);
+      else walk(std::integral_constant<int, 1>(), table, kvh, t0, UNIT, end, 0, ready);
     } else {
-      if (nb_used > 1) walk(std::integral_constant<int, 2>(), table, kvh, t0, UNIT, end, 0);
-      else walk(std::integral_constant<int, 1>(), table, kvh, t0, UNIT, end, 0);
+      if (nb_used > 1) walk(std::integral_constant<int, 2>(), table, kvh, t0, UNIT, end, 0, ready);
+      else walk(std::integral_constant<int, 1>(), table, kvh, t0, UNIT, end, 0, ready);
     }
 
     // the waves join in LDS, 16 columns at a time, and leave the piece
-    const bool whole = unit == 0 && last == units;
+    const bool whole = unit == 0 && last == item_units;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       if (nb >= nb_used) continue;
@@ -521,32 +585,41 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
       for (int w = 1; w < WAVES; ++w) top = fmaxf(top, ml[w][nb * COLS + c16][0]);
       const float shrink = __builtin_amdgcn_exp2f(m[nb] - (top == -INFINITY ? 0.0f : top));
 #pragma unroll
-      for (int e = 0; e < E; ++e)
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) stage[wave].part[c16][(4 * g + j) * E + e] = o[nb][e][j] * shrink;
+        for (int e = 0; e < E; e += 4)
+          *reinterpret_cast<v4f *>(&stage[wave].part[c16][(4 * g + j) * E + e]) =
+              v4f{o[nb][e][j] * shrink, o[nb][e + 1][j] * shrink, o[nb][e + 2][j] * shrink, o[nb][e + 3][j] * shrink};
       __syncthreads();
-      for (int i = threadIdx.x; i < COLS * DP; i += THREADS) {
-        const int c = i / DP, d = i % DP, row = nb * COLS + c;
-        if (row >= real_rows || d >= p.dim) continue;
-        float mh = ml[0][row][0], sum = 0.0f, of = 0.0f;
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) mh = fmaxf(mh, ml[w][row][0]);
-        const float base = mh == -INFINITY ? 0.0f : mh;
+      for (int i = threadIdx.x; i < COLS * DP / 4; i += THREADS) {
+        const int c = i / (DP / 4), d = i % (DP / 4) * 4, row = nb * COLS + c;
+        if (row >= real_rows || d >= p.dim) continue;
+        v4f of{0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-          sum += ml[w][row][1] * __builtin_amdgcn_exp2f(ml[w][row][0] - base);
-          of += stage[w].part[c][d];
+          const v4f x = *reinterpret_cast<const v4f *>(&stage[w].part[c][d]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) of[k] += x[k];
         }
         int b, hq;
         place(row, b, hq);
         const int64_t at = whole ? whole_at(p, false, b, hq) : cut_at(p, false, run, unit == 0, row);
-        p.part_o[at * p.dim + d] = of;
-        if (d == 0) p.part_ml[2 * at] = mh, p.part_ml[2 * at + 1] = sum;
+        *reinterpret_cast<v4f *>(p.part_o + at * p.dim + d) = of;
+        if (d == 0) {
+          float mh = ml[0][row][0], sum = 0.0f;
+#pragma unroll
+          for (int w = 1; w < WAVES; ++w) mh = fmaxf(mh, ml[w][row][0]);
+          const float base = mh == -INFINITY ? 0.0f : mh;
+#pragma unroll
+          for (int w = 0; w < WAVES; ++w) sum += ml[w][row][1] * __builtin_amdgcn_exp2f(ml[w][row][0] - base);
+          p.part_ml[2 * at] = mh, p.part_ml[2 * at + 1] = sum;
+        }
       }
       __syncthreads();
     }
     left -= last - unit, in += last - unit;
-    if (left > 0 && in == (int64_t)units * blocks * p.heads) {                // the next group that has units
+    if (left > 0 && in == item_units * blocks * p.heads) {                // the next group that has units
       in = 0;
       do ++item;
       while (work.units_of(item) == 0);
@@ -556,24 +629,27 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
 
   // ---- own tokens, every wave for itself ----
   int b = own_left > 0 ? __builtin_amdgcn_readfirstlane(from[1 + wave]) : 0;
-  in = own_left > 0 ? uniform64(own_runs.start(own_run) - before[1 + wave]) : 0;
-  const int own_chunks = work.own_chunks();
+  in = own_left > 0 ? __builtin_amdgcn_readfirstlane(own_runs.start(own_run) - before[1 + wave]) : 0;
+  const int chunks = own_chunks(p);
   while (own_left > 0) {
     const int t_begin = __builtin_amdgcn_readfirstlane(work.prefix_of(b)), len = __builtin_amdgcn_readfirstlane(work.len(b));
-    const int tiles = work.tiles(len - t_begin);
-    const int pair = __builtin_amdgcn_readfirstlane((int)(in / tiles)), tile = __builtin_amdgcn_readfirstlane((int)(in - (int64_t)pair * tiles));
-    const int kvh = pair / own_chunks, h0 = (pair - kvh * own_chunks) * COLS, heads = min(COLS, p.group - h0), hq = kvh * p.group + h0 + c16;
-    const int last = (int)min((int64_t)tiles, tile + own_left);
-    lanes_meet();
-    put_queries(wave, c16 < heads ? static_cast<const Q *>(p.q) + b * p.qt + hq * p.qh : nullptr);
-    lanes_meet();
-    q_scale[0] = q_scale_lds[wave][c16];
-    clear();
-    walk(std::integral_constant<int, 1>(), p.table + b * p.table_ld, kvh, t_begin + tile * TILE, TILE, min(len, t_begin + last * TILE), wave);
+    const int own_tiles = tiles(len - t_begin);
+    const int pair = __builtin_amdgcn_readfirstlane((int)((uint32_t)in / (uint32_t)own_tiles)), tile = in - pair * own_tiles;
+    const int kvh = pair / chunks, h0 = (pair - kvh * chunks) * COLS, heads = min(COLS, p.group - h0), hq = kvh * p.group + h0 + min(c16, heads - 1);
+    const int last = min(own_tiles, tile + own_left);
+    load_queries(static_cast<const Q *>(p.q) + b * p.qt + hq * p.qh);
+    auto ready = [&]() {
+      lanes_meet();
+      put_queries(wave, c16 < heads);
+      lanes_meet();
+      q_scale[0] = q_scale_lds[wave][c16];
+      clear();
+    };
+    walk(std::integral_constant<int, 1>(), p.table + b * p.table_ld, kvh, t_begin + tile * TILE, TILE, min(len, t_begin + last * TILE), wave, ready);
     l[0] += __shfl_xor(l[0], 16);
     l[0] += __shfl_xor(l[0], 32);
     if (c16 < heads) {
-      const int64_t at = tile == 0 && last == tiles ? whole_at(p, true, b, hq) : cut_at(p, true, own_run, tile == 0, c16);
+      const int64_t at = tile == 0 && last == own_tiles ? whole_at(p, true, b, hq) : cut_at(p, true, own_run, tile == 0, c16);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int d = (4 * g + j) * E;          // (dim is a multiple of 16 and so of E)
@@ -586,7 +662,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
       if (g == 0) p.part_ml[2 * at] = m[0], p.part_ml[2 * at + 1] = l[0];
     }
     own_left -= last - tile, in += last - tile;
-    if (own_left > 0 && in == (int64_t)tiles * own_chunks * p.heads) {         // the next request that has tiles
+    if (own_left > 0 && in == own_tiles * chunks * p.heads) {         // the next request that has tiles
       in = 0;
       do ++b;
       while (work.tiles_of(b) == 0);
@@ -599,13 +675,10 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
 // its query heads, 4 neighbours a thread and as many pieces at a time as threads are left; the pieces are added up in a fixed order.
 constexpr int JOINERS = 4, JOIN_PART = 256, JOIN_VECS = JOIN_PART / 4, JOIN_AT_ONCE = 64 * JOINERS / JOIN_VECS;
 
-template <typename Q>
+template <typename Q, int WGS>
 __global__ __launch_bounds__(64 * JOINERS) void join_shared_kernel(SharedParams p) {
   __shared__ v4f part[JOIN_AT_ONCE][JOIN_VECS];
   __shared__ float sums[JOIN_AT_ONCE][JOIN_VECS], tops[JOIN_AT_ONCE][JOIN_VECS];
-  __shared__ int64_t scan[JOINERS][2];
-  __shared__ int32_t first_lds[GROUPS_LDS + 1];
-  const Work work{p, bounds(p, first_lds, 64 * JOINERS)};
   const int per_b = p.heads * p.chunks, b = blockIdx.x / per_b, hc = blockIdx.x % per_b, kvh = hc / p.chunks, chunk = hc % p.chunks;
   const int h0 = chunk * p.rows, heads = p.chunks > 1 ? min(p.rows, p.group - h0) : p.group;
   const int vec = (int)threadIdx.x % JOIN_VECS, mine = (int)threadIdx.x / JOIN_VECS;
@@ -613,38 +686,22 @@ __global__ __launch_bounds__(64 * JOINERS) void join_shared_kernel(SharedParams 
   const int e = blockIdx.y * JOIN_PART + vec * 4, h = e / p.dim, d = e - h * p.dim;
   const bool real = h < heads;
   const int hq = kvh * p.group + h0 + (real ? h : 0), col = real ? d : 0;
-  // units in front of the group, tiles in front of the request, and all of them
-  const int g = work.group_of(b), prefix = work.prefix_of(b);
-  const Prefix x = g < 0 ? Prefix{0, 0, 0} : work.prefix(g);
-  int64_t sum[2] = {0, 0}, front[2] = {0, 0};
-  for (int i = threadIdx.x; i < p.groups; i += 64 * JOINERS) {
-    const int64_t u = work.units_of(i);
-    sum[0] += u;
-    if (i < g) front[0] += u;
-  }
-  for (int i = threadIdx.x; i < p.batch; i += 64 * JOINERS) {
-    const int64_t u = work.tiles_of(i);
-    sum[1] += u;
-    if (i < b) front[1] += u;
-  }
-  wg_sum<JOINERS>(sum, scan);
-  wg_sum<JOINERS>(front, scan);
+  const Record x = p.records[b], all = p.records[p.batch];
   // pieces of the prefix's pair and of the own one
   struct Pieces {
     int64_t first, rest, step;                // rows of piece 0 and 1, and from there to the next
     int n;
   };
-  auto pieces = [&](const Runs &runs, int64_t at, int units, bool own, int row) {
+  auto pieces = [&](const auto &runs, int at, int units, bool own, int row) {
     if (units == 0) return Pieces{0, 0, 0, 0};
-    const int64_t i0 = runs.of(at), i1 = runs.of(at + units - 1);
+    const int i0 = runs.of(at), i1 = runs.of(at + units - 1);
     if (i0 == i1) return Pieces{whole_at(p, own, b, hq), 0, 0, 1};
-    return Pieces{cut_at(p, own, i0, 1, row), cut_at(p, own, i0 + 1, 0, row), 2 * (own ? COLS : p.rows), (int)(i1 - i0) + 1};
+    return Pieces{cut_at(p, own, i0, 1, row), cut_at(p, own, i0 + 1, 0, row), 2 * (own ? COLS : p.rows), i1 - i0 + 1};
   };
-  const int pu = prefix > 0 ? work.units(prefix) : 0, ot = work.tiles(work.len(b) - prefix), in_group = h0 + (real ? h : 0);
-  const int blocks = work.blocks(x.n), block = (b - x.b0) / p.per_block * p.chunks + chunk;
-  const Pieces a = pieces(Runs(uniform64(sum[0]), p.wgs), uniform64(front[0] + ((int64_t)kvh * blocks + block) * pu), pu, false,
-                          (b - x.b0) % p.per_block * heads + (real ? h : 0));
-  const Pieces c = pieces(Runs(uniform64(sum[1]), p.wgs * WAVES), front[1] + ((int64_t)kvh * work.own_chunks() + in_group / COLS) * ot, ot, true, in_group % COLS);
+  const int pu = x.prefix > 0 && all.units > 0 ? units(x.prefix) : 0, ot = tiles(x.len - x.prefix), in_group = h0 + (real ? h : 0);
+  const int blocks = blocks_of(p, x.n), block = (b - x.b0) / p.per_block * p.chunks + chunk;
+  const Pieces a = pieces(Equal<WGS>(all.units), x.units + (kvh * blocks + block) * pu, pu, false, (b - x.b0) % p.per_block * heads + (real ? h : 0));
+  const Pieces c = pieces(Equal<WGS * WAVES>(all.tiles), x.tiles + (kvh * own_chunks(p) + in_group / COLS) * ot, ot, true, in_group % COLS);
   const int n = a.n + c.n;
   auto row_of = [&](int i) {
     const Pieces &k = i < a.n ? a : c;
@@ -693,21 +750,24 @@ __global__ __launch_bounds__(64 * JOINERS) void join_shared_kernel(SharedParams 
   for (int k = 0; k < 4; ++k) out[k] = (Q)(total == 0.0f ? 0.0f : o[k] / total);
 }
 
-template <typename C, typename Q>
-f8_status launch(const SharedParams &p, hipStream_t s) {
-  const dim3 grid(p.wgs), block(THREADS);
-  if (p.dim <= 64) hipLaunchKernelGGL((attend_shared_kernel<C, Q, 64, blocks_of(64, sizeof(C))>), grid, block, 0, s, p);
-  else if (p.dim <= 128) hipLaunchKernelGGL((attend_shared_kernel<C, Q, 128, blocks_of(128, sizeof(C))>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((attend_shared_kernel<C, Q, 256, blocks_of(256, sizeof(C))>), grid, block, 0, s, p);
+template <typename C, typename Q, int DP>
+f8_status launch_dim(const SharedParams &p, hipStream_t s) {
+  hipLaunchKernelGGL((attend_shared_kernel<C, Q, DP, blocks_of(DP, sizeof(C))>), dim3(p.wgs), dim3(THREADS), 0, s, p);
   const f8_status st = launch_status();
   if (st != F8_OK) return st;
   const int elements = (p.chunks > 1 ? p.rows : p.group) * p.dim;
-  hipLaunchKernelGGL(join_shared_kernel<Q>, dim3(p.batch * p.heads * p.chunks, (elements + JOIN_PART - 1) / JOIN_PART), dim3(64 * JOINERS), 0, s, p);
+  hipLaunchKernelGGL((join_shared_kernel<Q, wgs_of(DP)>), dim3(p.batch * p.heads * p.chunks, (elements + JOIN_PART - 1) / JOIN_PART), dim3(64 * JOINERS), 0, s, p);
   return launch_status();
 }
+template <typename C, typename Q>
+f8_status launch(const SharedParams &p, hipStream_t s) {
+  return p.dim <= 64 ? launch_dim<C, Q, 64>(p, s) : p.dim <= 128 ? launch_dim<C, Q, 128>(p, s) : launch_dim<C, Q, 256>(p, s);
+}
 
-// Where a request's tokens fit one launch of f8_attend_paged, that is the faster way.
-bool alone(int groups, int max_len) { return groups == 0 || max_len <= 4 * UNIT; }
+// Where a request's tokens fit one launch of f8_attend_paged, that is the faster way (and it counts in 64 bits).
+bool alone(int batch, int groups, int q_heads, int max_len) {
+  return groups == 0 || max_len <= 4 * UNIT || ((int64_t)max_len + TILE - 1) / TILE * batch * q_heads > 0x7fffffff;
+}
 size_t pieces_of(int64_t batch, int q_heads, int dim) { return (size_t)2 * batch * q_heads + (size_t)2 * wgs_of(dim) * (blocks_of(dim, 2) + WAVES) * COLS; }
 
 }  // namespace
@@ -719,8 +779,8 @@ extern "C" {
 
 size_t f8_attend_shared_workspace_bytes(int batch, int groups, int q_heads, int kv_heads, int dim, int max_len) {
   if (batch < 1 || groups < 0 || q_heads < 1 || kv_heads < 1 || dim < 1 || max_len < 1 || q_heads % kv_heads != 0) return 0;
-  if (alone(groups, max_len)) return f8_attend_workspace_bytes(batch, q_heads, kv_heads, dim, max_len);
-  return pieces_of(batch, q_heads, dim) * (dim + 2) * sizeof(float);
+  if (alone(batch, groups, q_heads, max_len)) return f8_attend_workspace_bytes(batch, q_heads, kv_heads, dim, max_len);
+  return ((size_t)batch + 1) * sizeof(Record) + pieces_of(batch, q_heads, dim) * (dim + 2) * sizeof(float) + groups * sizeof(int32_t);
 }
 
 f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cache, const float *k_scale, const float *v_scale,
@@ -732,7 +792,7 @@ f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cac
   if (st != F8_OK) return st;
   if (d->batch > 0 && groups > 0 && (!first || !shared)) return F8_ERR_NULL;
   if (!aligned_to(first, 4) || !aligned_to(shared, 4)) return F8_ERR_ALIGN;
-  if (d->batch == 0 || alone(groups, d->max_len))
+  if (d->batch == 0 || alone(d->batch, groups, d->q_heads, d->max_len))
     return f8_attend_paged(q, k_cache, v_cache, k_scale, v_scale, table, lens, out, c, d, workspace, workspace_bytes, stream);
   st = check_attend_pointers(q, k_cache, v_cache, k_scale, v_scale, table, lens, out, *c, *d);
   if (st != F8_OK) return st;
@@ -741,8 +801,11 @@ f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cac
   if (!workspace) return F8_ERR_NULL;
   if (!aligned_to(workspace, 16)) return F8_ERR_ALIGN;
   if (workspace_bytes < f8_attend_shared_workspace_bytes(d->batch, groups, d->q_heads, c->heads, c->dim, d->max_len)) return F8_ERR_SHAPE;
-  float *ws = static_cast<float *>(workspace);
-  const SharedParams p{q, k_cache, v_cache, k_scale, v_scale, table, lens, first, shared, out, ws, ws + pieces_of(d->batch, d->q_heads, c->dim) * c->dim,
+  Record *records = static_cast<Record *>(workspace);
+  const size_t pieces = pieces_of(d->batch, d->q_heads, c->dim);
+  float *ws = reinterpret_cast<float *>(records + d->batch + 1);
+  const SharedParams p{q, k_cache, v_cache, k_scale, v_scale, table, lens, first, shared, out, ws, ws + pieces * c->dim,
+                       records, reinterpret_cast<int32_t *>(ws + pieces * (c->dim + 2)),
                        d->q_token, d->q_head, d->o_token, d->o_head, c->page_stride, c->token_stride, c->head_stride,
                        c->scale_page, c->scale_token, c->scale_head, d->table_ld, d->batch, groups, c->heads, group, chunks,
                        chunks > 1 ? 1 : most / group, c->dim, c->pages, d->max_len, wgs_of(c->dim), most, FastDiv((uint32_t)c->page_size), FastDiv((uint32_t)group),
