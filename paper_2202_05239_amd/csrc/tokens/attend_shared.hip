@@ -126,7 +126,7 @@ struct Equal {
   }
 };
 
-// What a wave keeps in LDS of a tile: where its 32 rows begin, in elements, and (8-bit caches) the scales of its keys and values and the logarithms
+// What a wave keeps in LDS of a tile: where its 32 rows begin, in bytes, and (8-bit caches) the scales of its keys and values and the logarithms
 // of both, SMALL at least.
 struct TileRows {
   int64_t at[TILE];
@@ -193,6 +193,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
   };
   __shared__ Stage stage[WAVES];
   __shared__ TileRows rows[WAVES][2];
+  __shared__ int64_t no_rows[TILE];                       // for dimensions beyond the head's: where `zeros` lies
   __shared__ float ml[WAVES][NB * COLS][2];
   __shared__ int64_t scan[WAVES][2];
   __shared__ int from[1 + WAVES], before[1 + WAVES], found[WAVES];
@@ -200,6 +201,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
   __shared__ float q_scale_lds[BLOCKS][COLS];
   __shared__ Items items;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
+  if (threadIdx.x < TILE) no_rows[threadIdx.x] = reinterpret_cast<int64_t>(zeros);
   const Work work(p, items);
 
   // Units and tiles of all, and in front of each; this workgroup's and its waves' runs of them, and the items that these begin in
@@ -323,38 +325,40 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
       return;
     }
     const C *const kbase = static_cast<const C *>(p.k) + kvh * p.head, *const vbase = static_cast<const C *>(p.v) + kvh * p.head;
-    const int dv = c16 * E < p.dim ? c16 * E : 0;
+    const char *const value_base = reinterpret_cast<const char *>(vbase + (c16 * E < p.dim ? c16 * E : 0));
     // Keys come as they lie in memory, rows of neighbouring lanes, and become the product's left operand in LDS: its lanes hold 16 bytes of 16 rows each, which
     // the load unit would take a row at a time (a quarter of the rate).  A row's pieces are permuted by its number: no 16 rows' pieces share banks.
     auto turned = [](int row) { return PIECES >= 16 ? row & 15 : PIECES == 8 ? row & 7 : row >> 1 & 3; };
     const int key_row = lane / PIECES, key_piece = lane % PIECES;             // of load 0; load n is n * 64 / PIECES rows further
     const bool key_real = key_piece * (16 / (int)sizeof(C)) < p.dim;
-    const int64_t key_on = key_real ? -1 : 0, key_from = key_real ? key_piece * 16 : reinterpret_cast<const char *>(zeros) - reinterpret_cast<const char *>(kbase);
+    // (a lane of such dimensions takes its places from no_rows)
+    const int64_t key_base = key_real ? reinterpret_cast<int64_t>(kbase) + key_piece * 16 : 0;
     v4i *const keys = stage[wave].keys;
     // The next tile's keys are on their way from when this one's are in LDS, its values from when this one's have been summed up.  All loads are issued whether there is a next tile or not (a token that
     // does not exist reads row 0 of the cache): behind a branch around a load nobody knows how many are on their way, and the wait is for all.
     v4i k[KI];
     Raw<VB> v[8];
     float tile_scale = 1.0f;                  // lanes 0..31: of the key of token `lane`, 32..63: of the value of token `lane - 32`
-    uint32_t there;                           // its tokens that exist
+    int64_t scale_at = 0;                     // where the next tile's lies
+    uint32_t there, then;                     // tokens of this tile and of the next one that exist
     auto look_up = [&](int t0) {              // page of token lane % 32 of the tile at t0, where there is one
       return table[p.page_size.div((uint32_t)min(t0 + (lane & 31), end - 1))];
     };
     auto locate = [&](int t0, int page, int64_t (&at_lds)[TILE]) {
       const uint32_t tok = (uint32_t)(t0 + (lane & 31)), place = tok - p.page_size.div(tok) * p.page_size.d;
       const bool real = (int)tok < end && (uint32_t)page < (uint32_t)p.pages;
-      // (selected, not branched to, and written by both halves of the wave: see below)
+      // (selected, not branched to, and written by both halves of the wave: see above)
       const int64_t pg = real ? page : 0, pl = real ? (int)place : 0;
-      at_lds[lane & 31] = pg * p.page + pl * p.token;
-      lanes_meet();
-      if constexpr (S8) tile_scale = (lane < 32 ? p.k_scale : p.v_scale)[pg * p.spage + pl * p.stoken + kvh * p.shead];
+      at_lds[lane & 31] = (pg * p.page + pl * p.token) * (int64_t)sizeof(C);
+      if constexpr (S8) scale_at = pg * p.spage + pl * p.stoken + kvh * p.shead;
       return (uint32_t)__ballot(real);
     };
     auto load_keys = [&](const int64_t (&at_lds)[TILE]) {
+      if constexpr (S8) tile_scale = (lane < 32 ? p.k_scale : p.v_scale)[scale_at];
+      const int64_t *const at = key_real ? at_lds : no_rows;
 #pragma unroll
       for (int n = 0; n < KI; ++n) {
-        const int64_t row = at_lds[n * (64 / PIECES) + key_row] * (int64_t)sizeof(C);
-        k[n] = *reinterpret_cast<const v4i *>(reinterpret_cast<const char *>(kbase) + ((row & key_on) + key_from));
+        k[n] = *(const __attribute__((address_space(1))) v4i *)(key_base + at[n * (64 / PIECES) + key_row]);
       }
     };
     auto stage_keys = [&]() {
@@ -364,29 +368,32 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
         const int row = n * (64 / PIECES) + key_row;
         keys[row * PIECES + (key_piece ^ turned(row))] = k[n];
       }
-      lanes_meet();
     };
     auto key = [&](int h, int i) { return keys[(16 * h + c16) * PIECES + ((i * 4 + g) ^ turned(c16))]; };
     auto load_values = [&](const int64_t (&at_lds)[TILE]) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[4 * h + j] = load_raw<VB>(vbase + at_lds[16 * h + 4 * g + j] + dv);
+        for (int j = 0; j < 4; ++j) v[4 * h + j] = load_raw<VB>(value_base + at_lds[16 * h + 4 * g + j]);
     };
 
+      // A tile's places are looked up two tiles ahead and worked out one ahead, while the first product runs.
       int buf = 0;
       there = locate(t0, look_up(t0), rows[wave][0].at);
+      lanes_meet();
       load_keys(rows[wave][0].at);
       int page = look_up(t0 + step);          // (in the order of the loop below)
       load_values(rows[wave][0].at);
       ready();
+      then = locate(t0 + step, page, rows[wave][1].at);
+      page = look_up(t0 + 2 * step);
       for (;;) {
         const uint32_t now = there;
-        stage_keys();
+        there = then;
         const float now_scale = tile_scale;
-        there = locate(t0 + step, page, rows[wave][buf ^ 1].at);
+        stage_keys();
         load_keys(rows[wave][buf ^ 1].at);
-        page = look_up(t0 + 2 * step);
+        lanes_meet();
         v4f ks[2], vs[2], vl[2];
         if constexpr (S8) {
           float *const scale_lds = rows[wave][buf].scale;
@@ -427,6 +434,8 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
               for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(d, q_lds[q0 + nb][i][lane], acc[nb][h]);
             }
           }
+        then = locate(t0 + 2 * step, page, rows[wave][buf].at);
+        page = look_up(t0 + 3 * step);
         if (now != 0xffffffffu) {
 #pragma unroll
           for (int h = 0; h < 2; ++h)
@@ -477,7 +486,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
           for (int j = 0; j < 8; ++j) {
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[nb][j >> 2][j & 3], S8 ? q_scale[nb] * ks[j >> 2][j & 3] : q_scale[nb], -below));
             l[nb] += w;
-            wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : w + Wt::LEAST);
+            wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : Wt::LEAST > 0 ? w + Wt::LEAST : w);
           }
           pt[nb] = __builtin_bit_cast(v4i, wh);
         }
