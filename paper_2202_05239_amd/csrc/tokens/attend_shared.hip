@@ -22,8 +22,8 @@ constexpr int WAVES = 4, TILE = 32, COLS = 16, UNIT = WAVES * TILE, THREADS = 64
 constexpr int ITEMS_LDS = 512;               // groups, and requests, that a workgroup keeps in LDS
 constexpr int CUS = 256;
 // Workgroups, two to a CU where the registers allow it, and blocks of columns of a workgroup.
-constexpr int wgs_of(int dim) { return dim <= 128 ? 2 * CUS : CUS; }
-constexpr int blocks_of(int dim, int bytes) { return dim <= 64 && bytes == 2 ? 4 : 2; }
+constexpr int wgs_of(int dim, int bytes) { return dim <= 64 || (dim <= 128 && bytes == 1) ? 2 * CUS : CUS; }
+constexpr int blocks_of(int dim, int bytes) { return dim <= 128 && bytes == 2 ? 4 : 2; }
 
 // What the first launch leaves of a request for the second one: units in front of its group, tiles in front of it, its tokens and those of them that
 // its group reads, the group.  One more behind the last: the units and tiles of all.
@@ -174,7 +174,7 @@ __device__ __forceinline__ void scan_step(const int64_t (&mine)[2], int64_t (&at
 }
 
 template <typename C, typename Q, int DP, int NB>
-__global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kernel(SharedParams p) {
+__global__ __launch_bounds__(THREADS, wgs_of(DP, sizeof(C)) / CUS) void attend_shared_kernel(SharedParams p) {
   typedef Operand<C> Op;
   typedef Weights<C> Wt;
   typedef typename Op::t H;
@@ -184,6 +184,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
   constexpr int KL = DP * (int)sizeof(C) / 64;            // 16-byte loads of a key row per lane
   constexpr int KS = DP / 32;                             // products per block of 16 scores
   constexpr int BLOCKS = NB > WAVES ? NB : WAVES;
+  constexpr bool EARLY = wgs_of(DP, sizeof(C)) == CUS;    // registers for values on their way and turned ones at a time
   constexpr int PIECES = DP * (int)sizeof(C) / 16;        // 16-byte pieces of a key row, and loads of a tile's keys
   constexpr int KI = TILE * PIECES / 64;
   // A wave's keys, and its part of a piece when its run is over.
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
   const Work work(p, items);
 
   // Units and tiles of all, and in front of each; this workgroup's and its waves' runs of them, and the items that these begin in
-  constexpr int WGS = wgs_of(DP);
+  constexpr int WGS = wgs_of(DP, sizeof(C));
   const int most = max(p.groups, p.batch);
   int64_t mine[2], at[2], done[2] = {0, 0};
   auto scan_from = [&](int i0) {
@@ -356,10 +357,12 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
     auto load_keys = [&](const int64_t (&at_lds)[TILE]) {
       if constexpr (S8) tile_scale = (lane < 32 ? p.k_scale : p.v_scale)[scale_at];
       const int64_t *const at = key_real ? at_lds : no_rows;
+      int64_t from[KI];                       // (all read before the first is used)
 #pragma unroll
-      for (int n = 0; n < KI; ++n) {
-        k[n] = *(const __attribute__((address_space(1))) v4i *)(key_base + at[n * (64 / PIECES) + key_row]);
-      }
+      for (int n = 0; n < KI; ++n) from[n] = at[n * (64 / PIECES) + key_row];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < KI; ++n) k[n] = *(const __attribute__((address_space(1))) v4i *)(key_base + from[n]);
     };
     auto stage_keys = [&]() {
       lanes_meet();
@@ -375,6 +378,24 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[4 * h + j] = load_raw<VB>(value_base + at_lds[16 * h + 4 * g + j]);
+    };
+
+    // Element e of the lane's of its 8 rows: a column of V^T's block e
+    auto turn_values = [&](int e) {
+      v4i a;
+      if constexpr (S8) {
+        const uint32_t sel = 0x0c000c00u | (uint32_t)(e & 3) | (uint32_t)(4 + (e & 3)) << 16;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t u = __builtin_amdgcn_perm(v[2 * j + 1].d[e >> 2], v[2 * j].d[e >> 2], sel) ^ 0x64806480u;
+          a[j] = __builtin_bit_cast(int, __builtin_bit_cast(h2, u) - h2{(f16)1152, (f16)1152});
+        }
+      } else {
+        const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = (int)__builtin_amdgcn_perm(v[2 * j + 1].d[e >> 1], v[2 * j].d[e >> 1], sel);
+      }
+      return a;
     };
 
       // A tile's places are looked up two tiles ahead and worked out one ahead, while the first product runs.
@@ -411,11 +432,30 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
         v4f acc[N][2];
 #pragma unroll
         for (int nb = 0; nb < N; ++nb) acc[nb][0] = acc[nb][1] = v4f{0, 0, 0, 0};
+        // A step of the product needs two pieces of keys and N of queries (twice as many of the converted ones); the next step's are read from LDS
+        // before this one's products, which hide the way, where there are registers for both.
+        constexpr int QS = S8 ? 2 : 1, AHEAD = EARLY ? 2 : 1;
+        v4i kd[AHEAD][2], qd[AHEAD][QS][N];
+        auto read_step = [&](int i) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h) kd[i % AHEAD][h] = key(h, i);
 #pragma unroll
-          for (int i = 0; i < KL; ++i) {
-            const v4i d = key(h, i);
+          for (int s = 0; s < QS; ++s)
+#pragma unroll
+            for (int nb = 0; nb < N; ++nb) qd[i % AHEAD][s][nb] = q_lds[q0 + nb][QS * i + s][lane];
+        };
+        if constexpr (EARLY) read_step(0);
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+          if constexpr (EARLY) {
+            if (i + 1 < KL) read_step(i + 1);
+            __builtin_amdgcn_sched_barrier(0);
+          } else {
+            read_step(i);
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const v4i d = kd[i % AHEAD][h];
             if constexpr (S8) {
               h8 lo, hi;
 #pragma unroll
@@ -426,16 +466,19 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
                 to[4 * (j & 1)] = a[0], to[4 * (j & 1) + 1] = a[1], to[4 * (j & 1) + 2] = e[0], to[4 * (j & 1) + 3] = e[1];
               }
 #pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, lo), q_lds[q0 + nb][2 * i][lane], acc[nb][h]);
+              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, lo), qd[i % AHEAD][0][nb], acc[nb][h]);
 #pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, hi), q_lds[q0 + nb][2 * i + 1][lane], acc[nb][h]);
+              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, hi), qd[i % AHEAD][QS - 1][nb], acc[nb][h]);
             } else {
 #pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(d, q_lds[q0 + nb][i][lane], acc[nb][h]);
+              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(d, qd[i % AHEAD][0][nb], acc[nb][h]);
             }
           }
+          if constexpr (EARLY) __builtin_amdgcn_sched_barrier(0);
+        }
         then = locate(t0 + 2 * step, page, rows[wave][buf].at);
         page = look_up(t0 + 3 * step);
+        __builtin_amdgcn_sched_barrier(0);    // (ahead of the values' loads, which a wait for it must not wait for)
         if (now != 0xffffffffu) {
 #pragma unroll
           for (int h = 0; h < 2; ++h)
@@ -447,6 +490,12 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
 #pragma unroll
               for (int w = 0; w < VB / 4; ++w) v[4 * h + j].d[w] = real ? v[4 * h + j].d[w] : 0u;   // (0 * NaN is NaN)
             }
+        }
+        v4i turned_values[EARLY ? E : 1];
+        if constexpr (EARLY) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) turned_values[e] = turn_values(e);
+          load_values(rows[wave][buf ^ 1].at);
         }
         // the maximum of the scores (of what the values weigh, for 8 bits)
         float top[N];
@@ -492,19 +541,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          v4i a;
-          if constexpr (S8) {
-            const uint32_t sel = 0x0c000c00u | (uint32_t)(e & 3) | (uint32_t)(4 + (e & 3)) << 16;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t u = __builtin_amdgcn_perm(v[2 * j + 1].d[e >> 2], v[2 * j].d[e >> 2], sel) ^ 0x64806480u;
-              a[j] = __builtin_bit_cast(int, __builtin_bit_cast(h2, u) - h2{(f16)1152, (f16)1152});
-            }
-          } else {
-            const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) a[j] = (int)__builtin_amdgcn_perm(v[2 * j + 1].d[e >> 1], v[2 * j].d[e >> 1], sel);
-          }
+          const v4i a = EARLY ? turned_values[EARLY ? e : 0] : turn_values(e);
 #pragma unroll
           for (int nb = 0; nb < N; ++nb) o[nb][e] = Op::mfma(a, pt[nb], o[nb][e]);
         }
@@ -513,7 +550,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP) / CUS) void attend_shared_kerne
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_nop 15" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        load_values(rows[wave][buf ^ 1].at);
+        if constexpr (!EARLY) load_values(rows[wave][buf ^ 1].at);
         buf ^= 1, t0 += step;
         if (t0 >= end) break;
       }
@@ -765,7 +802,7 @@ f8_status launch_dim(const SharedParams &p, hipStream_t s) {
   const f8_status st = launch_status();
   if (st != F8_OK) return st;
   const int elements = (p.chunks > 1 ? p.rows : p.group) * p.dim;
-  hipLaunchKernelGGL((join_shared_kernel<Q, wgs_of(DP)>), dim3(p.batch * p.heads * p.chunks, (elements + JOIN_PART - 1) / JOIN_PART), dim3(64 * JOINERS), 0, s, p);
+  hipLaunchKernelGGL((join_shared_kernel<Q, wgs_of(DP, sizeof(C))>), dim3(p.batch * p.heads * p.chunks, (elements + JOIN_PART - 1) / JOIN_PART), dim3(64 * JOINERS), 0, s, p);
   return launch_status();
 }
 template <typename C, typename Q>
@@ -777,7 +814,10 @@ f8_status launch(const SharedParams &p, hipStream_t s) {
 bool alone(int batch, int groups, int q_heads, int max_len) {
   return groups == 0 || max_len <= 4 * UNIT || ((int64_t)max_len + TILE - 1) / TILE * batch * q_heads > 0x7fffffff;
 }
-size_t pieces_of(int64_t batch, int q_heads, int dim) { return (size_t)2 * batch * q_heads + (size_t)2 * wgs_of(dim) * (blocks_of(dim, 2) + WAVES) * COLS; }
+size_t pieces_of(int64_t batch, int q_heads, int dim) {
+  const int a = wgs_of(dim, 1) * (blocks_of(dim, 1) + WAVES), b = wgs_of(dim, 2) * (blocks_of(dim, 2) + WAVES);
+  return (size_t)2 * batch * q_heads + (size_t)2 * (a > b ? a : b) * COLS;
+}
 
 }  // namespace
 }  // namespace f8
@@ -817,7 +857,7 @@ f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cac
                        records, reinterpret_cast<int32_t *>(ws + pieces * (c->dim + 2)),
                        d->q_token, d->q_head, d->o_token, d->o_head, c->page_stride, c->token_stride, c->head_stride,
                        c->scale_page, c->scale_token, c->scale_head, d->table_ld, d->batch, groups, c->heads, group, chunks,
-                       chunks > 1 ? 1 : most / group, c->dim, c->pages, d->max_len, wgs_of(c->dim), most, FastDiv((uint32_t)c->page_size), FastDiv((uint32_t)group),
+                       chunks > 1 ? 1 : most / group, c->dim, c->pages, d->max_len, wgs_of(c->dim, (int)bytes_of(c->type)), most, FastDiv((uint32_t)c->page_size), FastDiv((uint32_t)group),
                        d->scale * LOG2E};
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (c->type == F8_S8) return d->type == F8_F16 ? launch<int8_t, f16>(p, hs) : launch<int8_t, bf16>(p, hs);
