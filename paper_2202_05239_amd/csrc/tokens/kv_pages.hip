@@ -135,6 +135,12 @@ __device__ __forceinline__ int fork_assign(const ForkParams &p, const Pool &pool
     if (b < p.batch) put(pool.at + b, 2 * (wanted + before[0]) + copies);
     wanted += all[0], beyond += all[1];
   }
+  // (from here on a tail's `writers` is its place among the new pages, -1: none.  A count that is not positive although a row names the page
+  // makes it a new one too, and what its holders give up before it is handed out is gone then)
+  for (int b = threadIdx.x; b < p.batch; b += blockDim.x) {
+    const int page = branch(b).tail;
+    if (page >= 0) put(pool.writers + page, -1);
+  }
   // the free pages of the lowest index
   int found = 0;
   for (int64_t i0 = 0; i0 < p.pages && found < wanted; i0 += EACH * blockDim.x) {
@@ -156,7 +162,10 @@ __device__ __forceinline__ int fork_assign(const ForkParams &p, const Pool &pool
   }
   found = min(found, wanted);
   __syncthreads();
-  for (int i = threadIdx.x; i < found; i += blockDim.x) put(pool.refs + seen(pool.fresh + i), 1);
+  for (int i = threadIdx.x; i < found; i += blockDim.x) {
+    const int page = seen(pool.fresh + i);
+    put(pool.refs + page, 1), put(pool.writers + page, i);
+  }
   __syncthreads();
   // the copies, one behind the other (those that no page was left for are the last)
   int copied = 0;
@@ -167,7 +176,7 @@ __device__ __forceinline__ int fork_assign(const ForkParams &p, const Pool &pool
     if (v[0]) {
       const Branch r = branch(b);
       const int to = (at >> 1) < found ? seen(pool.fresh + (at >> 1)) : -1;
-      add(pool.refs + r.tail, -1);
+      if (seen(pool.writers + r.tail) <= (at >> 1)) add(pool.refs + r.tail, -1);
       if (to >= 0) {
         int32_t *m = p.moves + 3 * (int64_t)(copied + before[0]);
         m[0] = r.tail, m[1] = to, m[2] = r.c.tokens - r.full * page_size;

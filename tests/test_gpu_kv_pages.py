@@ -115,6 +115,18 @@ def test_large_tables_and_pools(B, cols, page, spare, grow):
     check_fork(list(range(B)), table, lens, refs, page, grow)
 
 
+@pytest.mark.parametrize("B,cols,extra", [(1024, 16, 0), (1024, 16, 1), (1025, 15, 0), (1023, 17, 0)])
+def test_sizes_around_one_workgroup(B, cols, extra):
+    # as many requests, entries and pages as one workgroup takes, and one more of each
+    table, lens, refs, g, ri = state(B, B, cols, 4, 8192)
+    pages = 8192 + extra
+    refs = refs[:pages]
+    table = [[e if e < pages else e % pages for e in row] for row in table]
+    check_fork([ri(-1, B - 1) for _ in range(B)], table, lens, refs, 4, 1)
+    check_fork(list(range(B)), table, lens, refs, 4, 4)
+    check_fork(list(range(B)), table, lens, refs, 4, 5)
+
+
 def test_prompts_and_full_tables():
     # empty places take prompts of many tokens; tables without a column left; a pool without a page left
     for grow in (1, 100, 513):
@@ -199,6 +211,23 @@ def test_compaction(pages):
         assert torch.equal(t.cpu(), ints(want[0]))
         none = f8.f8_kv_compact(t[:0], refs.int().to(DEV), 16)
         assert torch.equal(none[1].cpu(), ints(want[1]))
+
+
+@pytest.mark.parametrize("pages,rows,cols", [(8191, 128, 128), (8192, 128, 128), (8193, 128, 128), (8192, 127, 130), (1, 5, 4000), (2, 3, 6000), (70001, 33, 700)])
+def test_compaction_around_one_workgroup(pages, rows, cols):
+    g = torch.Generator().manual_seed(pages + cols)
+    for used in (0.3, 0.9, -1.0):
+        refs = torch.where(torch.rand(pages, generator=g) < used, torch.randint(1, 6, (pages,), generator=g), 0)
+        if used < 0:
+            refs = (torch.arange(pages) >= pages // 2).int()
+        table = torch.randint(-3, pages + 3, (rows, cols), generator=g)
+        want = compacted(table.tolist(), refs.tolist(), 16)
+        wide = torch.full((rows, cols + 5), 77, dtype=torch.int32, device=DEV)
+        wide[:, 2:cols + 2] = table.int().to(DEV)
+        for src in (table.int().to(DEV), wide[:, 2:cols + 2]):
+            got = f8.f8_kv_compact(src, refs.int().to(DEV), 16)
+            for a, b in zip(got, want):
+                assert torch.equal(a.cpu(), torch.tensor(b, dtype=torch.int32).view(a.shape)), (pages, used)
 
 
 TYPES = {"s8": torch.int8, "f16": torch.float16, "bf16": torch.bfloat16}

@@ -87,6 +87,7 @@ def test_compaction():
     assert compact(desc(pages=1 << 30)) == 8 and compact(desc(), refs_out=at(1)) == 2
     need = L.f8_kv_compact_workspace_bytes(40)
     assert need > 0 and compact(desc(), n=need - 1) == 2 and compact(desc(), ws=ctypes.c_void_p(0x1008)) == 7
+    assert compact(desc(out_ld=6), table_out=at(0)) == 2                     # in place, with rows at another distance
     assert L.f8_kv_compact_workspace_bytes(0) == 0
 
 
