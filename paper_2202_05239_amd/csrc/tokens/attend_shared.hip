@@ -5,9 +5,15 @@
 //
 // both parts leave a maximum, a sum and a sum of values, which a second launch joins.  The prefix's part is a product with many rows, the query heads of
 // all the group's requests; as in f8_attend_paged both of its products run on the matrix cores with query heads as columns, S^T = K Q^T and
-// O^T = V^T P^T, the scores leaving the first one as the second one's operand, and K and V go from memory into registers: there by a tile for 16
-// columns, here for up to NB times 16 at once, so that what a tile costs to load, to bring into the products' form and, for 8 bits, to
-// convert, is shared among them.
+// O^T = V^T P^T, the scores leaving the first one as the second one's operand: there by a tile for 16 columns, here for up to NB times 16 at
+// once, so that what a tile costs to load, to bring into the products' form and, for 8 bits, to convert, is shared among them.
+//
+// What bounds it: few rows behind a prefix, HBM; many rows (16 to 64 columns to a byte), the vector instructions around the products
+// (of 64 columns: 330 to a tile's 64 products, exponentials of 16 cycles among them) and the waits of a wave that stands alone on its SIMD.  bf16, dim 128, 8 heads
+// of 4 query heads each: 64 requests behind 32768 tokens with 512 of their own 93 us, with one of their own 74 (455 TFLOP/s; a twentieth
+// less where every page is in the second-level cache).  8 bits, 16 groups of 4 behind 4096 tokens, 128 of their own: 38 us for 90 MB.
+// The way to the first rows (bounds, lengths, places, rows: four latencies one after the other), the join and the second
+// launch are 16 us, however little there is to read.
 #include <math.h>
 
 #include <type_traits>
@@ -21,7 +27,11 @@ namespace {
 constexpr int WAVES = 4, TILE = 32, COLS = 16, UNIT = WAVES * TILE, THREADS = 64 * WAVES;
 constexpr int ITEMS_LDS = 512;               // groups, and requests, that a workgroup keeps in LDS
 constexpr int CUS = 256;
-// Workgroups, two to a CU where the registers allow it, and blocks of columns of a workgroup.
+// Workgroups and blocks of columns of a workgroup.  Two to a CU hide one another's waits, one has registers for twice the columns, or for the next
+// tile's values and operands ahead of time.  One to a CU, two to a CU, us: 16 bits, dim 128 (64 and 32 columns), 64 requests behind 32768 tokens, 512
+// of their own 93, 98; 3 groups of 17 behind 9001 tokens, dim 80 40, 49; 64 requests of 600 tokens of their own alone 35, 33.  16 bits, dim 64 (64
+// columns each) 64, 54.  8 bits, dim 128 (64 and 32 columns) 108, 100, dim 64 77, 76; 16 groups of 4 behind 4096 tokens 44, 38.
+// Larger heads' accumulators leave one.
 constexpr int wgs_of(int dim, int bytes) { return dim <= 64 || (dim <= 128 && bytes == 1) ? 2 * CUS : CUS; }
 constexpr int blocks_of(int dim, int bytes) { return dim <= 128 && bytes == 2 ? 4 : 2; }
 
@@ -50,7 +60,7 @@ struct SharedParams {
 // A pair of the first kind is a group, a cache head and a block of up to `rows` query heads that read it; its units are rounds of a workgroup's
 // four waves over the prefix.  All units lie in a row and every workgroup takes an equal run of them.  A pair of the second kind is a request, a cache
 // head and up to 16 of its query heads; its units are tiles, and every wave takes an equal run on its own: these pairs are many and
-// short, and a pair's way to its first rows is 4 us (a workgroup to such a pair: 64 requests of 700 tokens, 8 heads, 107 us).
+// short, and a pair's way to its first rows is 3 us (64 requests of 600 tokens, 8 heads, bf16: 35 us so, 107 with a workgroup to such a pair).
 // A pair that lies in one run leaves its piece at its own place; one that is cut leaves a piece in each run, at slot 1 of the run that it begins in and at
 // slot 0 of the others.
 struct Prefix {
@@ -717,7 +727,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP, sizeof(C)) / CUS) void attend_s
   }
 }
 
-// Both parts of a request's heads together.  A workgroup takes JOIN_PART elements (heads by dimensions) of a request, a cache head and a chunk of
+// Both parts of a request's heads together: 5 us, a launch and three latencies (the record, the pieces, the store).  A workgroup takes JOIN_PART elements (heads by dimensions) of a request, a cache head and a chunk of
 // its query heads, 4 neighbours a thread and as many pieces at a time as threads are left; the pieces are added up in a fixed order.
 constexpr int JOINERS = 4, JOIN_PART = 256, JOIN_VECS = JOIN_PART / 4, JOIN_AT_ONCE = 64 * JOINERS / JOIN_VECS;
 

@@ -2,7 +2,9 @@
 //
 // Within a beam S falls with x, so a first launch needs no scores: a workgroup takes up to 16384 logits of a row into its registers and leaves
 // their maximum m, sum exp(x - m) and `keep` largest, and a second launch (a workgroup to a prompt) adds up the sums, forms S of what
-// is left in 64 bits and takes the `keep` largest of that.  Bound by HBM: the logits are read once.
+// is left in 64 bits and takes the `keep` largest of that.  Bound by HBM: the logits are read once (64 prompts of 8 beams, a fifth of them done,
+// 131072 bf16 logits, keep 16: 37 us for 107 MB, 2.9 TB/s: a wave waits for its piece and then has about 25 instructions to 8 logits; the second
+// launch 13.6).  A single prompt of 4 beams and 5001 logits takes 5 + 8 us, a chain of barriers each.
 //
 // The largest of a set.  Threads form at least `keep` groups; every group's largest element is one of the set's, so the least of these maxima is a
 // lower bound of the keep-th largest, which few elements reach (16 of 16384 random ones: about 45).  Those go to a list in LDS, as keys of which no

@@ -3,6 +3,11 @@
 //
 // A page is free where its count is not positive.  New pages are the free ones of the lowest index, handed out in the order of the
 // requests, so a result depends on its inputs alone: the only atomics add to counts or take a minimum.
+//
+// Bound by latencies: a few hundred kilobytes at most, in phases that wait for one another.  What fits one workgroup's LDS is one launch: 64
+// requests of up to 2048 tokens fork in 14 us (49 with the counts in memory), a pool of 1001 pages is compacted in 4.4 us (three launches
+// take 11).  More takes the phases as launches: 512 requests of up to 32768 tokens fork in 25 us, 262144 pages with 512 rows of 513 entries
+// are compacted in 18.
 #include "tokens_device.h"
 #include "tokens_host.h"
 
@@ -207,6 +212,8 @@ __device__ __forceinline__ int64_t slot_of(const ForkParams &p, const Pool &pool
 
 // All of it in one workgroup, with the counts in LDS: what takes time is that one reading waits for another (parent, length, tail), so each
 // is done once.
+// In a graph, one workgroup against the launches below, us: 4 requests, 600 pages 9.4, 14.6; 8192 pages, 64 requests of 128 columns 15.7, 20.4, 128
+// of 128 20.6, 20.5, 1024 of 16 23.7, 28.9; compaction of 600 pages 4.7, 10.0, of 8192 with 64 rows of 128 7.7, 12.6, with 128 9.9, 12.2.
 constexpr int SMALL_PAGES = 8192, SMALL_ENTRIES = 16384, SMALL_GROW = 4096;
 
 __global__ __launch_bounds__(THREADS) void fork_small_kernel(ForkParams p) {
