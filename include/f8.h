@@ -521,7 +521,7 @@ f8_status f8_kv_fork(const int32_t *parent, const int32_t *table, const int32_t 
                      void *workspace, size_t workspace_bytes, void *stream);
 
 /* Moves the pages in use to the front of the pool: with U pages in use, the ones at U and beyond go, in ascending order, to the free ones below U.
- * table [rows][cols] (table_out may be it) and refs [pages] (refs_out may not) are rewritten, entries that name no page in use stay.
+ * table [rows][cols] (table_out may be it, with the same distance of rows) and refs [pages] (refs_out may not) are rewritten, entries that name no page in use stay.
  * moves [pages / 2][3] lists (page, new page, page_size) for f8_kv_copy, behind the last one (-1, -1, 0); info[0]: number of moves, info[1]: U.
  * Workspace: f8_kv_compact_workspace_bytes(pages) bytes. */
 typedef struct {

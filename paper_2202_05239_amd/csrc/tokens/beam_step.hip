@@ -416,6 +416,7 @@ f8_status f8_beam_step(const void *logits, const float *scores, const uint8_t *d
       !aligned_to(workspace, 16))
     return F8_ERR_ALIGN;
   if (workspace_bytes < f8_beam_workspace_bytes(d->batch, d->beams, d->vocab, d->keep)) return F8_ERR_SHAPE;
+  if (score == scores) return F8_ERR_SHAPE;                // (other prompts' workgroups read them while they are written)
   int groups = 1;
   while (groups < d->keep) groups *= 2;
   const int64_t parts = rows * splits;

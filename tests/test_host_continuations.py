@@ -34,6 +34,7 @@ def test_beam_step():
         assert beam(b_desc(**bad)) == 8, bad
     need = L.f8_beam_workspace_bytes(2, 3, 100, 4)
     assert need == 2 * 3 * (16 + 4 * 8) and beam(b_desc(), n=need - 1) == 2
+    assert beam(b_desc(), scores=at(1), score=at(1)) == 2                   # scores that are read while they are written
     assert L.f8_beam_workspace_bytes(0, 3, 100, 4) == 0 and L.f8_beam_workspace_bytes(2, 3, 100, 65) == 0
     assert beam(b_desc(batch=0), logits=None) == 0
 
