@@ -4,7 +4,7 @@
 // their maximum m, sum exp(x - m) and `keep` largest, and a second launch (a workgroup to a prompt) adds up the sums, forms S of what
 // is left in 64 bits and takes the `keep` largest of that.  Bound by HBM: the logits are read once (64 prompts of 8 beams, a fifth of them done,
 // 131072 bf16 logits, keep 16: 37 us for 107 MB, 2.9 TB/s: a wave waits for its piece and then has about 25 instructions to 8 logits; the second
-// launch 13.6).  A single prompt of 4 beams and 5001 logits takes 5 + 8 us, a chain of barriers each.
+// launch 12.5).  A single prompt of 4 beams and 5001 logits takes 5 + 8 us, a chain of barriers each.
 //
 // The largest of a set.  Threads form at least `keep` groups; every group's largest element is one of the set's, so the least of these maxima is a
 // lower bound of the keep-th largest, which few elements reach (16 of 16384 random ones: about 45).  Those go to a list in LDS, as keys of which no
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(THREADS) void beam_join_kernel(BeamParams p) {
   __shared__ float score_of[BEAMS];
   __shared__ uint8_t done_of[BEAMS];
   __shared__ int count;
-  const int b = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int b = blockIdx.x, t = threadIdx.x;
   const int64_t row0 = (int64_t)b * p.beams;
   const uint32_t per_row = (uint32_t)p.splits * p.keep, all = per_row * p.beams;
   // the candidates' logits on their way, while the sums are added up (those of beams that are done were not written: not looked at)
@@ -259,15 +259,18 @@ __global__ __launch_bounds__(THREADS) void beam_join_kernel(BeamParams p) {
     logit[k] = p.best[row0 * per_row + c];
   }
   if (t == 0) count = 0;
-  // a wave to a beam, a lane to a workgroup's part of the row
-  for (int i = wave; i < p.beams; i += WAVES) {
+  // `width` lanes to a beam, one to a workgroup's part of the row: all beams at a time, if they fit
+  int width = 1;
+  while (width < p.splits && width < 64) width *= 2;
+  const int in_beam = t & (width - 1);
+  for (int i = t / width; i < p.beams; i += THREADS / width) {
     const float score = p.scores[row0 + i];
     const bool done = p.done && p.done[row0 + i];
     const Stat *s = p.stat + (row0 + i) * p.splits;
     float top = -INFINITY;
     double sum = 0;
     if (!done) {
-      for (int j = lane; j < p.splits; j += 64) {
+      for (int j = in_beam; j < p.splits; j += width) {
         const Stat x = s[j];
         const float now = fmaxf(top, x.top);
         // (a part without a number above -infinity adds its sum as it is: 0, or NaN)
@@ -276,14 +279,12 @@ __global__ __launch_bounds__(THREADS) void beam_join_kernel(BeamParams p) {
         top = now;
       }
       float all_top = top;
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) all_top = fmaxf(all_top, __shfl_xor(all_top, d));
+      for (int d = width >> 1; d > 0; d >>= 1) all_top = fmaxf(all_top, __shfl_xor(all_top, d));
       if (top != -INFINITY && top < all_top) sum *= exp((double)top - (double)all_top);
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+      for (int d = width >> 1; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
       top = all_top;
     }
-    if (lane == 0) {
+    if (in_beam == 0) {
       score_of[i] = score, done_of[i] = done;
       lse[i] = !(score < INFINITY) ? (double)__builtin_nanf("") : score == -INFINITY ? (double)score : done ? 0 : sum == 0 ? -(double)INFINITY : (double)top + log(sum);
     }
