@@ -194,7 +194,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP, sizeof(C)) / CUS) void attend_s
   constexpr int KL = DP * (int)sizeof(C) / 64;            // 16-byte loads of a key row per lane
   constexpr int KS = DP / 32;                             // products per block of 16 scores
   constexpr int BLOCKS = NB > WAVES ? NB : WAVES;
-  constexpr bool EARLY = wgs_of(DP, sizeof(C)) == CUS;    // registers for values on their way and turned ones at a time
+  constexpr bool EARLY = wgs_of(DP, sizeof(C)) == CUS;    // there are registers for what comes next
   constexpr int PIECES = DP * (int)sizeof(C) / 16;        // 16-byte pieces of a key row, and loads of a tile's keys
   constexpr int KI = TILE * PIECES / 64;
   // A wave's keys, and its part of a piece when its run is over.
@@ -337,16 +337,18 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP, sizeof(C)) / CUS) void attend_s
     }
     const C *const kbase = static_cast<const C *>(p.k) + kvh * p.head, *const vbase = static_cast<const C *>(p.v) + kvh * p.head;
     const char *const value_base = reinterpret_cast<const char *>(vbase + (c16 * E < p.dim ? c16 * E : 0));
-    // Keys come as they lie in memory, rows of neighbouring lanes, and become the product's left operand in LDS: its lanes hold 16 bytes of 16 rows each, which
-    // the load unit would take a row at a time (a quarter of the rate).  A row's pieces are permuted by its number: no 16 rows' pieces share banks.
+    // Keys come as they lie in memory, rows of neighbouring lanes, and become the product's left operand in LDS: its lanes hold 16 bytes of
+    // 16 rows each, which the load unit would take a row at a time (a quarter of the rate).  A row's pieces are permuted by its number: no 16
+    // rows' pieces share banks.
     auto turned = [](int row) { return PIECES >= 16 ? row & 15 : PIECES == 8 ? row & 7 : row >> 1 & 3; };
     const int key_row = lane / PIECES, key_piece = lane % PIECES;             // of load 0; load n is n * 64 / PIECES rows further
     const bool key_real = key_piece * (16 / (int)sizeof(C)) < p.dim;
     // (a lane of such dimensions takes its places from no_rows)
     const int64_t key_base = key_real ? reinterpret_cast<int64_t>(kbase) + key_piece * 16 : 0;
     v4i *const keys = stage[wave].keys;
-    // The next tile's keys are on their way from when this one's are in LDS, its values from when this one's have been summed up.  All loads are issued whether there is a next tile or not (a token that
-    // does not exist reads row 0 of the cache): behind a branch around a load nobody knows how many are on their way, and the wait is for all.
+    // The next tile's keys are on their way from when this one's are in LDS, its values from when this one's have been summed up, or before
+    // that where there are registers for both.  All loads are issued whether there is a next tile or not (a token that does not exist reads
+    // row 0 of the cache): behind a branch around a load nobody knows how many are on their way, and the wait is for all.
     v4i k[KI];
     Raw<VB> v[8];
     float tile_scale = 1.0f;                  // lanes 0..31: of the key of token `lane`, 32..63: of the value of token `lane - 32`
@@ -408,162 +410,162 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP, sizeof(C)) / CUS) void attend_s
       return a;
     };
 
-      // A tile's places are looked up two tiles ahead and worked out one ahead, while the first product runs.
-      int buf = 0;
-      there = locate(t0, look_up(t0), rows[wave][0].at);
+    // A tile's places are looked up two tiles ahead and worked out one ahead, while the first product runs.
+    int buf = 0;
+    there = locate(t0, look_up(t0), rows[wave][0].at);
+    lanes_meet();
+    load_keys(rows[wave][0].at);
+    int page = look_up(t0 + step);          // (in the order of the loop below)
+    load_values(rows[wave][0].at);
+    ready();
+    then = locate(t0 + step, page, rows[wave][1].at);
+    page = look_up(t0 + 2 * step);
+    for (;;) {
+      const uint32_t now = there;
+      there = then;
+      const float now_scale = tile_scale;
+      stage_keys();
+      load_keys(rows[wave][buf ^ 1].at);
       lanes_meet();
-      load_keys(rows[wave][0].at);
-      int page = look_up(t0 + step);          // (in the order of the loop below)
-      load_values(rows[wave][0].at);
-      ready();
-      then = locate(t0 + step, page, rows[wave][1].at);
-      page = look_up(t0 + 2 * step);
-      for (;;) {
-        const uint32_t now = there;
-        there = then;
-        const float now_scale = tile_scale;
-        stage_keys();
-        load_keys(rows[wave][buf ^ 1].at);
+      v4f ks[2], vs[2], vl[2];
+      if constexpr (S8) {
+        float *const scale_lds = rows[wave][buf].scale;
+        const float scale = now >> (lane & 31) & 1 ? now_scale : 1.0f;
+        scale_lds[lane] = scale;
+        scale_lds[64 + lane] = fmaxf(__log2f(scale), SMALL);
         lanes_meet();
-        v4f ks[2], vs[2], vl[2];
-        if constexpr (S8) {
-          float *const scale_lds = rows[wave][buf].scale;
-          const float scale = now >> (lane & 31) & 1 ? now_scale : 1.0f;
-          scale_lds[lane] = scale;
-          scale_lds[64 + lane] = fmaxf(__log2f(scale), SMALL);
-          lanes_meet();
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            ks[h] = *reinterpret_cast<const v4f *>(scale_lds + 16 * h + 4 * g);
-            vs[h] = *reinterpret_cast<const v4f *>(scale_lds + 32 + 16 * h + 4 * g);
-            vl[h] = *reinterpret_cast<const v4f *>(scale_lds + 96 + 16 * h + 4 * g);
-          }
+        for (int h = 0; h < 2; ++h) {
+          ks[h] = *reinterpret_cast<const v4f *>(scale_lds + 16 * h + 4 * g);
+          vs[h] = *reinterpret_cast<const v4f *>(scale_lds + 32 + 16 * h + 4 * g);
+          vl[h] = *reinterpret_cast<const v4f *>(scale_lds + 96 + 16 * h + 4 * g);
         }
-        v4f acc[N][2];
+      }
+      v4f acc[N][2];
 #pragma unroll
-        for (int nb = 0; nb < N; ++nb) acc[nb][0] = acc[nb][1] = v4f{0, 0, 0, 0};
-        // A step of the product needs two pieces of keys and N of queries (twice as many of the converted ones); the next step's are read from LDS
-        // before this one's products, which hide the way, where there are registers for both.
-        constexpr int QS = S8 ? 2 : 1, AHEAD = EARLY ? 2 : 1;
-        v4i kd[AHEAD][2], qd[AHEAD][QS][N];
-        auto read_step = [&](int i) {
+      for (int nb = 0; nb < N; ++nb) acc[nb][0] = acc[nb][1] = v4f{0, 0, 0, 0};
+      // A step of the product needs two pieces of keys and N of queries (twice as many of the converted ones); the next step's are read from LDS
+      // before this one's products, which hide the way, where there are registers for both.
+      constexpr int QS = S8 ? 2 : 1, AHEAD = EARLY ? 2 : 1;
+      v4i kd[AHEAD][2], qd[AHEAD][QS][N];
+      auto read_step = [&](int i) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) kd[i % AHEAD][h] = key(h, i);
+        for (int h = 0; h < 2; ++h) kd[i % AHEAD][h] = key(h, i);
 #pragma unroll
-          for (int s = 0; s < QS; ++s)
+        for (int s = 0; s < QS; ++s)
 #pragma unroll
-            for (int nb = 0; nb < N; ++nb) qd[i % AHEAD][s][nb] = q_lds[q0 + nb][QS * i + s][lane];
-        };
-        if constexpr (EARLY) read_step(0);
+          for (int nb = 0; nb < N; ++nb) qd[i % AHEAD][s][nb] = q_lds[q0 + nb][QS * i + s][lane];
+      };
+      if constexpr (EARLY) read_step(0);
 #pragma unroll
-        for (int i = 0; i < KL; ++i) {
-          if constexpr (EARLY) {
-            if (i + 1 < KL) read_step(i + 1);
-            __builtin_amdgcn_sched_barrier(0);
-          } else {
-            read_step(i);
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const v4i d = kd[i % AHEAD][h];
-            if constexpr (S8) {
-              h8 lo, hi;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const uint32_t u = (uint32_t)d[j] ^ 0x80808080u;
-                const h2 a = codes_lo(u), e = codes_hi(u);
-                h8 &to = j < 2 ? lo : hi;
-                to[4 * (j & 1)] = a[0], to[4 * (j & 1) + 1] = a[1], to[4 * (j & 1) + 2] = e[0], to[4 * (j & 1) + 3] = e[1];
-              }
-#pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, lo), qd[i % AHEAD][0][nb], acc[nb][h]);
-#pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, hi), qd[i % AHEAD][QS - 1][nb], acc[nb][h]);
-            } else {
-#pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(d, qd[i % AHEAD][0][nb], acc[nb][h]);
-            }
-          }
-          if constexpr (EARLY) __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < KL; ++i) {
+        if constexpr (EARLY) {
+          if (i + 1 < KL) read_step(i + 1);
+          __builtin_amdgcn_sched_barrier(0);
+        } else {
+          read_step(i);
         }
-        then = locate(t0 + 2 * step, page, rows[wave][buf].at);
-        page = look_up(t0 + 3 * step);
-        __builtin_amdgcn_sched_barrier(0);    // (ahead of the values' loads, which a wait for it must not wait for)
-        if (now != 0xffffffffu) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {
+          const v4i d = kd[i % AHEAD][h];
+          if constexpr (S8) {
+            h8 lo, hi;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const bool real = now >> (16 * h + 4 * g + j) & 1;
-#pragma unroll
-              for (int nb = 0; nb < N; ++nb) acc[nb][h][j] = real ? acc[nb][h][j] : -INFINITY;
-#pragma unroll
-              for (int w = 0; w < VB / 4; ++w) v[4 * h + j].d[w] = real ? v[4 * h + j].d[w] : 0u;   // (0 * NaN is NaN)
+              const uint32_t u = (uint32_t)d[j] ^ 0x80808080u;
+              const h2 a = codes_lo(u), e = codes_hi(u);
+              h8 &to = j < 2 ? lo : hi;
+              to[4 * (j & 1)] = a[0], to[4 * (j & 1) + 1] = a[1], to[4 * (j & 1) + 2] = e[0], to[4 * (j & 1) + 3] = e[1];
             }
-        }
-        v4i turned_values[EARLY ? E : 1];
-        if constexpr (EARLY) {
 #pragma unroll
-          for (int e = 0; e < E; ++e) turned_values[e] = turn_values(e);
-          load_values(rows[wave][buf ^ 1].at);
-        }
-        // the maximum of the scores (of what the values weigh, for 8 bits)
-        float top[N];
-        bool rises = false;
+            for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, lo), qd[i % AHEAD][0][nb], acc[nb][h]);
 #pragma unroll
-        for (int nb = 0; nb < N; ++nb) {
-          top[nb] = -INFINITY;
+            for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(__builtin_bit_cast(v4i, hi), qd[i % AHEAD][QS - 1][nb], acc[nb][h]);
+          } else {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              top[nb] = fmaxf(top[nb], S8 ? __builtin_fmaf(acc[nb][h][j], q_scale[nb] * ks[h][j], vl[h][j]) : acc[nb][h][j]);
-          if (!S8) top[nb] *= q_scale[nb];
-          rises = rises || top[nb] > m[nb] + Wt::SLACK;
-        }
-        if (__any(rises)) {                   // (seldom in a long context)
-#pragma unroll
-          for (int nb = 0; nb < N; ++nb) {
-            float to = fmaxf(top[nb], m[nb]);
-            to = fmaxf(to, __shfl_xor(to, 16));
-            to = fmaxf(to, __shfl_xor(to, 32));
-            const float shrink = __builtin_amdgcn_exp2f(m[nb] - (to == -INFINITY ? 0.0f : to));
-            l[nb] *= shrink;
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) o[nb][e][j] *= shrink;
-            m[nb] = to;
+            for (int nb = 0; nb < N; ++nb) acc[nb][h] = Op::mfma(d, qd[i % AHEAD][0][nb], acc[nb][h]);
           }
         }
-        v4i pt[N];
-#pragma unroll
-        for (int nb = 0; nb < N; ++nb) {
-          const float below = (m[nb] == -INFINITY ? 0.0f : m[nb]) - (Wt::TOP - Wt::SLACK);
-          t8 wh;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[nb][j >> 2][j & 3], S8 ? q_scale[nb] * ks[j >> 2][j & 3] : q_scale[nb], -below));
-            l[nb] += w;
-            wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : Wt::LEAST > 0 ? w + Wt::LEAST : w);
-          }
-          pt[nb] = __builtin_bit_cast(v4i, wh);
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const v4i a = EARLY ? turned_values[EARLY ? e : 0] : turn_values(e);
-#pragma unroll
-          for (int nb = 0; nb < N; ++nb) o[nb][e] = Op::mfma(a, pt[nb], o[nb][e]);
-        }
-        // The results of the last products are there before any branch: behind one the compiler (ROCm 7.2) has read an
-        // accumulator without the wait that a matrix instruction's result needs.
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_nop 15" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (!EARLY) load_values(rows[wave][buf ^ 1].at);
-        buf ^= 1, t0 += step;
-        if (t0 >= end) break;
+        if constexpr (EARLY) __builtin_amdgcn_sched_barrier(0);
       }
+      then = locate(t0 + 2 * step, page, rows[wave][buf].at);
+      page = look_up(t0 + 3 * step);
+      __builtin_amdgcn_sched_barrier(0);    // (ahead of the values' loads, which a wait for it must not wait for)
+      if (now != 0xffffffffu) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const bool real = now >> (16 * h + 4 * g + j) & 1;
+#pragma unroll
+            for (int nb = 0; nb < N; ++nb) acc[nb][h][j] = real ? acc[nb][h][j] : -INFINITY;
+#pragma unroll
+            for (int w = 0; w < VB / 4; ++w) v[4 * h + j].d[w] = real ? v[4 * h + j].d[w] : 0u;   // (0 * NaN is NaN)
+          }
+      }
+      v4i turned_values[EARLY ? E : 1];
+      if constexpr (EARLY) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) turned_values[e] = turn_values(e);
+        load_values(rows[wave][buf ^ 1].at);
+      }
+      // the maximum of the scores (of what the values weigh, for 8 bits)
+      float top[N];
+      bool rises = false;
+#pragma unroll
+      for (int nb = 0; nb < N; ++nb) {
+        top[nb] = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            top[nb] = fmaxf(top[nb], S8 ? __builtin_fmaf(acc[nb][h][j], q_scale[nb] * ks[h][j], vl[h][j]) : acc[nb][h][j]);
+        if (!S8) top[nb] *= q_scale[nb];
+        rises = rises || top[nb] > m[nb] + Wt::SLACK;
+      }
+      if (__any(rises)) {                   // (seldom in a long context)
+#pragma unroll
+        for (int nb = 0; nb < N; ++nb) {
+          float to = fmaxf(top[nb], m[nb]);
+          to = fmaxf(to, __shfl_xor(to, 16));
+          to = fmaxf(to, __shfl_xor(to, 32));
+          const float shrink = __builtin_amdgcn_exp2f(m[nb] - (to == -INFINITY ? 0.0f : to));
+          l[nb] *= shrink;
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[nb][e][j] *= shrink;
+          m[nb] = to;
+        }
+      }
+      v4i pt[N];
+#pragma unroll
+      for (int nb = 0; nb < N; ++nb) {
+        const float below = (m[nb] == -INFINITY ? 0.0f : m[nb]) - (Wt::TOP - Wt::SLACK);
+        t8 wh;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[nb][j >> 2][j & 3], S8 ? q_scale[nb] * ks[j >> 2][j & 3] : q_scale[nb], -below));
+          l[nb] += w;
+          wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : Wt::LEAST > 0 ? w + Wt::LEAST : w);
+        }
+        pt[nb] = __builtin_bit_cast(v4i, wh);
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const v4i a = EARLY ? turned_values[EARLY ? e : 0] : turn_values(e);
+#pragma unroll
+        for (int nb = 0; nb < N; ++nb) o[nb][e] = Op::mfma(a, pt[nb], o[nb][e]);
+      }
+      // The results of the last products are there before any branch: behind one the compiler (ROCm 7.2) has read an
+      // accumulator without the wait that a matrix instruction's result needs.
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_nop 15" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!EARLY) load_values(rows[wave][buf ^ 1].at);
+      buf ^= 1, t0 += step;
+      if (t0 >= end) break;
+    }
   };
 
   // ---- prefixes ----
@@ -727,7 +729,8 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP, sizeof(C)) / CUS) void attend_s
   }
 }
 
-// Both parts of a request's heads together: 5 us, a launch and three latencies (the record, the pieces, the store).  A workgroup takes JOIN_PART elements (heads by dimensions) of a request, a cache head and a chunk of
+// Both parts of a request's heads together: 5 us, a launch and three latencies (the record, the pieces, the store).  A workgroup takes
+// JOIN_PART elements (heads by dimensions) of a request, a cache head and a chunk of
 // its query heads, 4 neighbours a thread and as many pieces at a time as threads are left; the pieces are added up in a fixed order.
 constexpr int JOINERS = 4, JOIN_PART = 256, JOIN_VECS = JOIN_PART / 4, JOIN_AT_ONCE = 64 * JOINERS / JOIN_VECS;
 
@@ -812,7 +815,8 @@ f8_status launch_dim(const SharedParams &p, hipStream_t s) {
   const f8_status st = launch_status();
   if (st != F8_OK) return st;
   const int elements = (p.chunks > 1 ? p.rows : p.group) * p.dim;
-  hipLaunchKernelGGL((join_shared_kernel<Q, wgs_of(DP, sizeof(C))>), dim3(p.batch * p.heads * p.chunks, (elements + JOIN_PART - 1) / JOIN_PART), dim3(64 * JOINERS), 0, s, p);
+  hipLaunchKernelGGL((join_shared_kernel<Q, wgs_of(DP, sizeof(C))>), dim3(p.batch * p.heads * p.chunks, (elements + JOIN_PART - 1) / JOIN_PART),
+                     dim3(64 * JOINERS), 0, s, p);
   return launch_status();
 }
 template <typename C, typename Q>
@@ -867,7 +871,8 @@ f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cac
                        records, reinterpret_cast<int32_t *>(ws + pieces * (c->dim + 2)),
                        d->q_token, d->q_head, d->o_token, d->o_head, c->page_stride, c->token_stride, c->head_stride,
                        c->scale_page, c->scale_token, c->scale_head, d->table_ld, d->batch, groups, c->heads, group, chunks,
-                       chunks > 1 ? 1 : most / group, c->dim, c->pages, d->max_len, wgs_of(c->dim, (int)bytes_of(c->type)), most, FastDiv((uint32_t)c->page_size), FastDiv((uint32_t)group),
+                       chunks > 1 ? 1 : most / group, c->dim, c->pages, d->max_len, wgs_of(c->dim, (int)bytes_of(c->type)), most,
+                       FastDiv((uint32_t)c->page_size), FastDiv((uint32_t)group),
                        d->scale * LOG2E};
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (c->type == F8_S8) return d->type == F8_F16 ? launch<int8_t, f16>(p, hs) : launch<int8_t, bf16>(p, hs);
