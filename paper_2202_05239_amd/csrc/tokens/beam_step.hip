@@ -3,8 +3,8 @@
 // Within a beam S falls with x, so a first launch needs no scores: a workgroup takes up to 16384 logits of a row into its registers and leaves
 // their maximum m, sum exp(x - m) and `keep` largest, and a second launch (a workgroup to a prompt) adds up the sums, forms S of what
 // is left in 64 bits and takes the `keep` largest of that.  Bound by HBM: the logits are read once (64 prompts of 8 beams, a fifth of them done,
-// 131072 bf16 logits, keep 16: 37 us for 107 MB, 2.9 TB/s: a wave waits for its piece and then has about 25 instructions to 8 logits; the second
-// launch 12.5).  A single prompt of 4 beams and 5001 logits takes 5 + 8 us, a chain of barriers each.
+// 131072 bf16 logits, keep 16: 36.6 us for 107 MB, 2.9 TB/s: a wave waits for its piece and then has about 25 instructions to 8 logits; the second
+// launch 11.4).  A single prompt of 4 beams and 5001 logits takes 5 + 8 us, a chain of barriers each.
 //
 // The largest of a set.  Threads form at least `keep` groups; every group's largest element is one of the set's, so the least of these maxima is a
 // lower bound of the keep-th largest, which few elements reach (16 of 16384 random ones: about 45).  Those go to a list in LDS, as keys of which no
@@ -126,6 +126,7 @@ __device__ __forceinline__ float least_of_groups(float v, int groups, float *wav
 template <typename T, int NV>
 __global__ __launch_bounds__(THREADS, NV < 8 ? 6 : 4) void beam_rows_kernel(BeamParams p) {
   typedef RowMap<THREADS, NV> Map;
+  constexpr int AT_ONCE = 4;
   extern __shared__ __align__(16) uint8_t dynamic[];
   Key64 *const list = reinterpret_cast<Key64 *>(dynamic);             // list_of(keep, NV * 8)
   __shared__ Key64 top_keys[THREADS + 1];
@@ -169,13 +170,22 @@ __global__ __launch_bounds__(THREADS, NV < 8 ? 6 : 4) void beam_rows_kernel(Beam
     if (piece[i] >= least) pieces[atomicAdd(&reach, 1)] = (uint16_t)(i * THREADS + t);
   __syncthreads();
   const int elements = reach * 8;
-  for (int q = t; q < elements; q += THREADS) {
-    const int col = pieces[q >> 3] * 8 + (q & 7);
-    if (col < cols) {
-      const float e = (float)x[col];
-      if (e >= least) {
+  for (int q0 = t; q0 < elements; q0 += AT_ONCE * THREADS) {
+    int col[AT_ONCE];
+    T raw[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int q = min(q0 + u * THREADS, elements - 1);
+      col[u] = pieces[q >> 3] * 8 + (q & 7);
+      raw[u] = x[min(col[u], cols - 1)];
+      if (q0 + u * THREADS >= elements) col[u] = cols;
+    }
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const float e = (float)raw[u];
+      if (col[u] < cols && e >= least) {
         const int at = atomicAdd(&count, 1);
-        if (at < most) list[at].k = (uint64_t)order_of(e) << 32 | (uint32_t)~(base + col);
+        if (at < most) list[at].k = (uint64_t)order_of(e) << 32 | (uint32_t)~(base + col[u]);
       }
     }
   }
@@ -254,7 +264,7 @@ __global__ __launch_bounds__(THREADS) void beam_join_kernel(BeamParams p) {
   const uint32_t per_row = (uint32_t)p.splits * p.keep, all = per_row * p.beams;
   // the candidates' logits on their way, while the sums are added up (those of beams that are done were not written: not looked at)
   // A part of a row has its candidates in descending order: threads take different ranks, one of the first among them, so that their largest ones
-  // bound the keep-th largest closely (each its own rank: 64 of 131072 logits of one beam took 160 us, a thousand candidates passing).
+  // bound the keep-th largest closely (with one rank each: 64 of 131072 logits of one beam took 160 us, a thousand candidates passing).
   const uint32_t turn = (p.keep + PER - 1) / PER;
   auto candidate = [&](int k) { return (uint32_t)k * THREADS + ((t + k * turn) & (THREADS - 1)); };
   uint64_t logit[PER];
