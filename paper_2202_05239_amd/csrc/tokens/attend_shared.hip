@@ -601,6 +601,9 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP, sizeof(C)) / CUS) void attend_s
       const int r = p.chunks > 1 ? 0 : (int)p.by_group.div((uint32_t)row);
       b = b0 + req0 + r, hq = kvh * p.group + h0 + row - r * heads;
     };
+    // blocks of columns that a walk takes: three are taken as four, and the fourth one's zeros are put down like any other column that is none
+    // (its maximum counts where the walk asks whether any rises)
+    const int walked = nb_used == 3 ? 4 : nb_used;
     const int row0 = wave * COLS + c16;
     {
       int b, hq;
@@ -608,7 +611,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP, sizeof(C)) / CUS) void attend_s
       load_queries(static_cast<const Q *>(p.q) + b * p.qt + hq * p.qh);
     }
     auto ready = [&]() {
-      if (wave < nb_used) put_queries(wave, row0 < real_rows);
+      if (wave < walked) put_queries(wave, row0 < real_rows);
       __syncthreads();
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) q_scale[nb] = q_scale_lds[nb][c16];
@@ -617,11 +620,11 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP, sizeof(C)) / CUS) void attend_s
     const int32_t *table = p.table + leader * p.table_ld;
     const int t0 = unit * UNIT + wave * TILE;
     if constexpr (NB >= 4) {
-      if (nb_used > 2) walk(std::integral_constant<int, 4>(), table, kvh, t0, UNIT, end, 0, ready);
-      else if (nb_used > 1) walk(std::integral_constant<int, 2>(), table, kvh, t0, UNIT, end, 0, ready);
+      if (walked == 4) walk(std::integral_constant<int, 4>(), table, kvh, t0, UNIT, end, 0, ready);
+      else if (walked == 2) walk(std::integral_constant<int, 2>(), table, kvh, t0, UNIT, end, 0, ready);
       else walk(std::integral_constant<int, 1>(), table, kvh, t0, UNIT, end, 0, ready);
     } else {
-      if (nb_used > 1) walk(std::integral_constant<int, 2>(), table, kvh, t0, UNIT, end, 0, ready);
+      if (walked == 2) walk(std::integral_constant<int, 2>(), table, kvh, t0, UNIT, end, 0, ready);
       else walk(std::integral_constant<int, 1>(), table, kvh, t0, UNIT, end, 0, ready);
     }
 

@@ -289,3 +289,27 @@ def test_rounding_of_weights():
             base += (want.to(dtype).double() - want).square().sum().item()
         # a rounding to the same type, relative to the summed terms, which no cancellation makes smaller: sqrt(1 + 1) of the result's at most, 1.5 allowed
         assert far <= 1.5 ** 2 * base, (kind, far, base)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("n,group,D", [(10, 4, 128), (12, 4, 64), (5, 8, 80), (3, 16, 128), (11, 4, 64)])
+def test_results_depend_on_the_inputs_alone(dtype, n, group, D):
+    # 33 to 48 rows in a block of 64, several tiles to a wave: the columns that nobody fills are the same whatever ran before
+    page, heads, whole = 64, 8, 250
+    g = torch.Generator(device=DEV).manual_seed(n)
+    rand = lambda *s: torch.randn(*s, generator=g, device=DEV)  # noqa: E731
+
+    def batch(n, D):
+        """n requests behind 16000 tokens, with up to 50 of their own."""
+        kv = rand(2, whole + n, page, heads, D).to(dtype)
+        table = torch.cat([torch.arange(whole, device=DEV).expand(n, -1), whole + torch.arange(n, device=DEV)[:, None]], 1).int()
+        lens = ints([whole * page + 1 + 5 * b % 50 for b in range(n)])
+        return lambda q: f8.f8_attend_shared(q, kv[0], kv[1], table, lens, ints([0, n]), ints([whole * page]))
+    call, q = batch(n, D), rand(n, heads * group, D).to(dtype)
+    want = call(q)
+    other = batch(16, 128)                                        # fills all 64 columns; its scores rise late and far
+    for size in (1.0, 30.0, 900.0):
+        x = (size * rand(16, heads * 4, 128)).to(dtype)
+        for _ in range(3):
+            other(x)
+            assert torch.equal(call(q), want), size
