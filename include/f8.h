@@ -510,7 +510,8 @@ f8_status f8_beam_step(const void *logits, const float *scores, const uint8_t *d
  * Row b of table_out holds the pages and then -1.  slots [batch][grow] say where f8_kv_append puts the new tokens (-1: nowhere), moves [batch][3] what
  * f8_kv_copy has to copy before: (page, new page, tokens), behind the last one (-1, -1, 0).  info[0]: number of moves; info[1]: pages that were wanted
  * and not there, in the pool or as columns of the table.  Entries of these are -1 (of a copy: its tokens are lost), lens_out counts their tokens up to cols *
- * page_size all the same.  Workspace: f8_kv_fork_workspace_bytes(batch, pages) bytes. */
+ * page_size all the same.  batch 0: nothing is launched and nothing written, refs are the counts after the step too (the
+ * Python call copies them).  Workspace: f8_kv_fork_workspace_bytes(batch, pages) bytes. */
 typedef struct {
   int32_t batch, cols, pages, page_size, grow;
   int64_t table_ld, out_ld;          /* entries */

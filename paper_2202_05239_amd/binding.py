@@ -788,6 +788,9 @@ def f8_kv_fork(parent, table, lens, refs, page_size, grow=1, out=None, workspace
     rc = L.f8_kv_fork(*ins, *[t.data_ptr() for t in out], d, at_ws, n, _stream())
     if rc:
         raise F8Error(rc, "f8_kv_fork")
+    if B == 0:                                           # (the library launches nothing; these two do not shrink with the batch)
+        out[2].view(-1).copy_(refs.view(-1))
+        out[5].zero_()
     return out
 
 

@@ -296,3 +296,17 @@ def test_many_lines_and_no_lines():
     f8.f8_kv_copy(moves, kv[0], kv[1])
     assert torch.equal(kv[:, 15001:], kv[:, 1:15001])
     f8.f8_kv_copy(moves[:0], kv[0], kv[1])
+
+
+@pytest.mark.parametrize("pages", [1, 40, 20000])
+def test_forks_of_no_request(pages):
+    # the counts do not shrink with the batch: they and `info` are written all the same, into given tensors and new ones
+    new = lambda *s, t=torch.int32: torch.full(s, -77, dtype=t, device=DEV)  # noqa: E731
+    refs = torch.randint(-2, 5, (pages,), generator=torch.Generator().manual_seed(pages)).int().to(DEV)
+    kept = refs.clone()
+    out = (new(0, 3), new(0), new(pages), new(0, 2, t=torch.int64), new(0, 3), new(2))
+    for given in (out, None):
+        got = f8.f8_kv_fork(new(0), new(0, 3), new(0), refs, 16, 2, out=given)
+        assert torch.equal(got[2], kept) and got[5].tolist() == [0, 0] and torch.equal(refs, kept)
+        assert got[0].shape == (0, 3) and got[3].shape == (0, 2) and got[4].shape == (0, 3)
+    assert got[2].data_ptr() != refs.data_ptr()
