@@ -298,7 +298,8 @@ __global__ __launch_bounds__(THREADS) void beam_join_kernel(BeamParams p) {
     }
     if (in_beam == 0) {
       score_of[i] = score, done_of[i] = done;
-      lse[i] = !(score < INFINITY) ? (double)__builtin_nanf("") : score == -INFINITY ? (double)score : done ? 0 : sum == 0 ? -(double)INFINITY : (double)top + log(sum);
+      const bool bad = !(score < INFINITY) || sum != sum;               // (the sum of a beam that is done is 0)
+      lse[i] = bad ? (double)__builtin_nanf("") : score == -INFINITY ? (double)score : done ? 0 : sum == 0 ? -(double)INFINITY : (double)top + log(sum);
     }
   }
   __syncthreads();

@@ -202,3 +202,19 @@ def test_another_stream():
         got = f8.f8_beam_step(x, s)
     side.synchronize()
     check(logits, scores, 4, got=got)
+
+
+def test_what_is_no_number_shows_under_a_score_of_minus_infinity():
+    # -infinity plus NaN is NaN; of a beam that is done no logit is read
+    for V in (50, 20000):
+        for bad in (float("nan"), INF):
+            logits, scores = draw(13, 4, 3, V, torch.float32)
+            scores[:, 1] = -INF
+            logits[0, 1, 7] = bad
+            logits[1] = bad
+            logits[2, 1] = -INF
+            logits[3, 1, V - 1] = bad
+            done = torch.zeros(4, 3, dtype=torch.bool)
+            done[3, 1] = True
+            at, order = check(logits, scores, 5, done)
+            assert torch.equal(at[0], V + torch.arange(5))
