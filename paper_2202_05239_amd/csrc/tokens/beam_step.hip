@@ -38,7 +38,7 @@ struct BeamParams {
   uint64_t *best;                           // [rows][splits][keep]: order of the value, ~token; 0: none
   Stat *stat;                               // [rows][splits]
   int64_t ld;
-  int beams, vocab, keep, splits, eos, groups;              // groups of threads: a power of two, at least `keep`
+  int batch, beams, vocab, keep, splits, eos, groups;       // groups of threads: a power of two, at least `keep`
   int64_t blocks;
   FastDiv by_splits, by_row;                // by_row: candidates of a row in the second launch
 };
@@ -259,7 +259,8 @@ __global__ __launch_bounds__(THREADS) void beam_join_kernel(BeamParams p) {
   __shared__ float score_of[BEAMS];
   __shared__ uint8_t done_of[BEAMS];
   __shared__ int count;
-  const int b = blockIdx.x, t = threadIdx.x;
+  if (row_block() >= p.batch) return;
+  const int b = (int)row_block(), t = threadIdx.x;
   const int64_t row0 = (int64_t)b * p.beams;
   const uint32_t per_row = (uint32_t)p.splits * p.keep, all = per_row * p.beams;
   // the candidates' logits on their way, while the sums are added up (those of beams that are done were not written: not looked at)
@@ -394,9 +395,9 @@ void launch_rows(const BeamParams &p, int nv, hipStream_t s) {
 }
 
 template <int PER>
-void launch_join(const BeamParams &p, int batch, hipStream_t s) {
+void launch_join(const BeamParams &p, hipStream_t s) {
   static_assert(CANDIDATES <= 32 * THREADS, "candidates of a thread");
-  hipLaunchKernelGGL((beam_join_kernel<PER>), dim3(batch), dim3(THREADS), (size_t)list_of(p.keep, PER) * sizeof(KeyS), s, p);
+  hipLaunchKernelGGL((beam_join_kernel<PER>), block_grid(p.batch), dim3(THREADS), (size_t)list_of(p.keep, PER) * sizeof(KeyS), s, p);
 }
 
 }  // namespace
@@ -435,7 +436,7 @@ f8_status f8_beam_step(const void *logits, const float *scores, const uint8_t *d
   while (groups < d->keep) groups *= 2;
   const int64_t parts = rows * splits;
   Stat *stat = static_cast<Stat *>(workspace);
-  const BeamParams p{logits, scores, done, score, parent, token, reinterpret_cast<uint64_t *>(stat + parts), stat, d->ld, d->beams, d->vocab, d->keep, splits,
+  const BeamParams p{logits, scores, done, score, parent, token, reinterpret_cast<uint64_t *>(stat + parts), stat, d->ld, d->batch, d->beams, d->vocab, d->keep, splits,
                      d->eos, groups, parts, FastDiv((uint32_t)splits), FastDiv((uint32_t)(splits * d->keep))};
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (d->type == F8_F32) launch_rows<float>(p, nv, s);
@@ -444,9 +445,9 @@ f8_status f8_beam_step(const void *logits, const float *scores, const uint8_t *d
   const f8_status st = launch_status();
   if (st != F8_OK) return st;
   const int each = each_of((uint32_t)(d->beams * splits * d->keep));
-  if (each <= 4) launch_join<4>(p, d->batch, s);
-  else if (each <= 16) launch_join<16>(p, d->batch, s);
-  else launch_join<32>(p, d->batch, s);
+  if (each <= 4) launch_join<4>(p, s);
+  else if (each <= 16) launch_join<16>(p, s);
+  else launch_join<32>(p, s);
   return launch_status();
 }
 

@@ -218,3 +218,16 @@ def test_what_is_no_number_shows_under_a_score_of_minus_infinity():
             done[3, 1] = True
             at, order = check(logits, scores, 5, done)
             assert torch.equal(at[0], V + torch.arange(5))
+
+
+def test_more_prompts_than_a_grid_dimension_holds():
+    # 2^24 workgroups of 256 threads do not fit one dimension of a launch
+    B = 2 ** 24 + 3
+    x = torch.randn(B, 1, 2, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).half()
+    scores = torch.zeros(B, 1, device=DEV)
+    score, parent, token = f8.f8_beam_step(x, scores, keep=1)
+    d = x.float()[:, 0]
+    want = -torch.log1p(torch.exp(-(d[:, 0] - d[:, 1]).abs()))
+    assert torch.equal(parent[:, 0], torch.arange(B, device=DEV, dtype=torch.int32))
+    assert torch.equal(token[:, 0], (d[:, 1] > d[:, 0]).int())
+    assert (score[:, 0] - want).abs().max().item() <= 2.0 ** -16
