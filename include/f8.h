@@ -500,7 +500,8 @@ size_t f8_beam_workspace_bytes(int batch, int beams, int vocab, int keep);
 f8_status f8_beam_step(const void *logits, const float *scores, const uint8_t *done, float *score, int32_t *parent, int32_t *token,
                        const f8_beam_desc *d, void *workspace, size_t workspace_bytes, void *stream);
 
-/* One step of the requests that share a cache: request b goes on from request parent[b] (outside 0 .. batch - 1: it ends) by `grow` tokens.
+/* One step of the requests that share a cache: request b goes on from request parent[b] (outside 0 .. batch - 1: it ends) by `grow` tokens
+ * (grow and cols * page_size: up to 0x7fff0000).
  * table [batch][cols], lens and refs [pages] are those before the step, table_out, lens_out and refs_out those after it:
  *   - a request holds the pages of its parent, ceil(lens / page_size) entries of the table's row (entries outside 0 .. pages - 1 are
  *     carried along and hold nothing); pages that nobody holds any more are free from then on, for this step too;

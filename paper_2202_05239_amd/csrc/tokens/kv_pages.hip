@@ -493,7 +493,8 @@ f8_status f8_kv_fork(const int32_t *parent, const int32_t *table, const int32_t 
   if (!d) return F8_ERR_NULL;
   if (d->batch < 0 || d->batch > 65535 || d->cols < 1 || d->pages < 1 || d->page_size < 1 || d->grow < 0 || d->table_ld < d->cols || d->out_ld < d->cols)
     return F8_ERR_SHAPE;
-  if ((int64_t)d->cols * d->page_size > 0x7fff0000) return F8_ERR_SHAPE;
+  // (loops over tokens and columns count in 32 bits, a workgroup's threads at a time)
+  if ((int64_t)d->cols * d->page_size > 0x7fff0000 || d->grow > 0x7fff0000) return F8_ERR_SHAPE;
   if ((int64_t)d->batch * d->cols > 0x1fffffff || (int64_t)d->batch * (d->grow / d->page_size + 2) > 0x1fffffff || d->pages > 0x3fffffff)
     return F8_ERR_UNSUPPORTED;
   if (d->batch == 0) return F8_OK;

@@ -180,3 +180,10 @@ def test_binding_refuses_what_the_library_cannot_see():
         f8.f8_attend_shared(q, kv[0], kv[1], table, lens, torch.zeros(2), torch.zeros(1, dtype=i32))
     with pytest.raises(RuntimeError, match="gradient"):
         f8.f8_attend_shared(q.requires_grad_(), kv[0], kv[1], table, lens, torch.zeros(2, dtype=i32), torch.zeros(1, dtype=i32))
+
+
+def test_forks_by_more_tokens_than_a_cache_has():
+    # the largest step that 32-bit counters pass over; more is refused before anything is launched
+    for grow in (0x7fff0001, 0x7fffffff):
+        assert fork(k_desc(batch=1, grow=grow, page_size=1 << 20)) == 2
+    assert fork(k_desc(batch=1, grow=0x7fff0000, page_size=1 << 20), ws=None) == 1
