@@ -475,7 +475,8 @@ f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cach
  * group are their own) have their first shared[g] tokens in common, which are read once for all of them.  The result is f8_attend_paged's
  * of the same arguments but for rounding, wherever the pages that the members' rows list hold the same first shared[g] tokens, in one page or in copies: they are read through the
  * first member that has all of them (a shorter one reads its own).  first and shared are read on the device; weights of
- * 16-bit caches are rounded once to the cache's type.  Workspace: f8_attend_shared_workspace_bytes(batch, groups, q_heads, heads, dim, max_len) bytes. */
+ * 16-bit caches are rounded once to the cache's type, and an infinite value shows where its weight is at least 2^-40 (f16) or 2^-86 (bf16) of the
+ * largest one; below that the result may be NaN.  Workspace: f8_attend_shared_workspace_bytes(batch, groups, q_heads, heads, dim, max_len) bytes. */
 size_t f8_attend_shared_workspace_bytes(int batch, int groups, int q_heads, int kv_heads, int dim, int max_len);
 f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cache, const float *k_scale, const float *v_scale,
                            const int32_t *table, const int32_t *lens, const int32_t *first, const int32_t *shared, void *out,

@@ -145,16 +145,20 @@ struct TileRows {
 
 // The maximum that weights are taken against follows the scores only where they pass it by more than SLACK, as a power of two, and the largest
 // weight of a tile is at most 2^TOP: an accumulator is seldom touched by anything but products.  bf16 has the range of 32 bits.
-// f16 weights keep their relative error down to 2^-21 of the largest one, what lies below is off by 2^-32 of it at most.
+// f16 weights keep their relative error down to 2^-21 of the largest one; what lies below is off by 2^-32 of it at most.  Under f16 values those below
+// 2^-31 of it are also raised, 256-fold or to f16's smallest number, whichever is less: an infinite value then shows under every weight from 2^-40 of the
+// largest one up, as in f8_attend_paged, a weight below 2^-48 is 0, and one between is off by 2^-31 at most.  (The sum of the weights takes them unraised.)
 template <typename C>
 struct Weights {
   static constexpr float SLACK = 8.0f, TOP = 15.0f;
-  // what a weight has at least, so that it counts against an infinite value: f16's smallest number, 2^-31 of the largest weight
-  static constexpr float LEAST = sizeof(C) == 1 ? 0.0f : 0x1p-24f;
+  static __device__ __forceinline__ float raised(float w) {
+    return sizeof(C) == 1 ? w : __builtin_amdgcn_fmed3f(w, w * 0x1p8f, 0x1p-24f);
+  }
 };
 template <>
 struct Weights<bf16> {
-  static constexpr float SLACK = 40.0f, TOP = 0.0f, LEAST = 0.0f;
+  static constexpr float SLACK = 40.0f, TOP = 0.0f;
+  static __device__ __forceinline__ float raised(float w) { return w; }
 };
 
 __device__ const v4i zeros[1] = {v4i{0, 0, 0, 0}};          // keys' dimensions beyond the head's
@@ -547,7 +551,7 @@ __global__ __launch_bounds__(THREADS, wgs_of(DP, sizeof(C)) / CUS) void attend_s
         for (int j = 0; j < 8; ++j) {
           const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[nb][j >> 2][j & 3], S8 ? q_scale[nb] * ks[j >> 2][j & 3] : q_scale[nb], -below));
           l[nb] += w;
-          wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : Wt::LEAST > 0 ? w + Wt::LEAST : w);
+          wh[j] = (H)(S8 ? w * vs[j >> 2][j & 3] : Wt::raised(w));
         }
         pt[nb] = __builtin_bit_cast(v4i, wh);
       }

@@ -313,3 +313,45 @@ def test_results_depend_on_the_inputs_alone(dtype, n, group, D):
         for _ in range(3):
             other(x)
             assert torch.equal(call(q), want), size
+
+
+@pytest.mark.parametrize("at", [0, 1777, 4095, 4200])
+@pytest.mark.parametrize("score", [-34.0, -100.0])
+def test_tokens_that_weigh_nothing(at, score):
+    # one token of score 0 and value 0 among tokens of a score far below it and large values, in f16: weights below 2^-48 of the largest one
+    # are taken as 0, so the result is off by n 2^-48 of the largest value at most (6e-6), which is then rounded (2^-25 at least)
+    n, D = 4300, 64
+    c = Cache(18, [n, n - 40], 1, D, 16, "f16")
+    groups = share(c, [2], [4096])
+    c.kv[0] = 0
+    c.kv[0, ..., 0], c.kv[1] = score, 60000.0
+    for b in range(2):
+        page = c.table[b, at // 16].long()
+        c.kv[:, page, at % 16] = 0
+    c.dev.copy_(c.kv)
+    q = torch.zeros(2, 2, D, dtype=torch.float16)
+    q[..., 0] = 1
+    out = f8.f8_attend_shared(q.to(DEV), table=c.table.to(DEV), lens=ints(c.lens), first=groups[0], shared=groups[1], scale=1.0, **c.args()).cpu()
+    assert out.abs().max().item() <= n * 60000 * 2.0 ** -48 + 2.0 ** -25
+
+
+@pytest.mark.parametrize("kind,score", [("f16", -27.0), ("bf16", -58.0)])
+def test_infinite_values_of_small_weights(kind, score):
+    # an infinite value shows under any weight from 2^-40 (f16; e^-27 is 2^-38.95) or 2^-86 (bf16; e^-58 is 2^-83.7) of the largest one up
+    n, D, dtype = 3000, 64, {"f16": torch.float16, "bf16": torch.bfloat16}[kind]
+    c = Cache(19, [n, n - 40], 1, D, 16, kind)
+    groups = share(c, [2], [2900])
+    c.kv[0], c.kv[1] = 0, 1
+    for t in (5, 1500, 2899, 2950):
+        c.kv[0] = 0
+        c.kv[0, c.table[0, t // 16].long(), t % 16, 0, 0] = score
+        c.kv[0, c.table[1, t // 16].long(), t % 16, 0, 0] = score
+        c.dev.copy_(c.kv)
+        for b in range(2):
+            c.dev[1, c.table[b, t // 16].long(), t % 16, 0, 5] = float("inf")
+            c.dev[1, c.table[b, t // 16].long(), t % 16, 0, 9] = -float("inf")
+        q = torch.zeros(2, 2, D, dtype=dtype)
+        q[..., 0] = 1
+        out = f8.f8_attend_shared(q.to(DEV), table=c.table.to(DEV), lens=ints(c.lens), first=groups[0], shared=groups[1], scale=1.0, **c.args()).cpu()
+        assert (out[..., 5] == float("inf")).all() and (out[..., 9] == -float("inf")).all()
+        assert torch.isfinite(out).sum() == out.numel() - 8
