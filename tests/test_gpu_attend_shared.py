@@ -355,3 +355,12 @@ def test_infinite_values_of_small_weights(kind, score):
         out = f8.f8_attend_shared(q.to(DEV), table=c.table.to(DEV), lens=ints(c.lens), first=groups[0], shared=groups[1], scale=1.0, **c.args()).cpu()
         assert (out[..., 5] == float("inf")).all() and (out[..., 9] == -float("inf")).all()
         assert torch.isfinite(out).sum() == out.numel() - 8
+
+
+def test_a_prefix_that_is_longer_than_every_member():
+    # units are dealt out, no member can lead: every request reads its own tokens
+    for kind, dtype in KINDS:
+        c = Cache(20, [700, 0, 690, 3], 2, 64, 16, kind)
+        for shared in (701, 800, 2 ** 31 - 1):
+            q, out = run(c, 8, 64, dtype, (ints([0, 4]), ints([shared])), max_len=704)
+            check(c, q, out, 0.125)
