@@ -231,3 +231,9 @@ def test_more_prompts_than_a_grid_dimension_holds():
     assert torch.equal(parent[:, 0], torch.arange(B, device=DEV, dtype=torch.int32))
     assert torch.equal(token[:, 0], (d[:, 1] > d[:, 0]).int())
     assert (score[:, 0] - want).abs().max().item() <= 2.0 ** -16
+
+
+@pytest.mark.parametrize("B,K,V,keep", [(1, 16, 131072, 64), (1, 128, 100, 64), (2, 1024, 50, 8), (1, 32, 60000, 64), (1, 1, 2000000, 64)])
+def test_as_many_candidates_as_a_prompt_may_have(B, K, V, keep):
+    logits, scores = draw(V + K, B, K, V, torch.bfloat16)
+    check(logits, scores, keep)
