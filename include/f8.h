@@ -471,12 +471,14 @@ f8_status f8_attend_paged(const void *q, const void *k_cache, const void *v_cach
  * caller's does).  A page is free where its count is not positive.  The calls below keep tables and counts on the device and read them there;
  * they are functions of their inputs (outputs do not overlap inputs unless said otherwise), so a captured step runs on two sets of them in turn. */
 
-/* f8_attend_paged for requests that begin alike: requests first[g] .. first[g + 1] - 1 (first [groups + 1], ascending; requests in no
- * group are their own) have their first shared[g] tokens in common, which are read once for all of them.  The result is f8_attend_paged's
- * of the same arguments but for rounding, wherever the pages that the members' rows list hold the same first shared[g] tokens, in one page or in copies: they are read through the
- * first member that has all of them (a shorter one reads its own).  first and shared are read on the device; weights of
- * 16-bit caches are rounded once to the cache's type, and an infinite value shows where its weight is at least 2^-40 (f16) or 2^-86 (bf16) of the
- * largest one; below that the result may be NaN.  Workspace: f8_attend_shared_workspace_bytes(batch, groups, q_heads, heads, dim, max_len) bytes. */
+/* f8_attend_paged for requests that begin alike: requests first[g] .. first[g + 1] - 1 (first [groups + 1], ascending; requests in no group are
+ * their own) have their first shared[g] tokens in common, which are read once for all of them.  The result is f8_attend_paged's of the same arguments
+ * but for rounding, wherever the pages that the members' rows list hold the same first shared[g] tokens, in one page or in copies: they are read
+ * through the first member that has all of them (a shorter one reads its own).  first and shared are read on the device.  With max_len up to 512, or
+ * without groups, the call is f8_attend_paged's, bit for bit.  Otherwise weights of 16-bit caches are rounded once to the cache's type
+ * (f8_attend_paged: in two parts), relative 2^-11 or 2^-8 each, f16 ones below 2^-21 of the largest by up to 2^-31 of it, and an infinite value shows
+ * where its weight is at least 2^-40 (f16) or 2^-86 (bf16) of the largest one; below that the result may be NaN.  Workspace:
+ * f8_attend_shared_workspace_bytes(batch, groups, q_heads, heads, dim, max_len) bytes. */
 size_t f8_attend_shared_workspace_bytes(int batch, int groups, int q_heads, int kv_heads, int dim, int max_len);
 f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cache, const float *k_scale, const float *v_scale,
                            const int32_t *table, const int32_t *lens, const int32_t *first, const int32_t *shared, void *out,
@@ -485,10 +487,13 @@ f8_status f8_attend_shared(const void *q, const void *k_cache, const void *v_cac
 /* Beam search's selection.  With logits [batch][beams][vocab] (`type` real, rows ld elements apart, beam i of prompt b is row b * beams + i), the beams'
  * scores [batch][beams] and done [batch][beams] (0 or not; NULL: none is),
  *     S[b][i][t] = scores[b][i] + logits[b][i][t] - log sum_u exp logits[b][i][u],
- * of a beam that is done scores[b][i] for t = eos and -infinity for every other t.  The `keep` largest S of each prompt, in
- * descending order and ties in that of (i, t), come as score [batch][keep] (32 bits; formed and compared in 64), parent [batch][keep] = b * beams + i
- * and token [batch][keep].  A beam whose logits are all -infinity has S of -infinity; one with a NaN or +infinity among its
- * logits or as its score has S of NaN throughout, which stands above every number.  Logits of a beam that is done are not read.
+ * of a beam that is done scores[b][i] for t = eos and -infinity for every other t.  The `keep` largest S of each prompt, in descending order and ties
+ * in that of (i, t), come as score [batch][keep] (32 bits), parent [batch][keep] = b * beams + i and token [batch][keep].  S is put together and
+ * compared in 64 bits; its log sum is off by up to 2^-17, because the exponentials are taken, and 16 of them added, in 32.  So tokens of one beam
+ * come in the exact order of their logits (the larger one first also where 64 bits give both the same finite S), beams of the same score and the same row
+ * tie exactly, and others whose S differ by less than the error may change places: a row whose logits are another's in another order ties with it but
+ * for that.  A beam whose logits are all -infinity has S of -infinity; one with a NaN or +infinity among its logits or as its score has S of NaN
+ * throughout, which stands above every number.  Logits of a beam that is done are not read.
  * 1 <= keep <= F8_BEAM_MAX_KEEP, keep <= beams * vocab, beams * keep * ceil(vocab / 16384) <= 8192 and beams <= 1024 (else F8_ERR_UNSUPPORTED).
  * Workspace: f8_beam_workspace_bytes(batch, beams, vocab, keep) bytes. */
 #define F8_BEAM_MAX_KEEP 64
@@ -501,19 +506,19 @@ size_t f8_beam_workspace_bytes(int batch, int beams, int vocab, int keep);
 f8_status f8_beam_step(const void *logits, const float *scores, const uint8_t *done, float *score, int32_t *parent, int32_t *token,
                        const f8_beam_desc *d, void *workspace, size_t workspace_bytes, void *stream);
 
-/* One step of the requests that share a cache: request b goes on from request parent[b] (outside 0 .. batch - 1: it ends) by `grow` tokens
- * (grow and cols * page_size: up to 0x7fff0000).
- * table [batch][cols], lens and refs [pages] are those before the step, table_out, lens_out and refs_out those after it:
+/* One step of the requests that share a cache: request b goes on from request parent[b] (outside 0 .. batch - 1: it ends) by `grow` tokens (grow
+ * and cols * page_size: up to 0x7fff0000).  table [batch][cols], lens and refs [pages] are those before the step, table_out, lens_out and refs_out
+ * those after it:
  *   - a request holds the pages of its parent, ceil(lens / page_size) entries of the table's row (entries outside 0 .. pages - 1 are
  *     carried along and hold nothing); pages that nobody holds any more are free from then on, for this step too;
  *   - a page that is not full, that requests will write into (grow > 0), stays with the lowest of them if they are all that hold it; for the others it is
  *     copied: into a new page, with a line of moves;
  *   - new pages for these copies and for the tokens that find no room are the free ones of the lowest index, request by request, the copy's first.
- * Row b of table_out holds the pages and then -1.  slots [batch][grow] say where f8_kv_append puts the new tokens (-1: nowhere), moves [batch][3] what
- * f8_kv_copy has to copy before: (page, new page, tokens), behind the last one (-1, -1, 0).  info[0]: number of moves; info[1]: pages that were wanted
- * and not there, in the pool or as columns of the table.  Entries of these are -1 (of a copy: its tokens are lost), lens_out counts their tokens up to cols *
- * page_size all the same.  batch 0: nothing is launched and nothing written, refs are the counts after the step too (the
- * Python call copies them).  Workspace: f8_kv_fork_workspace_bytes(batch, pages) bytes. */
+ * Row b of table_out holds the pages and then -1.  slots [batch][grow] say where f8_kv_append puts the new tokens (-1: nowhere), moves [batch][3]
+ * what f8_kv_copy has to copy before: (page, new page, tokens), behind the last one (-1, -1, 0).  info[0]: number of moves; info[1]: pages that were
+ * wanted and not there, in the pool or as columns of the table.  Entries of these are -1 (of a copy: its tokens are lost), lens_out counts their
+ * tokens up to cols * page_size all the same.  batch 0: nothing is launched and nothing written, refs are the counts after the step too (the Python
+ * call copies them).  Workspace: f8_kv_fork_workspace_bytes(batch, pages) bytes. */
 typedef struct {
   int32_t batch, cols, pages, page_size, grow;
   int64_t table_ld, out_ld;          /* entries */

@@ -10,6 +10,11 @@
 // lower bound of the keep-th largest, which few elements reach (16 of 16384 random ones: about 45).  Those go to a list in LDS, as keys of which no
 // two are alike (value, then lowest index), and each one's place is the number of keys above it.  Where more reach it than
 // the list holds (many alike), the bound is the keep-th largest of the threads' own largest keys: what passes then are elements of `keep` threads.
+// (A vocabulary that a mask leaves a thousandth of takes that way, because a group without any other element has the mask's value as its largest:
+// 64 prompts of 8 beams, none done, 131072 bf16 logits, keep 16 then take 219 us instead of 52; with half of it masked 52.)  Placing the list
+// compares 64 bits for every two elements of it: with keep 64 the same prompts take 124 us, a single one 58 (keep 16: 27, 8: 20).
+//
+// The exponentials are taken in 32 bits and 16 of them added there, then on in 64: the log sum is good to 2^-17, and S no better.
 #include "tokens_device.h"
 #include "tokens_host.h"
 
@@ -193,7 +198,7 @@ __global__ __launch_bounds__(THREADS, NV < 8 ? 6 : 4) void beam_rows_kernel(Beam
   int n = count;
   if (n > most) {
     // the bound is the keep-th largest of the threads' own largest keys: what passes then are elements of `keep` threads (read once more, one
-    // by one: this way is seldom taken and must not cost the other one registers)
+    // by one: this way must not cost the other one registers)
     auto each = [&](auto f) {
 #pragma unroll 1
       for (int i = 0; i < NV; ++i)

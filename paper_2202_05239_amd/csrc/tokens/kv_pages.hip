@@ -7,7 +7,9 @@
 // Bound by latencies: a few hundred kilobytes at most, in phases that wait for one another.  What fits one workgroup's LDS is one launch: 64
 // requests of up to 2048 tokens fork in 14 us (49 with the counts in memory), a pool of 1001 pages is compacted in 4.4 us (three launches
 // take 11).  More takes the phases as launches: 512 requests of up to 32768 tokens fork in 25 us, 262144 pages with 512 rows of 513 entries
-// are compacted in 18.
+// are compacted in 18.  The search for free pages is one workgroup's and ends where enough are found: 512 new pages out of 262144, 97 % in use,
+// take 29 us where the free ones lie all over the pool and 160 where they lie at its end, as behind a compaction (of 65536: 29 and 51, of
+// 20000: 27 and 26).
 #include "tokens_device.h"
 #include "tokens_host.h"
 
